@@ -495,12 +495,173 @@ int kv_adapt_order(const kv_adapt_t *a, int group);
 int kv_adapt_update(kv_adapt_t *a, const kv_pipe_stats_t *stats);
 
 /* ------------------------------------------------------------------------------------------ */
+/* A serving step over a cache of 16, 8 or 4 bits (stream-ordered; nothing here blocks or     */
+/* allocates, and every call may be captured into a HIP graph)                                */
+/* ------------------------------------------------------------------------------------------ */
+
+/*
+ * Cache formats.  A block-scaled cache holds, for every 32 elements of a head's row (d = 0..31, 32..63, ...), their codes and one
+ * power of two 2^e as the byte e + 127:
+ *   KV_FORMAT_FP8  a byte per element, e4m3 (largest value 448): head_dim + head_dim/32 bytes per row
+ *   KV_FORMAT_FP4  4 bits per element, e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6), the even element in the lower half of a byte:
+ *                  head_dim/2 + head_dim/32 bytes per row
+ * e is the smallest integer in [-127, 127] with which no element of the block exceeds the largest code; an element is x * 2^-e, rounded to
+ * the nearest code, ties to even; its value is code * 2^e, exactly.  A block that holds an infinity or a NaN has the byte 255 and
+ * stands for NaN throughout.  Magnitudes that would round up beyond the plan's 16-bit type are cached as the largest that do not: fp16 61440 (FP8),
+ * 49152 (FP4), bf16 1.875 * 2^127, 1.5 * 2^127.  KV_FORMAT_16 is the plain cache of 16-bit rows.
+ */
+#define KV_FORMAT_16 0
+#define KV_FORMAT_FP8 1
+#define KV_FORMAT_FP4 2
+
+/*
+ * The scales of a block-scaled cache.  Its codes are the buffers of a kv_view_t whose 16-bit elements hold 2 (FP8) or 4 (FP4)
+ * codes: strides and layer_bytes are those of rows of head_dim/2 or head_dim/4 elements (so a plan of that head_dim packs, offloads and
+ * reloads the codes like any other cache).  Strides here are bytes; a row's head_dim/32 bytes lie side by side.
+ * In KV_LAYOUT_PAGED stride_b goes from block to block (the view's table applies), stride_h from head to head, stride_s from token to token.
+ * The calls below take the plan of the cache's real head_dim and dtype (the 16-bit type of rows written, read and attended with), and NULL in
+ * place of a kv_blocks_t for KV_FORMAT_16.
+ */
+typedef struct kv_blocks {
+    int32_t format;         /* KV_FORMAT_FP8 | KV_FORMAT_FP4 */
+    int32_t n_layers;       /* entries in k_scales / v_scales */
+    void *const *k_scales;  /* host array of device pointers */
+    void *const *v_scales;  /* host array of device pointers */
+    uint64_t layer_bytes;   /* bytes addressable behind every pointer (bounds check) */
+    int64_t stride_b, stride_h, stride_s;
+} kv_blocks_t;
+
+/*
+ * Rotary positions.  Element pairs of a head's first rot_dim elements, (d, d + rot_dim/2) in KV_ROPE_HALF or (2d, 2d + 1) in
+ * KV_ROPE_PAIRS, are turned by position * frequency_d; the others are left alone.  table holds cosine and sine of every
+ * position and pair, so any schedule of frequencies and any factor on the rotated part can be expressed; kv_rope_table fills it for the usual ones.
+ */
+#define KV_ROPE_HALF 0
+#define KV_ROPE_PAIRS 1
+typedef struct kv_rope {
+    const float *table; /* device [n_pos, rot_dim/2, 2] fp32, 16-byte aligned */
+    int32_t n_pos;      /* positions the table holds */
+    int32_t rot_dim;    /* a multiple of 16, at most head_dim */
+    int32_t style;      /* KV_ROPE_HALF | KV_ROPE_PAIRS */
+    int32_t reserved;
+} kv_rope_t;
+
+#define KV_ROPE_PLAIN 0      /* frequency_d = base^(-2d/rot_dim) */
+#define KV_ROPE_LINEAR 1     /* plain frequencies / factor */
+#define KV_ROPE_BASE 2       /* the base grows so that the longest wave is factor times as long: base * factor^(rot_dim/(rot_dim-2)) */
+#define KV_ROPE_WAVELENGTH 3 /* by the number of turns t = trained_pos * frequency_d / 2 pi within the trained context: frequencies with t <= low are
+                                divided by factor, with t >= high kept, in between a mixture that is linear in t */
+#define KV_ROPE_INDEX 4      /* the same, the mixture linear in d: it ends at the (rounded) d at which t = high and t = low */
+typedef struct kv_rope_desc {
+    int32_t n_pos;
+    int32_t rot_dim;
+    int32_t scaling;     /* KV_ROPE_PLAIN .. KV_ROPE_INDEX */
+    int32_t trained_pos; /* WAVELENGTH, INDEX: positions of the context before it was stretched */
+    double base;         /* > 1 */
+    double factor;       /* >= 1 (not read in KV_ROPE_PLAIN) */
+    double low, high;    /* WAVELENGTH, INDEX: 0 < low < high */
+    double magnitude;    /* factor on every cosine and sine; 0 = 1 */
+} kv_rope_desc_t;
+
+/* kv_rope_table -- cosines and sines of a schedule into host memory [n_pos, rot_dim/2, 2] fp32 (double precision angles, rounded once).
+ * KV_ENOSPC if bytes is too small.  Host only. */
+int kv_rope_table(const kv_rope_desc_t *desc, float *table_host, size_t bytes);
+
+/*
+ * kv_rope -- rotary positions of n_tok rows of n_heads heads: out[t,h,:] = rotated x[t,h,:] by positions[t].
+ * fp32 arithmetic (each product rounded), rounded to 16 bits once.  transposed != 0 turns the other way: the gradient of x from that of out, and,
+ * where the table has no factor, the inverse.  out may be x itself with equal strides; other overlaps are not allowed.  A position outside [0, n_pos) gives
+ * NaN in the rotated part.  head_dim: a multiple of 16; strides: elements, multiples of 8; pointers: 16-byte aligned.
+ */
+typedef struct kv_rope_args {
+    const void *x; /* device 16-bit */
+    void *out;     /* device 16-bit */
+    int64_t x_stride_t, x_stride_h, out_stride_t, out_stride_h;
+    const int32_t *positions; /* device [n_tok] */
+    int32_t n_tok, n_heads, head_dim;
+    int32_t dtype;      /* KV_F16 | KV_BF16 */
+    int32_t transposed; /* 0 | 1 */
+    int32_t reserved;
+} kv_rope_args_t;
+int kv_rope(const kv_rope_t *rope, const kv_rope_args_t *args, void *hip_stream);
+
+/*
+ * kv_cache_write -- rows of new tokens into one layer of a cache: K (rotated where rope is given, and rounded to 16 bits) and V, as 16-bit rows
+ * or as blocks.  Row t of k and v goes to token tok_slot[t] of sequence tok_seq[t].  A row whose sequence is outside
+ * [0, batch) or whose token is outside the cache (s_alloc rows; the table's blocks) or in a block id outside the pool is skipped; two rows of a
+ * call must not go to one place.  The view's seq_lens are not read.  A rotary position outside [0, n_pos) gives NaN.
+ * head_dim: a multiple of 32; strides: elements, multiples of 8; k and v: 16-byte aligned.
+ */
+typedef struct kv_write_args {
+    const void *k, *v;   /* device [n_tok, H, D] 16-bit, the plan's dtype */
+    int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;
+    const int32_t *tok_seq, *tok_slot; /* device [n_tok] */
+    const kv_rope_t *rope;             /* host, nullable */
+    const int32_t *positions;          /* device [n_tok]; with rope */
+    int32_t n_tok;
+    int32_t reserved;
+} kv_write_args_t;
+int kv_cache_write(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_write_args_t *args, void *hip_stream);
+
+/*
+ * kv_cache_read -- the inverse: rows of one layer of a cache as 16-bit values.  Row t of k and v is token tok_slot[t] of sequence
+ * tok_seq[t]; rows that kv_cache_write would skip are left as they are.  A place may be read any number of times.
+ */
+typedef struct kv_read_args {
+    void *k, *v; /* device [n_tok, H, D] 16-bit, the plan's dtype */
+    int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;
+    const int32_t *tok_seq, *tok_slot; /* device [n_tok] */
+    int32_t n_tok;
+    int32_t reserved;
+} kv_read_args_t;
+int kv_cache_read(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_read_args_t *args, void *hip_stream);
+
+/*
+ * kv_tree_masks -- which drafted tokens each token of a tree sees: itself and its ancestors.  parents (host [n]): parents[i] < i is the token
+ * that token i follows, -1 for one that follows the context.  masks (host [n, words], nullable): bit i % 64 of word i / 64 of
+ * row j is set where j sees i; depths (host [n], nullable): 0 for a token that follows the context (its rotary position is context length + depth).
+ * KV_ERANGE for a parent out of order or 64 * words < n.  Host only.
+ */
+int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t *masks, int32_t *depths);
+
+/*
+ * kv_tree_attn -- attention of drafted tokens over one layer of a cache.  Sequence b has T_b = tok_first[b+1] - tok_first[b] drafted
+ * tokens (0..KV_TREE_MAX), whose K and V are rows len_b .. len_b + T_b - 1 of the cache (kv_cache_write puts them there); len_b = the view's seq_lens[b]
+ * (its context; host and device arrays hold the same values, as in kv_decode_attn).  For drafted token i of sequence b, t = tok_first[b] + i:
+ *   out[t,hq,:] = softmax_j(q[t,hq,:] . K[b,h,j,:] * scale) V[b,h,j,:],  h = hq / (H_q/H),
+ * over the context j < len_b and those j = len_b + m whose bit m is set in mask[t] (without a mask: m <= i, a causal chain; a single token per
+ * sequence is plain decoding).  A row that sees nothing yields zeros; what a row does not see has no effect on it, infinities and NaNs included.
+ * fp32 scores, maxima and sums; probabilities enter the product with V in parts whose sum is the fp32 value (out_dtype KV_OUT_F32), or rounded to the
+ * plan's 16-bit type, and in that rounded form also their sum (KV_OUT_SAME: each output is rounded to that type anyway).
+ * head_dim 64, 128 or 256.  q: the plan's dtype; q strides: elements, multiples of 8; out strides: elements; q and workspace 16-byte aligned.
+ * workspace: at least kv_tree_attn_workspace() bytes lets the library split sequences as it likes; with less it splits less.
+ */
+#define KV_TREE_MAX 256
+typedef struct kv_tree_args {
+    const void *q; /* device [n_tok, H_q, D] */
+    void *out;     /* device [n_tok, H_q, D], fp32 or 16-bit (out_dtype) */
+    int64_t q_stride_t, q_stride_h, out_stride_t, out_stride_h;
+    const int32_t *tok_first_host; /* host [B+1]: first[0] = 0, ascending */
+    const int32_t *tok_first_dev;  /* device [B+1], the same values */
+    const uint64_t *mask;          /* device [n_tok, mask_words], nullable */
+    int32_t mask_words;            /* words per row: 64 * mask_words >= every T_b */
+    int32_t out_dtype;             /* KV_OUT_* */
+    int32_t n_splits;              /* 0 = choose; at most 128 */
+    float scale;                   /* 0 = 1 / sqrt(D) */
+} kv_tree_args_t;
+int kv_tree_attn(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *args, void *workspace,
+                 size_t ws_bytes, void *hip_stream);
+/* Bytes of workspace with which kv_tree_attn splits up to n_tok drafted tokens of the batch over contexts of up to max_len tokens as it likes. */
+size_t kv_tree_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
+
+/* ------------------------------------------------------------------------------------------ */
 int kv_last_hip_error(void);       /* hipError_t of the last KV_EHIP on this thread, else 0 */
 const char *kv_strerror(int code); /* static string */
 int kv_abi_version(void);
 /* sizeof of the ABI struct number `which` as this library was compiled (0 kv_plan_desc_t, 1 kv_plan_info_t,
  * 2 kv_extent_t, 3 kv_cmd_t, 4 kv_view_t, 5 kv_attn_args_t, 6 kv_pipe_opts_t, 7 kv_pipe_stats_t,
- * 8 kv_append_stats_t, 9 kv_adapt_t, 10 kv_chunk_trace_t; 0 for any other number): lets a binding verify its own
+ * 8 kv_append_stats_t, 9 kv_adapt_t, 10 kv_chunk_trace_t, 11 kv_blocks_t, 12 kv_rope_t, 13 kv_rope_desc_t, 14 kv_rope_args_t,
+ * 15 kv_write_args_t, 16 kv_read_args_t, 17 kv_tree_args_t; 0 for any other number): lets a binding verify its own
  * layouts. */
 size_t kv_abi_sizeof(int which);
 

@@ -33,6 +33,10 @@ KV_PIPE_NO_PACING = 8
 KV_ATTN_SCRATCH_BYTES = 8 << 20
 KV_COPY_AUTO, KV_COPY_MEMCPY, KV_COPY_KERNEL = 0, 1, 2
 KV_ORDER_CROSS, KV_ORDER_INTRA = 0, 1
+KV_FORMAT_16, KV_FORMAT_FP8, KV_FORMAT_FP4 = 0, 1, 2
+KV_ROPE_HALF, KV_ROPE_PAIRS = 0, 1
+KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BASE, KV_ROPE_WAVELENGTH, KV_ROPE_INDEX = 0, 1, 2, 3, 4
+KV_TREE_MAX = 256
 
 EXPORTS = [
     "kv_layout_plan", "kv_plan_destroy", "kv_plan_info", "kv_plan_tensor", "kv_plan_seq_base",
@@ -40,7 +44,8 @@ EXPORTS = [
     "kv_decode_attn_workspace", "kv_pipeline_run", "kv_last_hip_error", "kv_strerror", "kv_abi_version",
     "kv_append_tokens", "kv_budget", "kv_plan_trim", "kv_adapt_init", "kv_adapt_order", "kv_adapt_update",
     "kv_abi_sizeof", "kv_budget_sample", "kv_decode_attn_static", "kv_offload_pack_layers", "kv_reload_unpack_layers",
-    "kv_decode_attn_splits",
+    "kv_decode_attn_splits", "kv_rope_table", "kv_rope", "kv_cache_write", "kv_cache_read", "kv_tree_masks", "kv_tree_attn",
+    "kv_tree_attn_workspace",
 ]
 
 
@@ -118,6 +123,49 @@ class kv_append_stats_t(C.Structure):
     _fields_ = [("n_cmds", C.c_uint32), ("n_rmw_reads", C.c_uint32), ("blocks_written", C.c_uint64)]
 
 
+class kv_blocks_t(C.Structure):
+    _fields_ = [("format", C.c_int32), ("n_layers", C.c_int32), ("k_scales", C.POINTER(C.c_void_p)),
+                ("v_scales", C.POINTER(C.c_void_p)), ("layer_bytes", C.c_uint64),
+                ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_s", C.c_int64)]
+
+
+class kv_rope_t(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("style", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class kv_rope_desc_t(C.Structure):
+    _fields_ = [("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("scaling", C.c_int32), ("trained_pos", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("magnitude", C.c_double)]
+
+
+class kv_rope_args_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("x_stride_t", C.c_int64), ("x_stride_h", C.c_int64),
+                ("out_stride_t", C.c_int64), ("out_stride_h", C.c_int64), ("positions", C.c_void_p),
+                ("n_tok", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("transposed", C.c_int32), ("reserved", C.c_int32)]
+
+
+class kv_write_args_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride_t", C.c_int64), ("k_stride_h", C.c_int64),
+                ("v_stride_t", C.c_int64), ("v_stride_h", C.c_int64), ("tok_seq", C.c_void_p), ("tok_slot", C.c_void_p),
+                ("rope", C.POINTER(kv_rope_t)), ("positions", C.c_void_p), ("n_tok", C.c_int32), ("reserved", C.c_int32)]
+
+
+class kv_read_args_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride_t", C.c_int64), ("k_stride_h", C.c_int64),
+                ("v_stride_t", C.c_int64), ("v_stride_h", C.c_int64), ("tok_seq", C.c_void_p), ("tok_slot", C.c_void_p),
+                ("n_tok", C.c_int32), ("reserved", C.c_int32)]
+
+
+class kv_tree_args_t(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride_t", C.c_int64), ("q_stride_h", C.c_int64),
+                ("out_stride_t", C.c_int64), ("out_stride_h", C.c_int64), ("tok_first_host", C.POINTER(C.c_int32)),
+                ("tok_first_dev", C.c_void_p), ("mask", C.c_void_p), ("mask_words", C.c_int32), ("out_dtype", C.c_int32),
+                ("n_splits", C.c_int32), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -164,6 +212,14 @@ def lib() -> C.CDLL:
         L.kv_adapt_init.argtypes = [C.POINTER(kv_adapt_t)]
         L.kv_adapt_order.argtypes = [C.POINTER(kv_adapt_t), i]
         L.kv_adapt_update.argtypes = [C.POINTER(kv_adapt_t), C.POINTER(kv_pipe_stats_t)]
+        L.kv_rope_table.argtypes = [C.POINTER(kv_rope_desc_t), vp, C.c_size_t]
+        L.kv_rope.argtypes = [vp, C.POINTER(kv_rope_args_t), vp]
+        L.kv_cache_write.argtypes = [vp, vp, vp, i, C.POINTER(kv_write_args_t), vp]
+        L.kv_cache_read.argtypes = [vp, vp, vp, i, C.POINTER(kv_read_args_t), vp]
+        L.kv_tree_masks.argtypes = [C.POINTER(C.c_int32), i, i, vp, vp]
+        L.kv_tree_attn.argtypes = [vp, vp, vp, i, C.POINTER(kv_tree_args_t), vp, C.c_size_t, vp]
+        L.kv_tree_attn_workspace.argtypes = [vp, i, i]
+        L.kv_tree_attn_workspace.restype = C.c_size_t
         L.kv_strerror.restype = C.c_char_p
         L.kv_strerror.argtypes = [i]
         L.kv_abi_sizeof.argtypes = [i]
@@ -173,7 +229,8 @@ def lib() -> C.CDLL:
         # the ctypes mirrors must have the library's own struct sizes
         for which, t in enumerate((kv_plan_desc_t, kv_plan_info_t, kv_extent_t, kv_cmd_t, kv_view_t, kv_attn_args_t,
                                    kv_pipe_opts_t, kv_pipe_stats_t, kv_append_stats_t, kv_adapt_t,
-                                   kv_chunk_trace_t)):
+                                   kv_chunk_trace_t, kv_blocks_t, kv_rope_t, kv_rope_desc_t, kv_rope_args_t,
+                                   kv_write_args_t, kv_read_args_t, kv_tree_args_t)):
             if L.kv_abi_sizeof(which) != C.sizeof(t):
                 raise RuntimeError(f"{t.__name__}: binding has {C.sizeof(t)} bytes, library {L.kv_abi_sizeof(which)}")
         _lib = L
@@ -424,6 +481,157 @@ def kv_decode_attn_static(plan: Plan, kv: View, layer: int, q, out, out_dtype: i
     rc = (_lib or lib()).kv_decode_attn_static(plan.handle, kv._ref, layer, q.data_ptr(), out.data_ptr(), out_dtype, n_splits, _caller_stream(stream))
     if rc:
         raise KVError(rc, "kv_decode_attn_static")
+
+
+# ------------------------------------------------------------------------------------------ a cache of 16, 8 or 4 bits
+class Blocks:
+    """kv_blocks_t plus the Python objects that keep its host arrays and device tensors alive."""
+
+    def __init__(self, struct: kv_blocks_t, keep):
+        self.struct, self._keep = struct, keep
+        self._ref = C.byref(struct)
+
+
+def scale_blocks(format: int, k_scales, v_scales) -> Blocks:
+    """Scales of a block-scaled cache: per-layer uint8 tensors [B, H, S_alloc, D/32], or [n_pool, H, block_tokens, D/32] beside a
+    paged view, last dim contiguous.  The codes' view is made with bhsd_view / paged_view of code tensors seen as 16-bit
+    elements: [..., D] or [..., D/2] uint8 tensors' .view(torch.int16)."""
+    t0 = k_scales[0]
+    assert t0.dim() == 4 and t0.stride(3) == 1 and t0.element_size() == 1
+    for t in list(k_scales) + list(v_scales):
+        assert t.shape == t0.shape and t.stride() == t0.stride() and t.dtype == t0.dtype
+    kp, vp = _ptr_array(k_scales), _ptr_array(v_scales)
+    span = sum((t0.shape[i] - 1) * t0.stride(i) for i in range(4)) + 1
+    s = kv_blocks_t(format, len(k_scales), kp, vp, span, t0.stride(0), t0.stride(1), t0.stride(2))
+    return Blocks(s, (k_scales, v_scales, kp, vp))
+
+
+class Rope:
+    """Rotary positions: a device table [n_pos, rot_dim/2, 2] (kv_rope_table) and how a head's elements pair up."""
+
+    def __init__(self, table, style: int = KV_ROPE_HALF):
+        import torch
+        assert table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous() and table.dtype == torch.float32
+        self.table = table
+        self.struct = kv_rope_t(table.data_ptr(), table.shape[0], 2 * table.shape[1], style, 0)
+        self._ref, self._ptr = C.byref(self.struct), C.pointer(self.struct)
+
+
+def kv_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, scaling: int = KV_ROPE_PLAIN, factor: float = 1.0, trained_pos: int = 0,
+                  low: float = 1.0, high: float = 4.0, magnitude: float = 1.0):
+    """Cosines and sines of a schedule of frequencies, as a CPU tensor [n_pos, rot_dim/2, 2]."""
+    import torch
+    d = kv_rope_desc_t(n_pos, rot_dim, scaling, trained_pos, base, factor, low, high, magnitude)
+    t = torch.empty((max(0, n_pos), max(0, rot_dim // 2), 2), dtype=torch.float32)
+    _check(lib().kv_rope_table(C.byref(d), t.data_ptr() or None, t.nbytes), "kv_rope_table")
+    return t
+
+
+def _kv_dtype(t) -> int:
+    import torch
+    if t.dtype == torch.float16:
+        return KV_F16
+    if t.dtype == torch.bfloat16:
+        return KV_BF16
+    raise KVError(KV_EINVAL, f"rows of {t.dtype}")
+
+
+def kv_rope(rope: Rope, positions, x, out, transposed: bool = False, stream=None) -> None:
+    """x, out: [n_tok, heads, head_dim], last dim contiguous; positions: device int32 [n_tok].  out may be x."""
+    n, h, d = x.shape
+    xt, xh, xd = x.stride()
+    ot, oh, od = out.stride()
+    if xd != 1 or od != 1 or out.shape != x.shape or out.dtype != x.dtype or positions.numel() < n:
+        raise KVError(KV_EINVAL, "kv_rope")
+    a = kv_rope_args_t(x.data_ptr(), out.data_ptr(), xt, xh, ot, oh, positions.data_ptr(), n, h, d, _kv_dtype(x), 1 if transposed else 0, 0)
+    rc = (_lib or lib()).kv_rope(rope._ref, C.byref(a), _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_rope")
+
+
+def _row_pair(k, v, tok_seq, tok_slot, where):
+    (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
+    if kd != 1 or vd != 1 or k.shape != v.shape or k.dtype != v.dtype or tok_seq.numel() < k.shape[0] or tok_slot.numel() < k.shape[0]:
+        raise KVError(KV_EINVAL, where)
+    return kt, kh, vt, vh
+
+
+def _check_rows(plan: Plan, k, where):
+    if k.shape[1] != plan.info.n_kv_heads or k.shape[2] != plan.info.head_dim or _kv_dtype(k) != plan.info.dtype:
+        raise KVError(KV_EINVAL, where)
+
+
+def kv_cache_write(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, k, v, tok_seq, tok_slot, rope: Optional[Rope] = None,
+                   positions=None, stream=None) -> None:
+    """k, v: [n_tok, H, D], the plan's dtype, last dim contiguous; tok_seq, tok_slot, positions: device int32 [n_tok]."""
+    strides = _row_pair(k, v, tok_seq, tok_slot, "kv_cache_write")
+    _check_rows(plan, k, "kv_cache_write")
+    if rope is not None and (positions is None or positions.numel() < k.shape[0]):
+        raise KVError(KV_EINVAL, "kv_cache_write")
+    a = kv_write_args_t(k.data_ptr(), v.data_ptr(), *strides, tok_seq.data_ptr(), tok_slot.data_ptr(), rope._ptr if rope is not None else None,
+                        positions.data_ptr() if positions is not None else None, k.shape[0], 0)
+    rc = (_lib or lib()).kv_cache_write(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_cache_write")
+
+
+def kv_cache_read(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tok_seq, tok_slot, k_out, v_out, stream=None) -> None:
+    """k_out, v_out: [n_tok, H, D], the plan's dtype, last dim contiguous; tok_seq, tok_slot: device int32 [n_tok]."""
+    strides = _row_pair(k_out, v_out, tok_seq, tok_slot, "kv_cache_read")
+    _check_rows(plan, k_out, "kv_cache_read")
+    a = kv_read_args_t(k_out.data_ptr(), v_out.data_ptr(), *strides, tok_seq.data_ptr(), tok_slot.data_ptr(), k_out.shape[0], 0)
+    rc = (_lib or lib()).kv_cache_read(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_cache_read")
+
+
+def kv_tree_masks(parents: Sequence[int], words: int = 0):
+    """(masks int64 [n, words], depths int32 [n]) of one sequence's drafted tokens, as CPU tensors; words 0 = as many as n needs."""
+    import torch
+    n = len(parents)
+    words = words or max(1, (n + 63) // 64)
+    p = (C.c_int32 * max(1, n))(*[int(x) for x in parents])
+    masks, depths = torch.zeros((n, words), dtype=torch.int64), torch.zeros(n, dtype=torch.int32)
+    _check(lib().kv_tree_masks(p, n, words, masks.data_ptr() or None, depths.data_ptr() or None), "kv_tree_masks")
+    return masks, depths
+
+
+class TreeBatch:
+    """Which rows of a batch's drafted tokens belong to which sequence, and what they see (kv_tree_args_t's first and mask)."""
+
+    def __init__(self, first, first_dev, mask):
+        self.first, self.first_dev, self.mask, self.n_tok = first, first_dev, mask, first[len(first) - 1]
+        self._ptr = C.cast(first, C.POINTER(C.c_int32))
+        self._fixed = (self._ptr, first_dev.data_ptr(), mask.data_ptr() if mask is not None else None, mask.shape[1] if mask is not None else 0)
+
+
+def tree_batch(tok_first: Sequence[int], tok_first_dev, mask=None) -> TreeBatch:
+    """tok_first (host) and tok_first_dev (device int32), both [B + 1]: sequence b's drafted tokens are rows tok_first[b] ..
+    tok_first[b + 1] - 1.  mask: device int64 [n_tok, words] (kv_tree_masks of every sequence, one after the other); None: each token follows the
+    one before it."""
+    first = (C.c_int32 * len(tok_first))(*[int(x) for x in tok_first])
+    if tok_first_dev.numel() != len(tok_first) or (mask is not None and (mask.dim() != 2 or not mask.is_contiguous() or mask.shape[0] < tok_first[-1])):
+        raise KVError(KV_EINVAL, "tree_batch")
+    return TreeBatch(first, tok_first_dev, mask)
+
+
+def kv_tree_attn_workspace(plan: Plan, n_tok: int, max_len: int) -> int:
+    return int(lib().kv_tree_attn_workspace(plan.handle, n_tok, max_len))
+
+
+def kv_tree_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tree: TreeBatch, q, out, out_dtype: int, n_splits: int, workspace,
+                 scale: float = 0.0, stream=None) -> None:
+    """q, out: [n_tok, H_q, D], last dim contiguous; q of the plan's dtype, out of that or fp32 (out_dtype)."""
+    (qt, qh, qd), (ot, oh, od) = q.stride(), out.stride()
+    info = plan.info
+    if qd != 1 or od != 1 or q.shape != out.shape or q.shape[0] < tree.n_tok or q.shape[1] != info.n_q_heads or q.shape[2] != info.head_dim \
+            or len(tree.first) != info.batch + 1 or _kv_dtype(q) != info.dtype or out.element_size() != (4 if out_dtype == KV_OUT_F32 else 2):
+        raise KVError(KV_EINVAL, "kv_tree_attn")
+    a = kv_tree_args_t(q.data_ptr(), out.data_ptr(), qt, qh, ot, oh, *tree._fixed, out_dtype, n_splits, scale)
+    rc = (_lib or lib()).kv_tree_attn(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), workspace.data_ptr(),
+                                      workspace.nbytes, _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_tree_attn")
 
 
 # ------------------------------------------------------------------------------------------ pipeline

@@ -1,0 +1,298 @@
+// Rows of new tokens into a cache of 16, 8 or 4 bits (K rotated on its way), and rows of it back as 16-bit values.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "cache.hpp"
+#include "launch.hpp"
+#include "rope.hpp"
+
+namespace {
+
+using namespace kvb;
+
+constexpr int kThreads = 256;
+
+struct RowParams {
+    CacheAddr c;
+    char *k, *v;                       // rows of the call, 16-bit (read: const in all but name)
+    long long k_st, k_sh, v_st, v_sh;  // bytes
+    const int *tok_seq, *tok_slot;
+    const float *table;                // rotary positions; null: none
+    const int *positions;
+    int n_pos, rot;
+    int n_heads, vectors;              // vectors of 8 elements in a head's row
+    unsigned n_items;                  // of K; as many of V in the grid's second row
+};
+
+// Maximum over the four lanes of a block.
+__device__ __forceinline__ unsigned quad_max(unsigned x)
+{
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, false));        // quad_perm [1,0,3,2]
+    return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, false));     // quad_perm [2,3,0,1]
+}
+
+// One lane's eight elements of a block that four neighbouring lanes hold: codes, and the scale's byte (the same in all four).
+template <bool BF16, int FORMAT>
+__device__ __forceinline__ u32x2 encode8(u32x4 x, unsigned *scale)
+{
+    // magnitudes as 16-bit patterns: their order is that of whole numbers, and what is not finite lies above what is
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7fffu, x[i] >> 16 & 0x7fffu));
+    top = quad_max(top);
+    constexpr unsigned kInf = BF16 ? 0x7f80u : 0x7c00u;
+    // 1.875 or 1.5 times the largest power of two: what lies above rounds to the next one, which is no number of the type
+    constexpr unsigned kMost = BF16 ? (FORMAT == KV_FORMAT_FP8 ? 0x7f70u : 0x7f40u) : (FORMAT == KV_FORMAT_FP8 ? 0x7b80u : 0x7a00u);
+    const float most = unpack2<BF16>(kMost)[0];
+    const bool fine = top < kInf;
+    const unsigned bits = __float_as_uint(unpack2<BF16>(min(top, kMost))[0]);
+    // the largest code is 1.75 * 2^8 or 1.5 * 2^2: one exponent more where the mantissa is larger
+    constexpr unsigned kLargest = FORMAT == KV_FORMAT_FP8 ? 0x600000u : 0x400000u;
+    const int e = (int)(bits >> 23) - (FORMAT == KV_FORMAT_FP8 ? 8 : 2) + ((bits & 0x7fffffu) > kLargest ? 1 : 0);
+    const unsigned byte = fine ? (unsigned)max(e, 0) : 255u;
+    *scale = byte;
+    const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 y = unpack2<BF16>(x[i]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            f[2 * i + j] = fine ? fminf(fmaxf(y[j], -most), most) * inv : 0.f;
+        }
+    }
+    if constexpr (FORMAT == KV_FORMAT_FP8) {
+        unsigned a = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false), b = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], 0, false);
+        a = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], a, true);
+        b = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], b, true);
+        return u32x2{a, b};
+    } else {
+        unsigned a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, f[0], f[1], 1.f, 0);
+        a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(a, f[2], f[3], 1.f, 1);
+        a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(a, f[4], f[5], 1.f, 2);
+        a = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(a, f[6], f[7], 1.f, 3);
+        return u32x2{a, 0};
+    }
+}
+
+// Item i: vector, head and row of K (blockIdx.y = 0) or V.  The four vectors of a block are neighbouring lanes: head_dim is a multiple of 32.
+struct Item {
+    unsigned v, h, t;
+    bool is_v;
+};
+__device__ __forceinline__ bool item_of(const RowParams &p, Item *it)
+{
+    const unsigned i = blockIdx.x * kThreads + threadIdx.x;
+    if (i >= p.n_items) return false;
+    const unsigned r = i / (unsigned)p.vectors;
+    *it = Item{i - r * (unsigned)p.vectors, r % (unsigned)p.n_heads, r / (unsigned)p.n_heads, blockIdx.y != 0};
+    return true;
+}
+__device__ __forceinline__ char *row_of(const RowParams &p, const Item &it)
+{
+    return (it.is_v ? p.v : p.k) + it.t * (it.is_v ? p.v_st : p.k_st) + it.h * (it.is_v ? p.v_sh : p.k_sh);
+}
+
+// Bytes of a vector of eight elements.
+constexpr int vector_bytes(int format) { return format_bits(format); }
+
+template <bool BF16, int FORMAT, bool PAIRS>
+__global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(RowParams p)
+{
+    Item it;
+    if (!item_of(p, &it)) return;
+    unsigned block, row;
+    if (!find_row(p.c, p.tok_seq[it.t], p.tok_slot[it.t], &block, &row)) return;  // a block's lanes share the row: all leave or none
+    const char *const src = row_of(p, it);
+    u32x4 x = *(const u32x4 *)(src + 16 * it.v);
+    if (p.table && !it.is_v && it.v < (unsigned)p.rot / 8) {
+        const int pos = p.positions[it.t];
+        if constexpr (PAIRS) {
+            const Angles<4> ang = load_angles<4>(p.table, p.n_pos, p.rot / 2, pos, 4 * it.v, 1.f);
+            turn_pairs<BF16>(x, ang, 0);
+        } else {
+            const unsigned half = (unsigned)p.rot / 16;  // vectors
+            const bool second = it.v >= half;
+            u32x4 other = *(const u32x4 *)(src + 16 * (second ? it.v - half : it.v + half));
+            const Angles<8> ang = load_angles<8>(p.table, p.n_pos, p.rot / 2, pos, 8 * (second ? it.v - half : it.v), 1.f);
+            u32x4 a = second ? other : x, b = second ? x : other;
+            turn_halves<BF16>(a, b, ang);
+            x = second ? b : a;
+        }
+    }
+    char *const dst = (char *)(it.is_v ? p.c.v : p.c.k) + block * p.c.sb + it.h * p.c.sh + row * p.c.ss + vector_bytes(FORMAT) * it.v;
+    if constexpr (FORMAT == KV_FORMAT_16) {
+        *(u32x4 *)dst = x;
+    } else {
+        unsigned byte;
+        const u32x2 w = encode8<BF16, FORMAT>(x, &byte);
+        if constexpr (FORMAT == KV_FORMAT_FP8) *(u32x2 *)dst = w;
+        else *(unsigned *)dst = w[0];
+        char *const z = (char *)(it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + it.h * p.c.zh + row * p.c.zs;
+        if (it.v % 4 == 0) z[it.v / 4] = (char)byte;
+    }
+}
+
+template <bool BF16, int FORMAT>
+__global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(RowParams p)
+{
+    Item it;
+    if (!item_of(p, &it)) return;
+    unsigned block, row;
+    if (!find_row(p.c, p.tok_seq[it.t], p.tok_slot[it.t], &block, &row)) return;
+    const char *const src = (it.is_v ? p.c.v : p.c.k) + block * p.c.sb + it.h * p.c.sh + row * p.c.ss + vector_bytes(FORMAT) * it.v;
+    u32x4 x;
+    if constexpr (FORMAT == KV_FORMAT_16) {
+        x = *(const u32x4 *)src;
+    } else {
+        const char *const z = (it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + it.h * p.c.zh + row * p.c.zs;
+        u32x2 w;
+        if constexpr (FORMAT == KV_FORMAT_FP8) w = *(const u32x2 *)src;
+        else w = u32x2{*(const unsigned *)src, 0};
+        x = decode8<BF16, FORMAT>(w, scale_operand((unsigned char)z[it.v / 4]));
+    }
+    *(u32x4 *)(row_of(p, it) + 16 * it.v) = x;
+}
+
+typedef void (*RowKernel)(RowParams);
+template <bool BF16>
+RowKernel write_kernel(int format, bool pairs)
+{
+    if (format == KV_FORMAT_FP8) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP8, true> : kv_cache_write_kernel<BF16, KV_FORMAT_FP8, false>;
+    if (format == KV_FORMAT_FP4) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP4, true> : kv_cache_write_kernel<BF16, KV_FORMAT_FP4, false>;
+    return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_16, true> : kv_cache_write_kernel<BF16, KV_FORMAT_16, false>;
+}
+template <bool BF16>
+RowKernel read_kernel(int format)
+{
+    if (format == KV_FORMAT_FP8) return kv_cache_read_kernel<BF16, KV_FORMAT_FP8>;
+    if (format == KV_FORMAT_FP4) return kv_cache_read_kernel<BF16, KV_FORMAT_FP4>;
+    return kv_cache_read_kernel<BF16, KV_FORMAT_16>;
+}
+
+// Checks of the rows of a call and the launch, shared by both directions; p holds the cache's place and the rotary table.
+int launch_rows(const kv_plan *pl, RowParams &p, RowKernel kernel, const void *k, const void *v, int64_t k_st, int64_t k_sh, int64_t v_st, int64_t v_sh,
+                const int32_t *tok_seq, const int32_t *tok_slot, const int32_t *positions, int n_tok, void *hip_stream)
+{
+    if (n_tok < 0 || k_st < 0 || k_sh < 0 || v_st < 0 || v_sh < 0 || ((k_st | k_sh | v_st | v_sh) & 7)) return KV_EINVAL;
+    if (n_tok == 0) return KV_OK;
+    if (!k || !v || !tok_seq || !tok_slot || (((uintptr_t)k | (uintptr_t)v) & 15)) return KV_EINVAL;
+    p.k_st = 2 * k_st; p.k_sh = 2 * k_sh; p.v_st = 2 * v_st; p.v_sh = 2 * v_sh;
+    p.n_heads = pl->H;
+    p.vectors = pl->D / 8;
+    const long long per_tok = (long long)p.n_heads * p.vectors;
+    const long long most = (1ll << 31) / per_tok;  // tokens of a launch: items are counted in 32 bits
+    if (most < 1) return KV_ERANGE;
+    for (long long t0 = 0; t0 < n_tok; t0 += most) {
+        const long long n = std::min<long long>(most, n_tok - t0);
+        p.k = (char *)k + t0 * p.k_st;
+        p.v = (char *)v + t0 * p.v_st;
+        p.tok_seq = tok_seq + t0;
+        p.tok_slot = tok_slot + t0;
+        p.positions = positions ? positions + t0 : nullptr;
+        p.n_items = (unsigned)(n * per_tok);
+        (void)launch_kernel(kernel, dim3((p.n_items + kThreads - 1) / kThreads, 2), dim3(kThreads), (hipStream_t)hip_stream, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
+    }
+    return KV_OK;
+}
+
+}  // namespace
+
+int kvb::cache_addr(const kv_plan *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const int *lens, const int *first, CacheAddr *c)
+{
+    *c = CacheAddr{};
+    if (!view->k_layers || !view->v_layers) return KV_EINVAL;
+    if (layer < 0 || layer >= p->L || layer >= view->n_layers) return KV_ERANGE;
+    const int format = blocks ? blocks->format : KV_FORMAT_16;
+    if (blocks) {
+        if (format != KV_FORMAT_FP8 && format != KV_FORMAT_FP4) return KV_EINVAL;
+        if (!blocks->k_scales || !blocks->v_scales) return KV_EINVAL;
+        if (layer >= blocks->n_layers) return KV_ERANGE;
+        if (p->D % kBlockElems != 0) return KV_EINVAL;
+        if (blocks->stride_b < 0 || blocks->stride_h < 0 || blocks->stride_s < 0) return KV_EINVAL;
+    }
+    c->k = (const char *)view->k_layers[layer];
+    c->v = (const char *)view->v_layers[layer];
+    if (!c->k || !c->v || (((uintptr_t)c->k | (uintptr_t)c->v) & 15)) return KV_EINVAL;
+    if (blocks) {
+        c->kz = (const char *)blocks->k_scales[layer];
+        c->vz = (const char *)blocks->v_scales[layer];
+        if (!c->kz || !c->vz) return KV_EINVAL;
+        c->zb = (uint64_t)blocks->stride_b; c->zh = (uint64_t)blocks->stride_h; c->zs = (uint64_t)blocks->stride_s;
+    }
+    const uint64_t row = (uint64_t)p->D * format_bits(format) / 8, zrow = (uint64_t)p->D / kBlockElems;
+    c->B = p->B;
+    // no byte past the buffer's end; the sums are kept in 128 bits
+    auto inside = [](uint64_t nb, uint64_t sb, uint64_t nh, uint64_t sh, uint64_t ns, uint64_t ss, uint64_t row_bytes, uint64_t bytes) {
+        const unsigned __int128 end = (unsigned __int128)(nb - 1) * sb + (unsigned __int128)(nh - 1) * sh + (unsigned __int128)(ns - 1) * ss + row_bytes;
+        return end <= bytes;
+    };
+    if (view->layout == KV_LAYOUT_BHSD) {
+        if (view->stride_b < 0 || view->stride_h < 0 || view->stride_s < 0 || view->s_alloc < 0) return KV_EINVAL;
+        if ((view->stride_b | view->stride_h | view->stride_s) & 7) return KV_EINVAL;
+        if (view->seq_off_host || view->seq_off_dev) return KV_EINVAL;
+        c->sb = 2 * (uint64_t)view->stride_b; c->sh = 2 * (uint64_t)view->stride_h; c->ss = 2 * (uint64_t)view->stride_s;
+        c->rows = view->s_alloc;
+        for (int b = 0; b < p->B; ++b) {
+            const int64_t n = lens ? (int64_t)lens[b] + (first[b + 1] - first[b]) : view->s_alloc;
+            if (n > view->s_alloc) return KV_ERANGE;
+            if (n < 1) continue;
+            if (!inside(b + 1, c->sb, p->H, c->sh, n, c->ss, row, view->layer_bytes)) return KV_ERANGE;
+            if (blocks && !inside(b + 1, c->zb, p->H, c->zh, n, c->zs, zrow, blocks->layer_bytes)) return KV_ERANGE;
+        }
+    } else if (view->layout == KV_LAYOUT_PAGED) {
+        if (!view->block_table || view->block_tokens < 1 || view->n_pool_blocks < 0 || view->max_blocks_per_seq < 0) return KV_EINVAL;
+        c->table = view->block_table;
+        c->max_blocks = view->max_blocks_per_seq;
+        c->bt = view->block_tokens;
+        c->n_pool = view->n_pool_blocks;
+        c->ss = row;
+        c->sh = row * (uint64_t)c->bt;
+        c->sb = c->sh * (uint64_t)p->H;
+        if (c->n_pool > 0) {
+            if (!inside(c->n_pool, c->sb, p->H, c->sh, c->bt, c->ss, row, view->layer_bytes)) return KV_ERANGE;
+            if (blocks && !inside(c->n_pool, c->zb, p->H, c->zh, c->bt, c->zs, zrow, blocks->layer_bytes)) return KV_ERANGE;
+        }
+        for (int b = 0; lens && b < p->B; ++b)
+            if (ceil_div((uint64_t)lens[b] + (uint64_t)(first[b + 1] - first[b]), (uint64_t)c->bt) > (uint64_t)c->max_blocks) return KV_ERANGE;
+    } else {
+        return KV_EINVAL;
+    }
+    return KV_OK;
+}
+
+extern "C" int kv_cache_write(const kv_plan_t *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_write_args_t *a, void *hip_stream)
+{
+    if (!p || !view || !a || p->D % kBlockElems != 0) return KV_EINVAL;
+    RowParams r{};
+    int rc = cache_addr(p, view, blocks, layer, nullptr, nullptr, &r.c);
+    if (rc != KV_OK) return rc;
+    bool pairs = false;
+    if (a->rope) {
+        rc = check_rope(a->rope, p->D);
+        if (rc != KV_OK) return rc;
+        if (!a->positions && a->n_tok > 0) return KV_EINVAL;
+        r.table = a->rope->table;
+        r.n_pos = a->rope->n_pos;
+        r.rot = a->rope->rot_dim;
+        pairs = a->rope->style == KV_ROPE_PAIRS;
+    }
+    const int format = blocks ? blocks->format : KV_FORMAT_16;
+    return launch_rows(p, r, p->dtype == KV_BF16 ? write_kernel<true>(format, pairs) : write_kernel<false>(format, pairs), a->k, a->v, a->k_stride_t,
+                       a->k_stride_h, a->v_stride_t, a->v_stride_h, a->tok_seq, a->tok_slot, a->positions, a->n_tok, hip_stream);
+}
+
+extern "C" int kv_cache_read(const kv_plan_t *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_read_args_t *a, void *hip_stream)
+{
+    if (!p || !view || !a || p->D % kBlockElems != 0) return KV_EINVAL;
+    RowParams r{};
+    const int rc = cache_addr(p, view, blocks, layer, nullptr, nullptr, &r.c);
+    if (rc != KV_OK) return rc;
+    const int format = blocks ? blocks->format : KV_FORMAT_16;
+    return launch_rows(p, r, p->dtype == KV_BF16 ? read_kernel<true>(format) : read_kernel<false>(format), a->k, a->v, a->k_stride_t, a->k_stride_h,
+                       a->v_stride_t, a->v_stride_h, a->tok_seq, a->tok_slot, nullptr, a->n_tok, hip_stream);
+}

@@ -446,6 +446,13 @@ extern "C" size_t kv_abi_sizeof(int which)
     case 8: return sizeof(kv_append_stats_t);
     case 9: return sizeof(kv_adapt_t);
     case 10: return sizeof(kv_chunk_trace_t);
+    case 11: return sizeof(kv_blocks_t);
+    case 12: return sizeof(kv_rope_t);
+    case 13: return sizeof(kv_rope_desc_t);
+    case 14: return sizeof(kv_rope_args_t);
+    case 15: return sizeof(kv_write_args_t);
+    case 16: return sizeof(kv_read_args_t);
+    case 17: return sizeof(kv_tree_args_t);
     default: return 0;
     }
 }
