@@ -6,110 +6,59 @@
 #include <climits>
 #include <cmath>
 
-#include "cache.hpp"
-#include "launch.hpp"
+#include "tree_attn.hpp"
 
 namespace {
 
 using namespace kvb;
 
-struct TreeParams {
-    CacheAddr c;
-    const char *q;
-    void *out;
-    long long q_st, q_sh, o_st, o_sh;  // elements
-    const int *seq_lens, *tok_first;
-    const unsigned long long *mask;
-    int words, max_total, H, G, B;
-    float scale;
-    int out_mode;                      // 0 fp32, 1 fp16, 2 bf16
-};
-
-template <bool BF16, int FORMAT>
-__device__ __forceinline__ f32x2 load2(const char *row, const char *scales, int d)
-{
-    unsigned w;
-    if constexpr (FORMAT == KV_FORMAT_16) {
-        w = *(const unsigned *)(row + 2 * d);
-    } else {
-        const float s = scale_operand((unsigned char)scales[d / kBlockElems]);
-        if constexpr (FORMAT == KV_FORMAT_FP8) w = decode2<BF16, FORMAT, 0>(*(const unsigned short *)(row + d), s);
-        else w = decode2<BF16, FORMAT, 0>((unsigned char)row[d / 2], s);
-    }
-    return unpack2<BF16>(w);
-}
-
-// One workgroup of four wavefronts per query row; a wavefront takes every fourth token, its lanes pairs of elements.
-template <int D, bool BF16, int FORMAT>
-__global__ void __launch_bounds__(256) kv_tree_attn_kernel(TreeParams p)
-{
-    constexpr int N = (D + 127) / 128;
-    const int t = blockIdx.x, hq = blockIdx.y, h = hq / p.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool on = 2 * lane < D;
-    int b = 0;
-    while (b + 1 < p.B && p.tok_first[b + 1] <= t) ++b;
-    const int i = t - p.tok_first[b], drafted = p.tok_first[b + 1] - p.tok_first[b], len = max(0, min(p.seq_lens[b], p.max_total - drafted));
-    const char *const q = p.q + 2 * (t * p.q_st + hq * p.q_sh);
-    f32x2 x[N], acc[N] = {};
-    for (int k = 0; k < N; ++k) x[k] = on ? unpack2<BF16>(*(const unsigned *)(q + 2 * (128 * k + 2 * lane))) : f32x2{0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    for (int j = wave; j < len + drafted; j += 4) {
-        const int n = j - len;
-        if (n >= 0 && !(p.mask ? p.mask[(long long)t * p.words + n / 64] >> (n % 64) & 1 : n <= i)) continue;
-        unsigned block, row;
-        if (!find_row(p.c, b, j, &block, &row)) continue;
-        const unsigned long long at = block * p.c.sb + h * p.c.sh + row * p.c.ss, z = block * p.c.zb + h * p.c.zh + row * p.c.zs;
-        float s = 0.f;
-        f32x2 v[N];
-        for (int k = 0; k < N; ++k) {
-            const int d = on ? 128 * k + 2 * lane : 0;
-            const f32x2 y = load2<BF16, FORMAT>(p.c.k + at, p.c.kz + z, d);
-            v[k] = load2<BF16, FORMAT>(p.c.v + at, p.c.vz + z, d);
-            s += on ? x[k][0] * y[0] + x[k][1] * y[1] : 0.f;
-        }
-        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-        s *= p.scale;
-        const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
-        m = mn;
-        l = l * f + w;
-        for (int k = 0; k < N; ++k) acc[k] = acc[k] * f + v[k] * w;
-    }
-    __shared__ float sm[4], sl[4];
-    __shared__ f32x2 sa[4][N][64];
-    if (lane == 0) { sm[wave] = m; sl[wave] = l; }
-    for (int k = 0; k < N; ++k) sa[wave][k][lane] = acc[k];
-    __syncthreads();
-    if (wave > 0 || !on) return;
-    float M = -INFINITY, L = 0.f;
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w]);
-    f32x2 a[N] = {};
-    for (int w = 0; w < 4; ++w) {
-        if (sl[w] == 0.f) continue;
-        const float f = expf(sm[w] - M);
-        L += sl[w] * f;
-        for (int k = 0; k < N; ++k) a[k] += sa[w][k][lane] * f;
-    }
-    for (int k = 0; k < N; ++k)
-        for (int e = 0; e < 2; ++e) {
-            const long long o = t * p.o_st + hq * p.o_sh + 128 * k + 2 * lane + e;
-            const float r = L == 0.f ? 0.f : a[k][e] / L;
-            if (p.out_mode == 0) ((float *)p.out)[o] = r;
-            else if (p.out_mode == 1) ((_Float16 *)p.out)[o] = (_Float16)r;
-            else ((unsigned short *)p.out)[o] = bf16_bits(r);
-        }
-}
-
-typedef void (*TreeKernel)(TreeParams);
-template <int D, bool BF16>
-TreeKernel tree_kernel(int format)
-{
-    return format == KV_FORMAT_FP8 ? kv_tree_attn_kernel<D, BF16, KV_FORMAT_FP8> : format == KV_FORMAT_FP4 ? kv_tree_attn_kernel<D, BF16, KV_FORMAT_FP4>
-                                                                                                      : kv_tree_attn_kernel<D, BF16, KV_FORMAT_16>;
-}
+// A wavefront merges the splits of one query row.
+constexpr int kCombineWaves = 4;
 template <int D>
-TreeKernel tree_kernel(bool bf16, int format)
+__global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(TreeParams p, int n_rows)
 {
-    return bf16 ? tree_kernel<D, true>(format) : tree_kernel<D, false>(format);
+    constexpr int kLanes = D / 4, kTogether = 64 / kLanes;   // lanes of a row, splits at a time
+    const int row = blockIdx.x * kCombineWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= n_rows) return;
+    const int Hq = p.H * p.G, t = row / Hq, hq = row - t * Hq;
+    int lo = 0, hi = p.B - 1;   // the last sequence that starts at or before t
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (p.tok_first[mid] <= t) lo = mid;
+        else hi = mid - 1;
+    }
+    const int drafted = min(p.tok_first[lo + 1] - p.tok_first[lo], KV_TREE_MAX);
+    const int total = max(0, min(p.seq_lens[lo], p.max_total - drafted)) + drafted;
+    const int ns = min(p.ns, (total + p.split_tokens - 1) / p.split_tokens);
+    const f32x2 *const ml = (const f32x2 *)p.part_ml + (long long)row * p.ns;
+    const float *const part = p.part_acc + (long long)row * p.ns * D;
+    const int sub = lane / kLanes, d = lane % kLanes * 4;
+    float to = kNoScore;
+    for (int s = 0; s < ns; ++s) to = fmaxf(to, ml[s][0]);
+    float l = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < ns; ++s) l += ml[s][1] == 0.f ? 0.f : ml[s][1] * __builtin_amdgcn_exp2f(ml[s][0] - to);
+    for (int s = sub; s < ns; s += kTogether) {
+        const float f = ml[s][1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(ml[s][0] - to), 1.0e-37f);   // an infinity stays one
+        const f32x4 y = *(const f32x4 *)&part[(long long)s * D + d];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = fmaf(y[k], f, x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        for (int o = kLanes; o < 64; o *= 2) x[k] += __shfl_xor(x[k], o);
+    }
+    if (sub == 0) store_four(p.out, t * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
+}
+
+TreeShape shape_of(const kv_plan *p, int bits)
+{
+    static int cus = 0;
+    if (cus == 0) {
+        int dev = 0, n = 0;
+        cus = hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0 ? n : 256;
+    }
+    return TreeShape{p->D, p->H, p->Hq / p->H, bits, cus};
 }
 
 }  // namespace
@@ -133,7 +82,9 @@ extern "C" int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t 
 extern "C" size_t kv_tree_attn_workspace(const kv_plan_t *p, int n_tok, int max_len)
 {
     if (!p || n_tok < 0 || max_len < 0) return 0;
-    return 16;
+    const TreeShape s = shape_of(p, 16);
+    const int most = std::min(tree_most_splits(s, n_tok), (int)(((int64_t)max_len + KV_TREE_MAX + 31) / 32));
+    return (size_t)std::max<uint64_t>(16, tree_split_bytes(s, n_tok) * most);
 }
 
 extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *a, void *workspace,
@@ -161,6 +112,8 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     if (blocks && (((uintptr_t)t.c.kz | (uintptr_t)t.c.vz | t.c.zb | t.c.zh | t.c.zs) & (p->D / kBlockElems - 1))) return KV_EINVAL;
     const int n_tok = a->tok_first_host[p->B];
     if (n_tok == 0) return KV_OK;
+    if (t.c.table && t.c.n_pool < 1) return KV_ERANGE;
+    if ((int64_t)n_tok * p->Hq > INT_MAX) return KV_ERANGE;
     if (!a->q || !a->out || ((uintptr_t)a->q & 15)) return KV_EINVAL;
     if (a->q_stride_t < 0 || a->q_stride_h < 0 || a->out_stride_t < 0 || a->out_stride_h < 0 || ((a->q_stride_t | a->q_stride_h) & 7)) return KV_EINVAL;
     const bool bf16 = p->dtype == KV_BF16;
@@ -173,12 +126,37 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.words = a->mask_words;
     t.max_total = max_total;
     t.H = p->H; t.G = p->Hq / p->H; t.B = p->B;
-    t.scale = a->scale == 0.f ? (float)(1 / std::sqrt((double)p->D)) : a->scale;
+    t.scale_log2e = (float)(1.4426950408889634 * (a->scale == 0.f ? 1 / std::sqrt((double)p->D) : (double)a->scale));
     t.out_mode = a->out_dtype == KV_OUT_F32 ? 0 : bf16 ? 2 : 1;
+
     const int format = blocks ? blocks->format : KV_FORMAT_16;
-    TreeKernel k = p->D == 64 ? tree_kernel<64>(bf16, format) : p->D == 128 ? tree_kernel<128>(bf16, format) : tree_kernel<256>(bf16, format);
-    (void)launch_kernel(k, dim3((unsigned)n_tok, (unsigned)p->Hq), dim3(256), (hipStream_t)hip_stream, t);
-    const hipError_t e = hipGetLastError();
+    const TreeCut cut = cut_tree(shape_of(p, format_bits(format)), p->B, view->seq_lens_host, a->tok_first_host, a->n_splits, ws_bytes);
+    t.ns = cut.ns;
+    t.split_tokens = cut.split_tokens;
+    t.row_blocks = cut.row_blocks;
+    t.part_acc = (float *)workspace;
+    t.part_ml = t.part_acc + (size_t)n_tok * p->Hq * cut.ns * p->D;
+    t.bt_shift = -1;
+    if (t.c.table && (t.c.bt & (t.c.bt - 1)) == 0) t.bt_shift = __builtin_ctz((unsigned)t.c.bt);
+    const uint64_t units = ((uint64_t)p->B * p->H * cut.ns + 7) / 8 * 8, groups = units * cut.row_blocks;
+    if (groups > INT_MAX) return KV_ERANGE;
+    const bool f32 = t.out_mode == 0;
+    const bool paged = t.c.table != nullptr;
+    // 32 rows and their scales within 32-bit offsets; blocks of whole groups, their scales' rows side by side
+    t.grouped = paged ? t.c.bt % 8 == 0 && (!blocks || t.c.zs == (uint64_t)p->D / kBlockElems) : t.c.ss < 1ull << 26 && t.c.zs < 1ull << 26;
+    TreeKernel k = format == KV_FORMAT_FP8   ? (paged ? tree_kernel_fp8_paged : tree_kernel_fp8)(p->D, bf16, f32, cut.nb)
+                   : format == KV_FORMAT_FP4 ? (paged ? tree_kernel_fp4_paged : tree_kernel_fp4)(p->D, bf16, f32, cut.nb)
+                                             : (paged ? tree_kernel_16_paged : tree_kernel_16)(p->D, bf16, f32, cut.nb);
+    hipStream_t st = (hipStream_t)hip_stream;
+    (void)launch_kernel(k, dim3((unsigned)groups), dim3(kTreeThreads), st, t);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
+    if (cut.ns == 1) return KV_OK;
+    const long long rows = (long long)n_tok * p->Hq;
+    const dim3 cgrid((unsigned)((rows + kCombineWaves - 1) / kCombineWaves));
+    (void)launch_kernel(p->D == 64 ? kv_tree_combine_kernel<64> : p->D == 128 ? kv_tree_combine_kernel<128> : kv_tree_combine_kernel<256>, cgrid,
+                        dim3(64 * kCombineWaves), st, t, (int)rows);
+    e = hipGetLastError();
     if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     return KV_OK;
 }
