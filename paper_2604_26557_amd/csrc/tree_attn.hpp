@@ -1,9 +1,10 @@
-// Kernels of kv_tree_attn, a translation unit for each cache format and layout (tree_attn_16.hip, tree_attn_16_paged.hip, ...).
+// Kernels of kv_tree_attn, a translation unit for each cache format (tree_attn_16.hip, tree_attn_fp8.hip, tree_attn_fp4.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "cache.hpp"
 #include "launch.hpp"
@@ -23,7 +24,8 @@ struct TreeParams {
     int words, max_total, H, G, B, out_mode;  // out_mode: 0 fp32, 1 fp16, 2 bf16
     int ns, split_tokens, row_blocks;
     int bt_shift;                      // log2 of a block's tokens, or -1
-    int grouped;                       // rows of context are looked up by groups of eight
+    unsigned by_g, by_ns, by_h, by_row_blocks;  // 2^32 over G, ..., rounded up: x / G = x * by_g >> 32 as long as x * G < 2^32
+    int grouped;                       // rows of context are looked up by groups of 16
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -67,12 +69,28 @@ __device__ __forceinline__ void store_four(void *out, long long i, int mode, f32
     }
 }
 
-constexpr int kTreeWaves = 8, kTreeThreads = 64 * kTreeWaves;
+// C columns side by side; at column 8 of 16, those of rows of 512 bytes go on 128 columns further
+template <int C>
+__device__ __forceinline__ void store_columns(void *out, long long i, int mode, const float (&x)[C])
+{
+    if constexpr (C >= 4) {
+#pragma unroll
+        for (int c = 0; c < C; c += 4) store_four(out, i + c, mode, f32x4{x[c], x[c + 1], x[c + 2], x[c + 3]});
+    } else if constexpr (C == 2) {
+        if (mode == 0 && !(((uintptr_t)out | (uintptr_t)(4 * i)) & 7)) *(f32x2 *)((float *)out + i) = f32x2{x[0], x[1]};
+        else if (mode != 0 && !(((uintptr_t)out | (uintptr_t)(2 * i)) & 3)) *(unsigned *)((unsigned short *)out + i) = mode == 1 ? pack2<false>(x[0], x[1]) : pack2<true>(x[0], x[1]);
+        else store_one(out, i, mode, x[0]), store_one(out, i + 1, mode, x[1]);
+    } else {
+        store_one(out, i, mode, x[0]);
+    }
+}
+
 constexpr float kNoScore = -1.0e30f;    // reference of a row that has seen no score
-constexpr float kTreeRise = 4.f;        // a reference follows the running maximum when a score passes it by this (log2)
+// A reference follows the running maximum when a probability passes 2^4 of it.
 constexpr float kLargeRef = 1048576.f;  // beyond it the rounding of a reference would leave the range of the probabilities
 // fp16 probabilities are taken of 2^11 times themselves (at most 2^15): what is lost lies below 2^-36 of the largest
 template <bool BF16> constexpr float kLiftLog2 = BF16 ? 0.f : 11.f;
+template <bool BF16> constexpr float kMostProbability = BF16 ? 16.f : 32768.f;   // 2^(4 + kLiftLog2)
 template <bool BF16, bool F32> constexpr int kParts = F32 ? (BF16 ? 3 : 2) : 1;
 
 // Probabilities as 16-bit operands: rounded once, or as parts whose sum is the 32-bit value (bf16) or that value up to 2^-22 (fp16).
@@ -100,120 +118,88 @@ __device__ __forceinline__ void split_pair(float x, float y, unsigned (&out)[N])
     }
 }
 
-template <typename T, bool NT>
-__device__ __forceinline__ T load_as(const char *p)
-{
-    if constexpr (NT) return __builtin_nontemporal_load((const T *)p);
-    else return *(const T *)p;
-}
+constexpr int kTreeThreads = 256;
 
-// How rows of context alone are addressed (in groups of eight tokens): a strided cache, scalar bases and 32-bit offsets of the lanes; a block pool of multiples of
-// eight tokens, a pointer per lane and constant offsets.  Everything else is looked up row by row.
-constexpr int kTreeStrided = 0, kTreePaged = 1;
-
-// A step of a wavefront is 32 tokens.  Where their K and V are few bytes, four wavefronts a SIMD keep enough of them in flight, elsewhere two do.
-template <int D, int FORMAT, int NB> constexpr int kTreeWavesPerSimd = NB == 1 && D * format_bits(FORMAT) <= 512 ? 4 : 2;
-
-template <int D, bool BF16, int FORMAT, int NB, bool F32>
+// The tile of a wavefront's step: 32 tokens, whose K and V pass through LDS as they lie in the cache.
+template <int D, int FORMAT, int NB>
 struct TreeTile {
-    static constexpr int kColumns = D / 16;           // columns of V that a lane loads of a token
-    static constexpr int kSteps = D / 32;             // products of a tile of q K^T
-    static constexpr int kRows = 16 * NB;             // query rows of a workgroup
     static constexpr int kBits = format_bits(FORMAT);
     static constexpr bool kBlocks = FORMAT != KV_FORMAT_16;
-    static constexpr bool kQInLds = NB * D > 256;   // more rows than their registers are worth
-    static constexpr bool kNT = NB <= 2;              // more rows: other workgroups may read the same K and V out of L2
-    static constexpr int kP = kParts<BF16, F32>;
-    // K: a lane holds a quarter of a token's row, as pieces of 16 bytes (8 where the row is 32 bytes long)
-    static constexpr int kQuarter = D * kBits / 32;   // bytes
-    static constexpr int kPiece = kQuarter < 16 ? kQuarter : 16;
-    static constexpr int kPieces = kQuarter / kPiece;
-    static constexpr int kPieceElems = kPiece * 8 / kBits;
-    static constexpr int kVBytes = kColumns * kBits / 8;
-    static constexpr int kVWords = kVBytes < 4 ? 1 : kVBytes / 4;
-
-    struct K {
-        u32x4 w[kPieces];
-        unsigned z[kBlocks ? kPieces : 1];
-    };
-    struct V {
-        unsigned w[8][kVWords];
-        unsigned z[kBlocks ? 8 : 1];
-    };
+    static constexpr int kColumns = D / 16;           // columns of V that a lane works on
+    static constexpr int kSteps = D / 32;             // products of 16 tokens' q K^T
+    static constexpr int kRows = 16 * NB;             // query rows of a workgroup
+    static constexpr bool kQInLds = NB * D > 256;     // more rows than their registers are worth
+    static constexpr int kRow = D * kBits / 8;        // bytes of a token's row
+    static constexpr int kPieces = kRow / 16;         // a row's pieces of 16 bytes: a lane's share of a load
+    static constexpr int kTokens = 64 / kPieces;      // rows of a load (1 KiB)
+    static constexpr int kLoads = 32 / kTokens;       // loads of a step's K, and as many of V
+    static constexpr int kKPiece = kRow >= 64 ? 16 : 8;   // bytes of K that a lane reads from LDS at a time
+    static constexpr int kKReads = kRow / 4 / kKPiece;
+    static constexpr int kKElems = kKPiece * 8 / kBits;
+    static constexpr int kVBytes = kColumns * kBits / 8;  // bytes of a token's row that a lane works on
+    static constexpr int kKBytes = 32 * kRow;         // of a stage, and as many of V
+    static constexpr int kZRow = D / kBlockElems;
+    static constexpr int kZBytes = !kBlocks ? 0 : D == 256 ? 512 : 256;   // 32 rows' scales of K, then of V, each 4 (8) bytes apart
+    static constexpr int kZLoads = !kBlocks ? 0 : D == 256 ? 2 : 1;
+    static constexpr int kWaves = 4;                  // two workgroups and more on a compute unit: one merges while another reads
+    static constexpr int kStage = 2 * kKBytes + kZBytes;
+    static constexpr int kQBytes = kQInLds ? NB * kSteps * 1024 : 0;
+    static constexpr int kHalfLds = 80 * 1024;
+    // Steps on their way while one is worked on: up to 16 KiB of a wavefront, as long as two workgroups fit
+    static constexpr int kStages = kWaves * 4 * kStage + kQBytes <= kHalfLds && kStage <= 4096 ? 4 : kWaves * 2 * kStage + kQBytes <= kHalfLds ? 2 : 1;
+    static constexpr int kRing = kWaves * kStages * kStage;
+    static constexpr int kMerge = kWaves * NB * kColumns / 2 * 1024, kStates = (2 * kWaves * kRows + kWaves) * 4;   // bytes
+    static constexpr int kLds = kRing + kQBytes > kMerge + kStates ? kRing + kQBytes : kMerge + kStates;
+    static_assert(kLds <= (D == 256 ? 2 : 1) * kHalfLds, "LDS of a compute unit");
+    static constexpr int kPerCu = kLds <= 40 * 1024 ? 4 : kLds <= kHalfLds / 3 * 2 ? 3 : kLds <= kHalfLds ? 2 : 1;
 
     // The first of the eight elements of d that a lane contributes to product s: any order will do that q follows as well.
     static __device__ __forceinline__ int q_at(int s, int group)
     {
-        constexpr int per = kPieceElems / 8;  // products of a piece
-        return (s / per) * 4 * kPieceElems + group * kPieceElems + (s % per) * 8;
+        constexpr int per = kKElems / 8;  // products of a read
+        return (s / per) * 4 * kKElems + group * kKElems + (s % per) * 8;
     }
-
-    static __device__ __forceinline__ void load_k(K &k, const char *row, const char *zrow, int group) { load_k(k, row, 0, zrow, 0, group); }
-    // Rows at a base that all lanes share and an offset of the lane's.
-    static __device__ __forceinline__ void load_k(K &k, const char *row, unsigned lane_at, const char *zrow, unsigned lane_z, int group)
+    // K's pieces are exchanged within a row by a number of the token's, so that the 16 rows of which a read takes one piece lie in different banks.
+    static __device__ __forceinline__ int k_turn(int token)
     {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const char *const at = row + 4 * kPiece * i + (lane_at + kPiece * group);
-            if constexpr (kPiece == 16) {
-                k.w[i] = load_as<u32x4, kNT>(at);
-            } else {
-                const u32x2 w = load_as<u32x2, kNT>(at);
-                k.w[i] = u32x4{w[0], w[1], 0, 0};
-            }
-            if constexpr (kBlocks) k.z[i] = (unsigned char)(zrow + i * 4 * kPieceElems / kBlockElems)[lane_z + group * kPieceElems / kBlockElems];
-        }
+        return kPieces >= 16 ? token & 15 : kPieces == 8 ? token >> 1 & 7 : kPieces == 4 ? token >> 2 & 3 : 0;
     }
-    static __device__ __forceinline__ u32x4 k_operand(const K &k, int s)
-    {
-        if constexpr (!kBlocks) {
-            return k.w[s];
-        } else {
-            constexpr int per = kPieceElems / 8;
-            const u32x4 w = k.w[s / per];
-            const float z = scale_operand(k.z[s / per]);
-            if constexpr (FORMAT == KV_FORMAT_FP8) return decode8<BF16, FORMAT>(u32x2{w[2 * (s % per)], w[2 * (s % per) + 1]}, z);
-            else return decode8<BF16, FORMAT>(u32x2{w[s % per], 0}, z);
-        }
-    }
-    // Token j of the lane's eight.
-    static __device__ __forceinline__ void load_v(V &v, int j, const char *row, const char *zrow, int n) { load_v(v, j, row, 0, zrow, 0, n); }
-    static __device__ __forceinline__ void load_v(V &v, int j, const char *row, unsigned lane_at, const char *zrow, unsigned lane_z, int n)
-    {
-        const char *const at = row + (lane_at + kVBytes * n);
-        if constexpr (kVBytes == 2) {
-            v.w[j][0] = load_as<unsigned short, kNT>(at);
-        } else if constexpr (kVBytes == 4) {
-            v.w[j][0] = load_as<unsigned, kNT>(at);
-        } else if constexpr (kVBytes == 8) {
-            const u32x2 w = load_as<u32x2, kNT>(at);
-            v.w[j][0] = w[0];
-            v.w[j][1] = w[1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < kVBytes / 16; ++i) {
-                const u32x4 w = load_as<u32x4, kNT>(at + 16 * i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v.w[j][4 * i + e] = w[e];
-            }
-        }
-        if constexpr (kBlocks) v.z[j] = (unsigned char)zrow[lane_z + kColumns * n / kBlockElems];
-    }
-    // Columns 2 * i and 2 * i + 1 of token j as 16-bit numbers.
-    static __device__ __forceinline__ unsigned v_pair(const V &v, int j, int i)
-    {
-        if constexpr (!kBlocks) {
-            return v.w[j][i];
-        } else {
-            const float z = scale_operand(v.z[j]);
-            if constexpr (FORMAT == KV_FORMAT_FP8)
-                return i % 2 ? decode2<BF16, FORMAT, 1>(v.w[j][i / 2], z) : decode2<BF16, FORMAT, 0>(v.w[j][i / 2], z);
-            else
-                return i % 4 == 0 ? decode2<BF16, FORMAT, 0>(v.w[j][i / 4], z) : i % 4 == 1 ? decode2<BF16, FORMAT, 1>(v.w[j][i / 4], z)
-                     : i % 4 == 2 ? decode2<BF16, FORMAT, 2>(v.w[j][i / 4], z) : decode2<BF16, FORMAT, 3>(v.w[j][i / 4], z);
-        }
-    }
+    // Column of V (of d) behind row m of the product's result and the lane's column c: rows of 512 bytes are read in two halves.
+    static __device__ __forceinline__ int v_column(int m, int c) { return kVBytes == 32 ? (c / 8) * 128 + 8 * m + c % 8 : kColumns * m + c; }
 };
+
+// 16 (4, 2) bytes per lane from memory to LDS, behind the wavefront's back: lane l's arrive at lds + 16 l (4 l).  Only counted waits (wait_loads) say when.
+template <int BYTES, bool NT>
+__device__ __forceinline__ void load_to_lds(const char *from, unsigned lds)
+{
+    if constexpr (BYTES == 16 && NT) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(lds) : "memory");
+    else if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+    else if constexpr (BYTES == 4) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ushort %0, off" ::"v"(from), "s"(lds) : "memory");
+}
+// The same from a start that all lanes share and a lane's 32-bit offset.
+template <bool NT>
+__device__ __forceinline__ void load_to_lds16(unsigned long long start, unsigned offset, unsigned lds)
+{
+    // in scalar registers, wherever the compiler has it
+    start = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)start) | (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(start >> 32)) << 32;
+    if constexpr (NT) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(start), "s"(lds) : "memory");
+    else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(start), "s"(lds) : "memory");
+}
+// x as if it was new here: what follows from it is computed where it is used, and not kept in registers that the loop has none of.
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+template <int N>
+__device__ __forceinline__ void wait_loads()   // all but the last N
+{
+    static_assert(N < 64, "vmcnt");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// What was read from LDS has arrived: its place may be loaded into again.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Byte offsets of a token row of one sequence and head (the same for K and V), and of its scales.
 struct RowAt {
@@ -229,23 +215,29 @@ __device__ __forceinline__ RowAt row_at(const CacheAddr &c, const int *table, un
     return RowAt{base + at * c.sb + r * c.ss, zbase + at * c.zb + r * c.zs, there};
 }
 
+// The drafted token of row r of a KV head's query rows.
+__device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.by_g); }
+
+// A value that all lanes load, through the scalar cache: nothing writes it while the kernel runs.
+__device__ __forceinline__ int load_uniform(const int *at) { return *(const __attribute__((address_space(4))) int *)(unsigned long long)at; }
+
 // Does row r of a KV head's query rows see token j of its sequence?
 __device__ __forceinline__ bool row_sees(const TreeParams &p, int first, int r, int j, int len, int total)
 {
     if (j < len) return true;
     if (j >= total || r >= (total - len) * p.G) return false;
-    const int t = r / p.G, i = j - len;
+    const int t = token_of(p, r), i = j - len;
     if (!p.mask) return i <= t;
     return (bool)(p.mask[(long long)(first + t) * p.words + (i >> 6)] >> (i & 63) & 1);
 }
 
-// The same of eight tokens from j on, as bits.
-__device__ __forceinline__ unsigned row_sees8(const TreeParams &p, int first, int r, int j, int len, int total)
+// The same of 32 tokens from j on, as bits.
+__device__ __forceinline__ unsigned row_sees32(const TreeParams &p, int first, int r, int j, int len, int total)
 {
-    auto below = [](int x) { return x >= 8 ? 0xffu : (1u << max(x, 0)) - 1u; };
+    auto below = [](int x) { return x >= 32 ? ~0u : (1u << max(x, 0)) - 1u; };
     const unsigned context = below(len - j), drafted = below(total - j) & ~context;
     if (drafted == 0 || r >= (total - len) * p.G) return context;
-    const int t = r / p.G, i = j - len;   // i > -8: a token's bit is i + its place
+    const int t = token_of(p, r), i = j - len;   // i > -32: a token's bit is i + its place
     unsigned long long bits;
     if (!p.mask) {
         bits = below(t + 1 - i);
@@ -253,7 +245,7 @@ __device__ __forceinline__ unsigned row_sees8(const TreeParams &p, int first, in
         const unsigned long long *const row = p.mask + (long long)(first + t) * p.words;
         const int w = max(i, 0) >> 6, shift = max(i, 0) & 63;
         bits = row[w] >> shift;
-        if (shift > 56 && w + 1 < p.words) bits |= row[w + 1] << (64 - shift);
+        if (shift > 32 && w + 1 < p.words) bits |= row[w + 1] << (64 - shift);
         if (i < 0) bits <<= -i;
     }
     return context | (drafted & (unsigned)bits);
@@ -263,7 +255,7 @@ __device__ __forceinline__ unsigned row_sees8(const TreeParams &p, int first, in
 template <int D>
 __device__ __forceinline__ void store_sums(const TreeParams &p, unsigned h, int first, int r, unsigned split, int d, f32x4 x, float ref, float l)
 {
-    const int t = r / p.G, hq = (int)h * p.G + r - t * p.G;
+    const int t = token_of(p, r), hq = (int)h * p.G + r - t * p.G;
     if (p.ns == 1) {
         store_four(p.out, (first + t) * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
     } else {
@@ -279,16 +271,23 @@ template <int D, bool BF16, int FORMAT>
 __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table, unsigned long long base, unsigned long long zbase, unsigned h, int first, int r,
                                        int len, int total, int s0, int s1, unsigned split, int lane)
 {
-    using T = TreeTile<64, BF16, FORMAT, 1, false>;   // four columns of a lane, sixteen lanes: here D / 4 lanes
-    const int t = r / p.G, hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
+    const int t = token_of(p, r), hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
     const u32x2 qw = *(const u32x2 *)(p.q + 2 * ((first + t) * p.q_st + hq * p.q_sh + 4 * at));
     const f32x2 q0 = unpack2<BF16>(qw[0]), q1 = unpack2<BF16>(qw[1]);
     auto row = [&](const char *rows, const char *scales, int j, bool *there) {
         const RowAt x = row_at(p.c, table, base, zbase, j);
         *there = x.there;
-        typename T::V v;
-        T::load_v(v, 0, rows + x.at, scales + x.z, at);
-        const f32x2 a = unpack2<BF16>(T::v_pair(v, 0, 0)), b = unpack2<BF16>(T::v_pair(v, 0, 1));
+        u32x2 w;
+        if constexpr (FORMAT == KV_FORMAT_16) {
+            w = *(const u32x2 *)(rows + x.at + 8 * at);
+        } else {
+            const float z = scale_operand((unsigned char)scales[x.z + at / 8]);
+            unsigned codes;
+            if constexpr (FORMAT == KV_FORMAT_FP8) codes = *(const unsigned *)(rows + x.at + 4 * at);
+            else codes = *(const unsigned short *)(rows + x.at + 2 * at);
+            w = u32x2{decode2<BF16, FORMAT, 0>(codes, z), decode2<BF16, FORMAT, 1>(codes, z)};
+        }
+        const f32x2 a = unpack2<BF16>(w[0]), b = unpack2<BF16>(w[1]);
         return f32x4{a[0], a[1], b[0], b[1]};
     };
     auto score = [&](int j) {
@@ -318,21 +317,27 @@ __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table,
     if (lane < D / 4) store_sums<D>(p, h, first, r, split, 4 * at, x, top == -INFINITY ? kNoScore : top, l);
 }
 
-template <int D, bool BF16, int FORMAT, int NB, bool F32, int LAYOUT>
-__global__ void __launch_bounds__(kTreeThreads, (kTreeWavesPerSimd<D, FORMAT, NB>)) kv_tree_partial_kernel(TreeParams p)
+template <int D, bool BF16, int FORMAT, int NB, bool F32>
+__global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1)) kv_tree_partial_kernel(TreeParams p)
 {
-    using T = TreeTile<D, BF16, FORMAT, NB, F32>;
-    constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = T::kP;
+    using T = TreeTile<D, FORMAT, NB>;
+    constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = kParts<BF16, F32>, kWaves = T::kWaves, kStages = T::kStages;
+    constexpr bool kNT = NB <= 2;   // with more rows other workgroups may read the same K and V out of L2
 
-    // Workgroups go round the eight XCDs: the row blocks of a split follow each other on one of them and share its L2.
-    const unsigned xcd = blockIdx.x % 8, turn = blockIdx.x / 8;
-    const unsigned rb = turn % (unsigned)p.row_blocks, unit = turn / (unsigned)p.row_blocks * 8 + xcd;
-    const unsigned split = unit % (unsigned)p.ns, bh = unit / (unsigned)p.ns, b = bh / (unsigned)p.H, h = bh % (unsigned)p.H;
+    // Workgroups go round the eight XCDs: the row blocks of a split are eight apart, run at the same time on one XCD and share its L2.
+    unsigned unit = blockIdx.x, rb = 0;
+    if (p.row_blocks > 1) {
+        const unsigned turn = blockIdx.x / 8, eights = __umulhi(turn, p.by_row_blocks);
+        rb = turn - eights * (unsigned)p.row_blocks;
+        unit = eights * 8 + blockIdx.x % 8;
+    }
+    const unsigned bh = p.ns == 1 ? unit : __umulhi(unit, p.by_ns), split = unit - bh * (unsigned)p.ns;
+    const unsigned b = p.H == 1 ? bh : __umulhi(bh, p.by_h), h = bh - b * (unsigned)p.H;
     if (b >= (unsigned)p.B) return;
-    const int first = p.tok_first[b], drafted = min(p.tok_first[b + 1] - first, KV_TREE_MAX);
+    const int first = load_uniform(p.tok_first + b), drafted = min(load_uniform(p.tok_first + b + 1) - first, KV_TREE_MAX);
     const int n_rows = drafted * p.G - (int)rb * kRows;   // of this block: the first kRows of them
     if (n_rows <= 0) return;
-    const int len = max(0, min(p.seq_lens[b], p.max_total - drafted)), total = len + drafted;
+    const int len = max(0, min(load_uniform(p.seq_lens + b), p.max_total - drafted)), total = len + drafted;
     const int s0 = (int)split * p.split_tokens, s1 = min(s0 + p.split_tokens, total);
     if (s0 >= total) return;
 
@@ -342,9 +347,110 @@ __global__ void __launch_bounds__(kTreeThreads, (kTreeWavesPerSimd<D, FORMAT, NB
     const unsigned long long zbase = p.c.table ? h * p.c.zh : b * p.c.zb + h * p.c.zh;
     const int *const table = p.c.table ? p.c.table + (long long)b * p.c.max_blocks : nullptr;
 
+    // The ring of each wavefront's stages, then q; after the last step the merge's rows and states.
+    __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+    const unsigned ring_at = (unsigned)wave * (kStages * T::kStage);
+    const unsigned lds_at = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char *)lds + ring_at;
+    const char *const ring = lds + ring_at;
+
+    const int n_steps = (s1 - s0 + 31) / 32;
+    const int mine = (n_steps - wave + kWaves - 1) / kWaves;   // steps of this wavefront: wave, wave + kWaves, ...
+    auto block_of = [&](int j) { return p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt; };
+
+    // Where a step's rows are.  16 rows lie stride by stride from a start that all lanes share, in a block pool from an id that some lane holds; blocks of other
+    // sizes and rows far apart are looked up one by one.  A row past the end is the last one; what has no place in the cache is block 0 of the pool; neither is seen.
+    unsigned long long at0 = 0, at1 = 0, z0 = 0, z1 = 0;   // starts
+    unsigned long long lane_at = 0, lane_z = 0;            // where not all rows exist, or they are looked up: the row of token lane % 32
+    unsigned next_there = ~0u;                             // a bit for each token that the cache has
+    unsigned ids = 0;                                      // lane l: block of half l % 2 of the wavefront's step l / 2 (of 32 steps)
+    bool groups = false;
+    auto where = [&](int m) {   // this wavefront's m-th step
+        const int j0 = s0 + 32 * (wave + m * kWaves), left = total - 1 - j0;
+        groups = p.grouped && left >= 31;
+        next_there = ~0u;
+        if (!p.grouped) {
+            const RowAt r = row_at(p.c, table, base, zbase, j0 + min(lane & 31, left));
+            lane_at = r.at;
+            lane_z = r.z;
+            next_there = (unsigned)__ballot(r.there);
+            return;
+        }
+        if (!p.c.table) {
+            at0 = base + (unsigned)j0 * p.c.ss;
+            at1 = at0 + 16 * (unsigned)p.c.ss;
+            if (T::kBlocks) {
+                z0 = zbase + (unsigned)j0 * p.c.zs;
+                z1 = z0 + 16 * (unsigned)p.c.zs;
+            }
+        } else {
+            if (m % 32 == 0) ids = (unsigned)table[block_of(min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1))];
+            unsigned id0 = (unsigned)__builtin_amdgcn_readlane((int)ids, 2 * (m % 32)), id1 = (unsigned)__builtin_amdgcn_readlane((int)ids, 2 * (m % 32) + 1);
+            const unsigned in0 = j0 - block_of(j0) * p.c.bt, in1 = j0 + 16 - block_of(j0 + 16) * p.c.bt;
+            if (id0 >= (unsigned)p.c.n_pool) id0 = 0, next_there &= 0xffff0000u;
+            if (id1 >= (unsigned)p.c.n_pool) id1 = 0, next_there &= 0xffffu;
+            at0 = base + (unsigned long long)id0 * (unsigned)p.c.sb + in0 * (unsigned)p.c.ss;
+            at1 = base + (unsigned long long)id1 * (unsigned)p.c.sb + in1 * (unsigned)p.c.ss;
+            if (T::kBlocks) {
+                z0 = zbase + (unsigned long long)id0 * (unsigned)p.c.zb + in0 * (unsigned)p.c.zs;
+                z1 = zbase + (unsigned long long)id1 * (unsigned)p.c.zb + in1 * (unsigned)p.c.zs;
+            }
+        }
+        if (!groups) {
+            const int t = min(lane & 31, left);
+            lane_at = (t & 16 ? at1 : at0) + (unsigned)(t & 15) * (unsigned)p.c.ss;
+            lane_z = (t & 16 ? z1 : z0) + (unsigned)(t & 15) * (unsigned)p.c.zs;
+        }
+    };
+    auto from_lane = [](unsigned long long x, int l) {
+        return (unsigned long long)(unsigned)__shfl((int)(unsigned)x, l) | (unsigned long long)(unsigned)__shfl((int)(unsigned)(x >> 32), l) << 32;
+    };
+    // Loads of a step's K (is_v = false) or V into a stage.
+    auto issue_rows = [&](unsigned stage, auto is_v) {
+        constexpr bool V = decltype(is_v)::value;
+        const char *const rows = V ? p.c.v : p.c.k;
+        const unsigned to = lds_at + stage * T::kStage + (V ? T::kKBytes : 0);
+        const int l = here(lane), piece = l % T::kPieces, slot = l / T::kPieces;   // of a load
+        if (groups) {
+            const unsigned lane_row = (unsigned)slot * (unsigned)p.c.ss;
+#pragma unroll
+            for (int q = 0; q < T::kLoads; ++q) {
+                const int token = q * T::kTokens + slot;
+                const unsigned from = 16 * (V ? piece : piece ^ T::k_turn(token));
+                if constexpr (T::kTokens <= 16) {
+                    const unsigned long long start = (q * T::kTokens < 16 ? at0 : at1) + (q * T::kTokens & 15) * (unsigned)p.c.ss;
+                    load_to_lds16<kNT>((unsigned long long)rows + start, lane_row + from, to + q * 1024);
+                } else {   // both groups in one
+                    load_to_lds<16, kNT>(rows + (slot & 16 ? at1 : at0) + ((slot & 15) * (unsigned)p.c.ss + from), to + q * 1024);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < T::kLoads; ++q) {
+                const int token = q * T::kTokens + slot;
+                const int from = 16 * (V ? piece : piece ^ T::k_turn(token));
+                load_to_lds<16, kNT>(rows + from_lane(lane_at, token) + from, to + q * 1024);
+            }
+        }
+    };
+    auto issue_scales = [&](unsigned stage) {
+        if constexpr (T::kBlocks) {
+            const unsigned to = lds_at + stage * T::kStage + 2 * T::kKBytes;
+            const int l = here(lane);
+#pragma unroll
+            for (int q = 0; q < T::kZLoads; ++q) {
+                const int token = D == 256 ? l >> 1 : l & 31, half = D == 256 ? (l & 1) * 4 : 0;
+                const char *const scales = (D == 256 ? q : l >> 5) ? p.c.vz : p.c.kz;
+                unsigned long long z;
+                if (groups) z = (token & 16 ? z1 : z0) + (unsigned)(token & 15) * (unsigned)p.c.zs;
+                else z = from_lane(lane_z, token);
+                load_to_lds<D == 64 ? 2 : 4, false>(scales + z + half, to + 256 * q);
+            }
+        }
+    };
+
     // Query rows: token-major, the G heads of a token side by side.  Rows past the last one are zeros.
-    auto row_token = [&](int r) { return ((int)rb * kRows + r) / p.G; };
-    __shared__ __attribute__((aligned(16))) u32x4 q_lds[T::kQInLds ? NB * kSteps * 64 : 1];
+    auto row_token = [&](int r) { return token_of(p, (int)rb * kRows + r); };
+    u32x4 *const q_lds = (u32x4 *)(lds + T::kRing);
     u32x4 q_reg[T::kQInLds ? 1 : NB][kSteps];
     auto load_q = [&](int nb, int s) {
         const int r = nb * 16 + n;
@@ -352,59 +458,108 @@ __global__ void __launch_bounds__(kTreeThreads, (kTreeWavesPerSimd<D, FORMAT, NB
         const int t = row_token(r), g = (int)rb * kRows + r - t * p.G;
         return *(const u32x4 *)(p.q + 2 * ((first + t) * p.q_st + ((int)h * p.G + g) * p.q_sh + T::q_at(s, group)));
     };
-    if constexpr (T::kQInLds) {
-        for (int i = wave; i < NB * kSteps; i += kTreeWaves) q_lds[i * 64 + lane] = load_q(i / kSteps, i % kSteps);
-        __syncthreads();
-    } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) q_reg[nb][s] = load_q(nb, s);
-    }
-
     f32x4 acc[NB][kColumns], sum[NB];
     float ref[NB];
     const u32x4 ones = BF16 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u} : u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 
-    // Scores of 32 tokens: lane (n, group) gets those of tokens 8 * group + 0..3 from the first tile and + 4..7 from the second.
-    auto scores = [&](const typename T::K (&k)[2], f32x4 (&s)[NB][2]) {
+    // Scores of 32 tokens: lane (n, group) gets those of tokens group, group + 4, ..., from each half four; rows n of K's operand are tokens n / 4 + 4 * (n % 4) (+ 16).
+    auto scores = [&](const char *stage, f32x4 (&s)[NB][2]) {
+        const char *const k = stage, *const z = stage + 2 * T::kKBytes;
+        u32x4 w[T::kKReads][2];
+        float scale[T::kKReads][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int r = 0; r < T::kKReads; ++r)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) s[nb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 2; ++i) {
+                const int token = (n >> 2) + 4 * (n & 3) + 16 * i;
+                if constexpr (T::kKPiece == 16) {
+                    w[r][i] = *(const u32x4 *)(k + token * T::kRow + 16 * ((4 * r + group) ^ T::k_turn(token)));
+                } else {
+                    const u32x2 v = *(const u32x2 *)(k + token * T::kRow + 8 * group);
+                    w[r][i] = u32x4{v[0], v[1], 0, 0};
+                }
+                scale[r][i] = 1.f;
+                if constexpr (T::kBlocks) scale[r][i] = scale_operand((unsigned char)z[token * (D == 256 ? 8 : 4) + (4 * r + group) * T::kKElems / kBlockElems]);
+            }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int per = T::kKElems / 8;
 #pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                const u32x4 a = T::k_operand(k[i], st);
+        for (int r = 0; r < T::kKReads; ++r)
+#pragma unroll
+            for (int e = 0; e < per; ++e) {
+                u32x4 q[NB];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    u32x4 q;
-                    if constexpr (T::kQInLds) q = q_lds[(nb * kSteps + st) * 64 + lane];
-                    else q = q_reg[nb][st];
-                    s[nb][i] = mfma32<BF16>(a, q, s[nb][i]);
+                    if constexpr (T::kQInLds) q[nb] = q_lds[(nb * kSteps + r * per + e) * 64 + lane];
+                    else q[nb] = q_reg[nb][r * per + e];
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 a;
+                    if constexpr (!T::kBlocks) a = w[r][i];
+                    else if constexpr (FORMAT == KV_FORMAT_FP8) a = decode8<BF16, FORMAT>(u32x2{w[r][i][2 * e], w[r][i][2 * e + 1]}, scale[r][i]);
+                    else a = decode8<BF16, FORMAT>(u32x2{w[r][i][e], 0}, scale[r][i]);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) s[nb][i] = mfma32<BF16>(a, q[nb], s[nb][i]);
                 }
             }
     };
-    auto product = [&](const typename T::V &v, const u32x4 (&pr)[NB][kP]) {
+    auto product = [&](const char *stage, const u32x4 (&pr)[NB][kP]) {
+        const char *const v = stage + T::kKBytes, *const z = stage + 2 * T::kKBytes + (D == 256 ? 256 : 128);
+        constexpr int kHalves = T::kVBytes == 32 ? 2 : 1, kPairs = kColumns / 2 / kHalves, kBytes = T::kVBytes / kHalves;
 #pragma unroll
         for (int t = 0; t < kP; ++t)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) sum[nb] = mfma32<BF16>(ones, pr[nb][t], sum[nb]);
+        float scale[8];
+        if constexpr (T::kBlocks) {
 #pragma unroll
-        for (int c = 0; c < kColumns; c += 2) {
-            unsigned w[8];
+            for (int j = 0; j < 8; ++j) scale[j] = scale_operand((unsigned char)z[(group + 4 * j) * (D == 256 ? 8 : 4) + kColumns * n / kBlockElems]);
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = T::v_pair(v, j, c / 2);
+        for (int half = 0; half < kHalves; ++half) {
+            unsigned w[8][kBytes < 4 ? 1 : kBytes / 4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const unsigned sel = e ? 0x07060302u : 0x05040100u;
-                const u32x4 a = {__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel),
-                                 __builtin_amdgcn_perm(w[5], w[4], sel), __builtin_amdgcn_perm(w[7], w[6], sel)};
+            for (int j = 0; j < 8; ++j) {
+                const char *const at = v + (group + 4 * j) * T::kRow + kBytes * n + half * 256;
+                if constexpr (kBytes == 2) {
+                    w[j][0] = *(const unsigned short *)at;
+                } else if constexpr (kBytes == 4) {
+                    w[j][0] = *(const unsigned *)at;
+                } else if constexpr (kBytes == 8) {
+                    const u32x2 x = *(const u32x2 *)at;
+                    w[j][0] = x[0];
+                    w[j][1] = x[1];
+                } else {
+                    const u32x4 x = *(const u32x4 *)at;
 #pragma unroll
-                for (int t = 0; t < kP; ++t)
+                    for (int e = 0; e < 4; ++e) w[j][e] = x[e];
+                }
+            }
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) acc[nb][c + e] = mfma32<BF16>(a, pr[nb][t], acc[nb][c + e]);
+            for (int c = 0; c < kPairs; ++c) {
+                unsigned y[8];   // two columns of the eight tokens
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (!T::kBlocks) y[j] = w[j][c];
+                    else if constexpr (FORMAT == KV_FORMAT_FP8) y[j] = c % 2 ? decode2<BF16, FORMAT, 1>(w[j][c / 2], scale[j]) : decode2<BF16, FORMAT, 0>(w[j][c / 2], scale[j]);
+                    else y[j] = c % 4 == 0 ? decode2<BF16, FORMAT, 0>(w[j][c / 4], scale[j]) : c % 4 == 1 ? decode2<BF16, FORMAT, 1>(w[j][c / 4], scale[j])
+                              : c % 4 == 2 ? decode2<BF16, FORMAT, 2>(w[j][c / 4], scale[j]) : decode2<BF16, FORMAT, 3>(w[j][c / 4], scale[j]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const unsigned sel = e ? 0x07060302u : 0x05040100u;
+                    const u32x4 a = {__builtin_amdgcn_perm(y[1], y[0], sel), __builtin_amdgcn_perm(y[3], y[2], sel),
+                                     __builtin_amdgcn_perm(y[5], y[4], sel), __builtin_amdgcn_perm(y[7], y[6], sel)};
+#pragma unroll
+                    for (int t = 0; t < kP; ++t)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            f32x4 &to = acc[nb][(half * kPairs + c) * 2 + e];
+                            to = mfma32<BF16>(a, pr[nb][t], to);
+                        }
+                }
             }
         }
     };
@@ -413,21 +568,27 @@ __global__ void __launch_bounds__(kTreeThreads, (kTreeWavesPerSimd<D, FORMAT, NB
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) acc[nb][c] *= f;
     };
-    // Probabilities against a reference that follows the running maximum lazily.
+    // Probabilities against a reference that follows the running maximum lazily: only where a probability came out above 2^4 are maxima formed, sums
+    // rescaled and the probabilities formed again.
     auto softmax = [&](f32x4 (&s)[NB][2], u32x4 (&pr)[NB][kP]) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const f32x4 a = s[nb][0], b4 = s[nb][1];
-            const float top = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]))) * p.scale_log2e;
-            if (__any(top > ref[nb] + kTreeRise)) {
-                const float to = fmaxf(ref[nb], groups_max(top));
+            float x[8];
+            auto exponentials = [&] {
+                const float sub = kLiftLog2<BF16> - ref[nb];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(fmaf(s[nb][j / 4][j % 4], p.scale_log2e, sub));
+                return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            };
+            if (__any(exponentials() > kMostProbability<BF16>)) {
+                float top = s[nb][0][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) top = fmaxf(top, s[nb][j / 4][j % 4]);
+                const float to = fmaxf(ref[nb], groups_max(top) * p.scale_log2e);
                 rescale(nb, __builtin_amdgcn_exp2f(ref[nb] - to));
                 ref[nb] = to;
+                (void)exponentials();
             }
-            const float sub = kLiftLog2<BF16> - ref[nb];
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(fmaf(s[nb][j / 4][j % 4], p.scale_log2e, sub));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 unsigned w[kP];
@@ -445,166 +606,201 @@ __global__ void __launch_bounds__(kTreeThreads, (kTreeWavesPerSimd<D, FORMAT, NB
         for (int c = 0; c < kColumns; ++c) acc[nb][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int n_steps = (s1 - s0 + 31) / 32;
-    const int grouped = p.grouped ? max(0, min(len, s1) - s0) / 32 : 0;   // steps of context alone, looked up by groups of eight rows
-    constexpr int kRow = D * T::kBits / 8, kZRow = D / kBlockElems;      // a pool's rows lie side by side
-    const unsigned lane_k = LAYOUT == kTreePaged ? (n & 3) * kRow : (8 * (n >> 2) + (n & 3)) * (unsigned)p.c.ss;
-    const unsigned lane_zk = LAYOUT == kTreePaged ? (n & 3) * kZRow : (8 * (n >> 2) + (n & 3)) * (unsigned)p.c.zs;
-    const unsigned lane_v = LAYOUT == kTreePaged ? 0 : 8 * group * (unsigned)p.c.ss, lane_zv = LAYOUT == kTreePaged ? 0 : 8 * group * (unsigned)p.c.zs;
-    auto block_of = [&](int j) { return p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt; };
-    unsigned id_k = 0, id_v = 0;
-    auto look_up = [&](int i) {
-        if (LAYOUT == kTreePaged && i < grouped) {
-            id_k = (unsigned)table[block_of(s0 + 32 * i + 8 * (n >> 2))];
-            id_v = (unsigned)table[block_of(s0 + 32 * i + 8 * group)];
-        }
-    };
-    look_up(wave);
-    for (int i = wave; i < n_steps; i += kTreeWaves) {
-        const int j0 = s0 + 32 * i;
-        typename T::K k[2];
-        typename T::V v;
-        unsigned there = 0xff;
-        // the lanes of K look all four groups up
-        const bool one_by_one = i >= grouped || (LAYOUT == kTreePaged && __any(id_k >= (unsigned)p.c.n_pool));
-        if (one_by_one) {
-            // where a sequence ends, drafted tokens begin, a block has no place, or blocks are no multiples of eight tokens
-            there = 0;
+    // Steps.  A stage's K is loaded again as soon as its scores are formed, its V after its product.  Loads come back in order: all but those issued later are waited for.
+    constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
+    unsigned there[kStages], stage = 0;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const RowAt r = row_at(p.c, table, base, zbase, min(j0 + 8 * (n >> 2) + (n & 3) + 4 * t, total - 1));
-                T::load_k(k[t], p.c.k + r.at, p.c.kz + r.z, group);
+    for (int m = 0; m < kStages; ++m) {
+        there[m] = ~0u;
+        if (m >= mine) continue;
+        where(m);
+        issue_rows(m, std::false_type{});
+        issue_scales(m);
+        issue_rows(m, std::true_type{});
+        there[m] = next_there;
+    }
+    if constexpr (T::kQInLds) {
+        for (int i = wave; i < NB * kSteps; i += kWaves) q_lds[i * 64 + lane] = load_q(i / kSteps, i % kSteps);
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                q_reg[nb][s] = load_q(nb, s);
+                asm volatile("" : "+v"(q_reg[nb][s]));   // arrived: a wait for them within the loop would be one for every load
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const RowAt r = row_at(p.c, table, base, zbase, min(j0 + 8 * group + j, total - 1));
-                T::load_v(v, j, p.c.v + r.at, p.c.vz + r.z, n);
-                there |= (unsigned)r.there << j;
-            }
-        } else if constexpr (LAYOUT == kTreePaged) {
-            const int jk = j0 + 8 * (n >> 2), jv = j0 + 8 * group;
-            const int in_k = jk - block_of(jk) * p.c.bt, in_v = jv - block_of(jv) * p.c.bt;
-            const char *const rk = p.c.k + base + id_k * p.c.sb + in_k * kRow + lane_k, *const zk = p.c.kz + zbase + id_k * p.c.zb + in_k * kZRow + lane_zk;
-            const char *const rv = p.c.v + base + id_v * p.c.sb + in_v * kRow, *const zv = p.c.vz + zbase + id_v * p.c.zb + in_v * kZRow;
-            T::load_k(k[0], rk, zk, group);
-            T::load_k(k[1], rk + 4 * kRow, zk + 4 * kZRow, group);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) T::load_v(v, j, rv + j * kRow, zv + j * kZRow, n);
-        } else {
-            const unsigned long long at = base + j0 * p.c.ss, z = zbase + j0 * p.c.zs;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) T::load_k(k[t], p.c.k + (at + 4 * t * p.c.ss), lane_k, p.c.kz + (z + 4 * t * p.c.zs), lane_zk, group);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) T::load_v(v, j, p.c.v + (at + j * p.c.ss), lane_v, p.c.vz + (z + j * p.c.zs), lane_zv, n);
-        }
-        look_up(i + kTreeWaves);
+    }
+
+#pragma unroll 1
+    for (int m = 0; m < mine; ++m) {
+        const bool more = m + kStages < mine;
+        if (more) where(m + kStages);
         f32x4 s[NB][2];
-        scores(k, s);
-        if (one_by_one) {
+        {
+            const int j0 = s0 + 32 * (wave + m * kWaves);
+            if (m + kStages <= mine) wait_loads<kVIssues + (kStages - 1) * (kKIssues + kVIssues)>();
+            else wait_loads<0>();
+            scores(ring + stage * T::kStage, s);
+            if (j0 + 32 > len || there[0] != ~0u) {
+                // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
+                const int row = (int)rb * kRows + here(n);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const unsigned seen = there & row_sees8(p, first, (int)rb * kRows + nb * 16 + n, j0 + 8 * group, len, total);
+                for (int nb = 0; nb < NB; ++nb) {
+                    const unsigned seen = (there[0] & row_sees32(p, first, row + nb * 16, j0, len, total)) >> group;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = seen >> j & 1 ? s[nb][j / 4][j % 4] : -INFINITY;
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = seen >> 4 * j & 1 ? s[nb][j / 4][j % 4] : -INFINITY;
+                }
             }
         }
-        u32x4 pr[NB][kP];
-        softmax(s, pr);
-        product(v, pr);
+        __builtin_amdgcn_sched_barrier(0);   // a phase's registers at a time
+        if (more) {
+            wait_reads();
+            issue_rows(stage, std::false_type{});
+        }
+        {
+            u32x4 pr[NB][kP];
+            __builtin_amdgcn_sched_barrier(0);
+            softmax(s, pr);
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) wait_loads<(kStages - 1) * (kKIssues + kVIssues) + T::kLoads>();
+            else wait_loads<0>();
+            product(ring + stage * T::kStage, pr);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            wait_reads();
+            issue_scales(stage);
+            issue_rows(stage, std::true_type{});
+        }
+#pragma unroll
+        for (int k = 0; k + 1 < kStages; ++k) there[k] = there[k + 1];
+        there[kStages - 1] = more ? next_there : ~0u;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
     }
 
     // What is not finite may be none of a row's business (a probability of zero times it), and references may have grown too large:
     // then the workgroup does its split again, row by row.
+    float finite[4] = {0.f, 0.f, 0.f, 0.f};   // zeros, or NaN
     bool bad = false;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        float worst = fabsf(sum[nb][0]);
+        finite[0] = fmaf(sum[nb][0], 0.f, finite[0]);
 #pragma unroll
         for (int c = 0; c < kColumns; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) worst = fabsf(acc[nb][c][i]) < INFINITY ? worst : INFINITY;
-        bad = bad || !(worst < INFINITY) || (fabsf(ref[nb]) > kLargeRef && ref[nb] != kNoScore);
+            for (int i = 0; i < 4; ++i) finite[i] = fmaf(acc[nb][c][i], 0.f, finite[i]);
+        bad = bad || (fabsf(ref[nb]) > kLargeRef && ref[nb] != kNoScore);
     }
-    if (__syncthreads_or(bad)) {
-        for (int r = wave; r < min(n_rows, kRows); r += kTreeWaves)
+    bad = bad || !((finite[0] + finite[1]) + (finite[2] + finite[3]) == 0.f);
+
+    // Merge: the wavefronts' references and sums become factors of their accumulators; these are added by halves: a wavefront gives the one that is not in its keeping to
+    // another and gets that one's half of what is, twice.  In the end each has a quarter of the sums of all four.
+    static_assert(kWaves == 4 && NB * kColumns % 4 == 0, "halves of halves");
+    constexpr int kTiles = NB * kColumns;
+    f32x4 *const give = (f32x4 *)lds;                                                                // [kWaves][kTiles / 2][64]
+    float *const ref_lds = (float *)(lds + T::kMerge), *const sum_lds = ref_lds + kWaves * kRows;   // [kWaves][kRows]
+    float *const bad_lds = sum_lds + kWaves * kRows;                                                // [kWaves]
+    __syncthreads();   // the rings are done with
+    if (group == 0) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            ref_lds[wave * kRows + nb * 16 + n] = ref[nb];
+            sum_lds[wave * kRows + nb * 16 + n] = sum[nb][0];
+        }
+    }
+    const bool wave_bad = __any(bad);
+    if (lane == 0) bad_lds[wave] = wave_bad ? 1.f : 0.f;
+    __syncthreads();
+    if ((bad_lds[0] + bad_lds[1]) + (bad_lds[2] + bad_lds[3]) != 0.f) {
+        for (int r = wave; r < min(n_rows, kRows); r += kWaves)
             plain_row<D, BF16, FORMAT>(p, table, base, zbase, h, first, (int)rb * kRows + r, len, total, s0, s1, split, lane);
         return;
     }
-
-    // Merge: the wavefronts' references and sums of each row, then their accumulators in two rounds.
-    constexpr int kPad = D + 4;
-    __shared__ __attribute__((aligned(16))) float rows_lds[4][kRows][kPad];
-    __shared__ float ref_lds[kTreeWaves][kRows], sum_lds[kTreeWaves][kRows];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-        if (group == 0) {
-            ref_lds[wave][nb * 16 + n] = ref[nb] - kLiftLog2<BF16>;
-            sum_lds[wave][nb * 16 + n] = sum[nb][0];
-        }
-    __syncthreads();
+    float to[NB], total_sum[NB];
+    f32x4 tiles[kTiles];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        float to = kNoScore;
+        float r[kWaves], l[kWaves];
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) to = fmaxf(to, ref_lds[w][nb * 16 + n]);
-        const float f = sum[nb][0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref[nb] - kLiftLog2<BF16> - to);
+        for (int w = 0; w < kWaves; ++w) {
+            r[w] = ref_lds[w * kRows + nb * 16 + n];
+            l[w] = sum_lds[w * kRows + nb * 16 + n];
+        }
+        to[nb] = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
+        total_sum[nb] = 0.f;
 #pragma unroll
-        for (int c = 0; c < kColumns; ++c) acc[nb][c] *= f;
+        for (int w = 0; w < kWaves; ++w) total_sum[nb] += l[w] == 0.f ? 0.f : l[w] * __builtin_amdgcn_exp2f(r[w] - to[nb]);
+        float f = sum[nb][0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref[nb] - to[nb]);
+        if (p.ns == 1) f = total_sum[nb] == 0.f ? 0.f : f / total_sum[nb];
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) tiles[nb * kColumns + c] = acc[nb][c] * f;
     }
-    auto put = [&](int buf, bool add) {
+    const bool upper = wave & 2, odd = wave & 1;
+    f32x4 half[kTiles / 2], mine_now[kTiles / 4];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int c = 0; c < kColumns; c += 4) {
-                    f32x4 *const at = (f32x4 *)&rows_lds[buf][nb * 16 + n][kColumns * (4 * group + i) + c];
-                    f32x4 x = {acc[nb][c][i], acc[nb][c + 1][i], acc[nb][c + 2][i], acc[nb][c + 3][i]};
-                    if (add) x += *at;
-                    *at = x;
-                }
-    };
-    if (wave >= 4) put(wave - 4, false);
+    for (int t = 0; t < kTiles / 2; ++t) {
+        half[t] = upper ? tiles[kTiles / 2 + t] : tiles[t];
+        give[(wave * (kTiles / 2) + t) * 64 + lane] = upper ? tiles[t] : tiles[kTiles / 2 + t];
+    }
     __syncthreads();
-    if (wave < 4) put(wave, true);
+#pragma unroll
+    for (int t = 0; t < kTiles / 2; ++t) half[t] += give[((wave ^ 2) * (kTiles / 2) + t) * 64 + lane];
     __syncthreads();
-    for (int i = threadIdx.x; i < kRows * (D / 4); i += kTreeThreads) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        if (r >= n_rows) break;
-        float to = kNoScore, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) to = fmaxf(to, ref_lds[w][r]);
+    for (int t = 0; t < kTiles / 4; ++t) {
+        mine_now[t] = odd ? half[kTiles / 4 + t] : half[t];
+        give[(wave * (kTiles / 4) + t) * 64 + lane] = odd ? half[t] : half[kTiles / 4 + t];
+    }
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) l += sum_lds[w][r] == 0.f ? 0.f : sum_lds[w][r] * __builtin_amdgcn_exp2f(ref_lds[w][r] - to);
-        f32x4 x = *(const f32x4 *)&rows_lds[0][r][d] + *(const f32x4 *)&rows_lds[1][r][d];
-        x += *(const f32x4 *)&rows_lds[2][r][d] + *(const f32x4 *)&rows_lds[3][r][d];
-        store_sums<D>(p, h, first, (int)rb * kRows + r, split, d, x, to, l);
+    for (int t = 0; t < kTiles / 4; ++t) mine_now[t] += give[((wave ^ 1) * (kTiles / 4) + t) * 64 + lane];
+
+    // The wavefront's quarter is a row group's columns from c0 on; of these a lane has those of rows 4 * group + i of the product.
+    constexpr int kShare = kTiles / 4;
+    static_assert(kColumns % kShare == 0, "of one row group");
+    const int nb = kShare * wave / kColumns, c0 = kShare * wave % kColumns, r = nb * 16 + n;
+    if (r >= n_rows) return;
+    const int t = row_token(r), hq = (int)h * p.G + (int)rb * kRows + r - t * p.G;
+    const long long part = ((long long)(first + t) * (p.H * p.G) + hq) * p.ns + split, at = p.ns == 1 ? (first + t) * p.o_st + hq * p.o_sh : part * D;
+    if (p.ns > 1 && group == 0 && c0 == 0) {
+        float ml[2] = {to[0], total_sum[0]};
+#pragma unroll
+        for (int k = 1; k < NB; ++k) {
+            ml[0] = k == nb ? to[k] : ml[0];
+            ml[1] = k == nb ? total_sum[k] : ml[1];
+        }
+        *(f32x2 *)&p.part_ml[part * 2] = f32x2{ml[0] - kLiftLog2<BF16>, ml[1]};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long o = at + T::v_column(4 * group + i, c0);
+        float x[kShare];
+#pragma unroll
+        for (int c = 0; c < kShare; ++c) x[c] = mine_now[c][i];
+        if (p.ns > 1) store_columns<kShare>(p.part_acc, o, 0, x);
+        else store_columns<kShare>(p.out, o, p.out_mode, x);
     }
 }
 
 typedef void (*TreeKernel)(TreeParams);
-template <int FORMAT, int LAYOUT, int D, int NB>
+template <int FORMAT, int D, int NB>
 TreeKernel tree_kernel_of(bool bf16, bool f32)
 {
-    return bf16 ? (f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true, LAYOUT> : kv_tree_partial_kernel<D, true, FORMAT, NB, false, LAYOUT>)
-                : (f32 ? kv_tree_partial_kernel<D, false, FORMAT, NB, true, LAYOUT> : kv_tree_partial_kernel<D, false, FORMAT, NB, false, LAYOUT>);
+    return bf16 ? (f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true> : kv_tree_partial_kernel<D, true, FORMAT, NB, false>)
+                : (f32 ? kv_tree_partial_kernel<D, false, FORMAT, NB, true> : kv_tree_partial_kernel<D, false, FORMAT, NB, false>);
 }
-template <int FORMAT, int LAYOUT>
+template <int FORMAT>
 TreeKernel tree_kernel_for(int D, bool bf16, bool f32, int nb)
 {
-    if (D == 256) return nb == 1 ? tree_kernel_of<FORMAT, LAYOUT, 256, 1>(bf16, f32) : tree_kernel_of<FORMAT, LAYOUT, 256, 2>(bf16, f32);
+    if (D == 256) return nb == 1 ? tree_kernel_of<FORMAT, 256, 1>(bf16, f32) : tree_kernel_of<FORMAT, 256, 2>(bf16, f32);
     if (D == 128)
-        return nb == 1 ? tree_kernel_of<FORMAT, LAYOUT, 128, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, LAYOUT, 128, 2>(bf16, f32)
-                                                                                     : tree_kernel_of<FORMAT, LAYOUT, 128, 4>(bf16, f32);
-    return nb == 1 ? tree_kernel_of<FORMAT, LAYOUT, 64, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, LAYOUT, 64, 2>(bf16, f32)
-                                                                                : tree_kernel_of<FORMAT, LAYOUT, 64, 4>(bf16, f32);
+        return nb == 1 ? tree_kernel_of<FORMAT, 128, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, 128, 2>(bf16, f32) : tree_kernel_of<FORMAT, 128, 4>(bf16, f32);
+    return nb == 1 ? tree_kernel_of<FORMAT, 64, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, 64, 2>(bf16, f32) : tree_kernel_of<FORMAT, 64, 4>(bf16, f32);
 }
 // In a translation unit each.
 TreeKernel tree_kernel_16(int D, bool bf16, bool f32, int nb);
-TreeKernel tree_kernel_16_paged(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp8(int D, bool bf16, bool f32, int nb);
-TreeKernel tree_kernel_fp8_paged(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp4(int D, bool bf16, bool f32, int nb);
-TreeKernel tree_kernel_fp4_paged(int D, bool bf16, bool f32, int nb);
 
 }  // namespace kvb

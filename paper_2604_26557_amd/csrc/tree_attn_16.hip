@@ -1,3 +1,3 @@
 #include "tree_attn.hpp"
 
-kvb::TreeKernel kvb::tree_kernel_16(int D, bool bf16, bool f32, int nb) { return tree_kernel_for<KV_FORMAT_16, kTreeStrided>(D, bf16, f32, nb); }
+kvb::TreeKernel kvb::tree_kernel_16(int D, bool bf16, bool f32, int nb) { return tree_kernel_for<KV_FORMAT_16>(D, bf16, f32, nb); }

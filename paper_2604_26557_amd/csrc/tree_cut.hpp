@@ -22,7 +22,7 @@ struct TreeCut {
 inline int tree_row_groups(int D, int rows) { return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4; }
 
 // Workgroups that the card holds at a time.
-inline int tree_slots(const TreeShape &s, int nb) { return s.cus * (nb == 1 && s.D * s.bits <= 512 ? 2 : 1); }
+inline int tree_slots(const TreeShape &s, int nb) { return s.cus; }
 
 // More splits than this are never made for n_tok drafted tokens: so many that each slot gets two workgroups.
 inline int tree_most_splits(const TreeShape &s, long long n_tok)

@@ -138,15 +138,15 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.part_ml = t.part_acc + (size_t)n_tok * p->Hq * cut.ns * p->D;
     t.bt_shift = -1;
     if (t.c.table && (t.c.bt & (t.c.bt - 1)) == 0) t.bt_shift = __builtin_ctz((unsigned)t.c.bt);
-    const uint64_t units = ((uint64_t)p->B * p->H * cut.ns + 7) / 8 * 8, groups = units * cut.row_blocks;
-    if (groups > INT_MAX) return KV_ERANGE;
+    // units (a split of a KV head) go in eights where they have several row blocks (the kernel's note on XCDs)
+    const uint64_t units = (uint64_t)p->B * p->H * cut.ns, groups = cut.row_blocks > 1 ? (units + 7) / 8 * 8 * cut.row_blocks : units;
+    if ((groups + 8) * std::max(std::max(cut.ns, cut.row_blocks), p->H) >= 1ull << 32) return KV_ERANGE;   // what the divisions below allow
+    auto over = [](int d) { return (unsigned)(((1ull << 32) + d - 1) / d); };
+    t.by_g = over(t.G); t.by_ns = over(cut.ns); t.by_h = over(p->H); t.by_row_blocks = over(cut.row_blocks);
     const bool f32 = t.out_mode == 0;
-    const bool paged = t.c.table != nullptr;
-    // 32 rows and their scales within 32-bit offsets; blocks of whole groups, their scales' rows side by side
-    t.grouped = paged ? t.c.bt % 8 == 0 && (!blocks || t.c.zs == (uint64_t)p->D / kBlockElems) : t.c.ss < 1ull << 26 && t.c.zs < 1ull << 26;
-    TreeKernel k = format == KV_FORMAT_FP8   ? (paged ? tree_kernel_fp8_paged : tree_kernel_fp8)(p->D, bf16, f32, cut.nb)
-                   : format == KV_FORMAT_FP4 ? (paged ? tree_kernel_fp4_paged : tree_kernel_fp4)(p->D, bf16, f32, cut.nb)
-                                             : (paged ? tree_kernel_16_paged : tree_kernel_16)(p->D, bf16, f32, cut.nb);
+    // offsets of a step's rows, and of a block, fit 32 bits; blocks hold whole groups of 16
+    t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < 1ull << 16 : t.c.ss < 1ull << 26 && t.c.zs < 1ull << 26;
+    TreeKernel k = (format == KV_FORMAT_FP8 ? tree_kernel_fp8 : format == KV_FORMAT_FP4 ? tree_kernel_fp4 : tree_kernel_16)(p->D, bf16, f32, cut.nb);
     hipStream_t st = (hipStream_t)hip_stream;
     (void)launch_kernel(k, dim3((unsigned)groups), dim3(kTreeThreads), st, t);
     hipError_t e = hipGetLastError();
