@@ -45,6 +45,14 @@ constexpr int format_bits(int format) { return format == KV_FORMAT_16 ? 16 : for
 // sequence b may be touched.
 int cache_addr(const kv_plan *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const int *lens, const int *first, CacheAddr *c);
 
+// Heads of a row that a thread of the row kernels goes over: what it looks up of the row (its place, the angles of its position) serves all of them, but with few
+// rows they are rather worked on side by side.  Four once that leaves 2048 wavefronts, two with half of it.
+inline int heads_per_thread(long long n_tok, int n_heads, int vectors)
+{
+    const long long waves = n_tok * n_heads * vectors / 64;
+    return n_heads >= 4 && waves >= 4 * 2048 ? 4 : n_heads >= 2 && waves >= 2 * 1024 ? 2 : 1;
+}
+
 // A rotary table that fits head_dim.
 int check_rope(const kv_rope_t *r, int head_dim);
 

@@ -23,6 +23,7 @@ struct RowParams {
     const int *positions;
     int n_pos, rot;
     int n_heads, vectors;              // vectors of 8 elements in a head's row
+    int n_rows;
     unsigned n_items;                  // of K; as many of V in the grid's second row
 };
 
@@ -77,103 +78,138 @@ __device__ __forceinline__ u32x2 encode8(u32x4 x, unsigned *scale)
     }
 }
 
-// Item i: vector, head and row of K (blockIdx.y = 0) or V.  The four vectors of a block are neighbouring lanes: head_dim is a multiple of 32.
+// A thread has a vector column of a row, found once, in HPT heads of K (blockIdx.y = 0) or V.  Neighbouring lanes have a row's vectors, then the next rows': what lies
+// side by side in the call's rows or in the cache is read and written by one wavefront.  The four vectors of a block are neighbouring lanes: head_dim is a multiple of 32.
 struct Item {
     unsigned v, h, t;
     bool is_v;
 };
+template <int HPT>
 __device__ __forceinline__ bool item_of(const RowParams &p, Item *it)
 {
     const unsigned i = blockIdx.x * kThreads + threadIdx.x;
     if (i >= p.n_items) return false;
-    const unsigned r = i / (unsigned)p.vectors;
-    *it = Item{i - r * (unsigned)p.vectors, r % (unsigned)p.n_heads, r / (unsigned)p.n_heads, blockIdx.y != 0};
+    const unsigned r = i / (unsigned)p.vectors, g = r / (unsigned)p.n_rows;   // head groups one after the other
+    *it = Item{i - r * (unsigned)p.vectors, g * HPT, r - g * (unsigned)p.n_rows, blockIdx.y != 0};
     return true;
-}
-__device__ __forceinline__ char *row_of(const RowParams &p, const Item &it)
-{
-    return (it.is_v ? p.v : p.k) + it.t * (it.is_v ? p.v_st : p.k_st) + it.h * (it.is_v ? p.v_sh : p.k_sh);
 }
 
 // Bytes of a vector of eight elements.
 constexpr int vector_bytes(int format) { return format_bits(format); }
 
-template <bool BF16, int FORMAT, bool PAIRS>
+template <bool BF16, int FORMAT, bool PAIRS, int HPT>
 __global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(RowParams p)
 {
     Item it;
-    if (!item_of(p, &it)) return;
+    if (!item_of<HPT>(p, &it)) return;
     unsigned block, row;
     if (!find_row(p.c, p.tok_seq[it.t], p.tok_slot[it.t], &block, &row)) return;  // a block's lanes share the row: all leave or none
-    const char *const src = row_of(p, it);
-    u32x4 x = *(const u32x4 *)(src + 16 * it.v);
-    if (p.table && !it.is_v && it.v < (unsigned)p.rot / 8) {
+    const char *const src = (it.is_v ? p.v + it.t * p.v_st : p.k + it.t * p.k_st);
+    const long long sh = it.is_v ? p.v_sh : p.k_sh;
+    char *const dst = (char *)(it.is_v ? p.c.v : p.c.k) + block * p.c.sb + row * p.c.ss + vector_bytes(FORMAT) * it.v;
+    char *const scales = (char *)(it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + row * p.c.zs + it.v / 4;
+    const bool turned = p.table && !it.is_v && it.v < (unsigned)p.rot / 8;
+    const unsigned half = (unsigned)p.rot / 16;   // vectors
+    const bool second = it.v >= half;
+    Angles<8> ang;
+    if (turned) {
         const int pos = p.positions[it.t];
         if constexpr (PAIRS) {
-            const Angles<4> ang = load_angles<4>(p.table, p.n_pos, p.rot / 2, pos, 4 * it.v, 1.f);
-            turn_pairs<BF16>(x, ang, 0);
+            const Angles<4> a = load_angles<4>(p.table, p.n_pos, p.rot / 2, pos, 4 * it.v, 1.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) ang.c[k] = a.c[k], ang.s[k] = a.s[k];
         } else {
-            const unsigned half = (unsigned)p.rot / 16;  // vectors
-            const bool second = it.v >= half;
-            u32x4 other = *(const u32x4 *)(src + 16 * (second ? it.v - half : it.v + half));
-            const Angles<8> ang = load_angles<8>(p.table, p.n_pos, p.rot / 2, pos, 8 * (second ? it.v - half : it.v), 1.f);
-            u32x4 a = second ? other : x, b = second ? x : other;
-            turn_halves<BF16>(a, b, ang);
-            x = second ? b : a;
+            ang = load_angles<8>(p.table, p.n_pos, p.rot / 2, pos, 8 * (second ? it.v - half : it.v), 1.f);
         }
     }
-    char *const dst = (char *)(it.is_v ? p.c.v : p.c.k) + block * p.c.sb + it.h * p.c.sh + row * p.c.ss + vector_bytes(FORMAT) * it.v;
-    if constexpr (FORMAT == KV_FORMAT_16) {
-        *(u32x4 *)dst = x;
-    } else {
-        unsigned byte;
-        const u32x2 w = encode8<BF16, FORMAT>(x, &byte);
-        if constexpr (FORMAT == KV_FORMAT_FP8) *(u32x2 *)dst = w;
-        else *(unsigned *)dst = w[0];
-        char *const z = (char *)(it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + it.h * p.c.zh + row * p.c.zs;
-        if (it.v % 4 == 0) z[it.v / 4] = (char)byte;
+    u32x4 x[HPT], other[HPT];
+#pragma unroll
+    for (int k = 0; k < HPT; ++k) {
+        const char *const at = src + min(it.h + k, (unsigned)p.n_heads - 1) * sh;   // a head past the last one is not stored
+        x[k] = *(const u32x4 *)(at + 16 * it.v);
+        if (!PAIRS && turned) other[k] = *(const u32x4 *)(at + 16 * (second ? it.v - half : it.v + half));
+    }
+#pragma unroll
+    for (int k = 0; k < HPT; ++k) {
+        const unsigned h = it.h + k;
+        if (h >= (unsigned)p.n_heads) break;
+        if (turned) {
+            if constexpr (PAIRS) {
+                turn_pairs<BF16>(x[k], ang, 0);
+            } else {
+                u32x4 a = second ? other[k] : x[k], b = second ? x[k] : other[k];
+                turn_halves<BF16>(a, b, ang);
+                x[k] = second ? b : a;
+            }
+        }
+        if constexpr (FORMAT == KV_FORMAT_16) {
+            *(u32x4 *)(dst + h * p.c.sh) = x[k];
+        } else {
+            unsigned byte;
+            const u32x2 w = encode8<BF16, FORMAT>(x[k], &byte);
+            if constexpr (FORMAT == KV_FORMAT_FP8) *(u32x2 *)(dst + h * p.c.sh) = w;
+            else *(unsigned *)(dst + h * p.c.sh) = w[0];
+            if (it.v % 4 == 0) scales[h * p.c.zh] = (char)byte;
+        }
     }
 }
 
-template <bool BF16, int FORMAT>
+template <bool BF16, int FORMAT, bool, int HPT>
 __global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(RowParams p)
 {
     Item it;
-    if (!item_of(p, &it)) return;
+    if (!item_of<HPT>(p, &it)) return;
     unsigned block, row;
     if (!find_row(p.c, p.tok_seq[it.t], p.tok_slot[it.t], &block, &row)) return;
-    const char *const src = (it.is_v ? p.c.v : p.c.k) + block * p.c.sb + it.h * p.c.sh + row * p.c.ss + vector_bytes(FORMAT) * it.v;
-    u32x4 x;
-    if constexpr (FORMAT == KV_FORMAT_16) {
-        x = *(const u32x4 *)src;
-    } else {
-        const char *const z = (it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + it.h * p.c.zh + row * p.c.zs;
-        u32x2 w;
-        if constexpr (FORMAT == KV_FORMAT_FP8) w = *(const u32x2 *)src;
-        else w = u32x2{*(const unsigned *)src, 0};
-        x = decode8<BF16, FORMAT>(w, scale_operand((unsigned char)z[it.v / 4]));
+    const char *const src = (it.is_v ? p.c.v : p.c.k) + block * p.c.sb + row * p.c.ss + vector_bytes(FORMAT) * it.v;
+    const char *const scales = (it.is_v ? p.c.vz : p.c.kz) + block * p.c.zb + row * p.c.zs + it.v / 4;
+    char *const dst = (it.is_v ? p.v + it.t * p.v_st : p.k + it.t * p.k_st) + 16 * it.v;
+    const long long sh = it.is_v ? p.v_sh : p.k_sh;
+    u32x4 x[HPT];
+    unsigned byte[HPT];
+#pragma unroll
+    for (int k = 0; k < HPT; ++k) {
+        const unsigned h = min(it.h + k, (unsigned)p.n_heads - 1);
+        if constexpr (FORMAT == KV_FORMAT_16) {
+            x[k] = *(const u32x4 *)(src + h * p.c.sh);
+        } else if constexpr (FORMAT == KV_FORMAT_FP8) {
+            const u32x2 w = *(const u32x2 *)(src + h * p.c.sh);
+            x[k] = u32x4{w[0], w[1], 0, 0};
+        } else {
+            x[k] = u32x4{*(const unsigned *)(src + h * p.c.sh), 0, 0, 0};
+        }
+        if constexpr (FORMAT != KV_FORMAT_16) byte[k] = (unsigned char)scales[h * p.c.zh];
     }
-    *(u32x4 *)(row_of(p, it) + 16 * it.v) = x;
+#pragma unroll
+    for (int k = 0; k < HPT; ++k) {
+        const unsigned h = it.h + k;
+        if (h >= (unsigned)p.n_heads) break;
+        if constexpr (FORMAT != KV_FORMAT_16) x[k] = decode8<BF16, FORMAT>(u32x2{x[k][0], x[k][1]}, scale_operand(byte[k]));
+        __builtin_nontemporal_store(x[k], (u32x4 *)(dst + h * sh));
+    }
 }
 
 typedef void (*RowKernel)(RowParams);
-template <bool BF16>
-RowKernel write_kernel(int format, bool pairs)
+template <bool BF16, int HPT>
+RowKernel kernel_of(bool write, int format, bool pairs)
 {
-    if (format == KV_FORMAT_FP8) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP8, true> : kv_cache_write_kernel<BF16, KV_FORMAT_FP8, false>;
-    if (format == KV_FORMAT_FP4) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP4, true> : kv_cache_write_kernel<BF16, KV_FORMAT_FP4, false>;
-    return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_16, true> : kv_cache_write_kernel<BF16, KV_FORMAT_16, false>;
+    if (write) {
+        if (format == KV_FORMAT_FP8) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP8, true, HPT> : kv_cache_write_kernel<BF16, KV_FORMAT_FP8, false, HPT>;
+        if (format == KV_FORMAT_FP4) return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_FP4, true, HPT> : kv_cache_write_kernel<BF16, KV_FORMAT_FP4, false, HPT>;
+        return pairs ? kv_cache_write_kernel<BF16, KV_FORMAT_16, true, HPT> : kv_cache_write_kernel<BF16, KV_FORMAT_16, false, HPT>;
+    }
+    return format == KV_FORMAT_FP8   ? kv_cache_read_kernel<BF16, KV_FORMAT_FP8, false, HPT>
+           : format == KV_FORMAT_FP4 ? kv_cache_read_kernel<BF16, KV_FORMAT_FP4, false, HPT>
+                                     : kv_cache_read_kernel<BF16, KV_FORMAT_16, false, HPT>;
 }
-template <bool BF16>
-RowKernel read_kernel(int format)
+RowKernel kernel_of(bool bf16, int heads, bool write, int format, bool pairs)
 {
-    if (format == KV_FORMAT_FP8) return kv_cache_read_kernel<BF16, KV_FORMAT_FP8>;
-    if (format == KV_FORMAT_FP4) return kv_cache_read_kernel<BF16, KV_FORMAT_FP4>;
-    return kv_cache_read_kernel<BF16, KV_FORMAT_16>;
+    if (bf16) return heads == 1 ? kernel_of<true, 1>(write, format, pairs) : heads == 2 ? kernel_of<true, 2>(write, format, pairs) : kernel_of<true, 4>(write, format, pairs);
+    return heads == 1 ? kernel_of<false, 1>(write, format, pairs) : heads == 2 ? kernel_of<false, 2>(write, format, pairs) : kernel_of<false, 4>(write, format, pairs);
 }
 
 // Checks of the rows of a call and the launch, shared by both directions; p holds the cache's place and the rotary table.
-int launch_rows(const kv_plan *pl, RowParams &p, RowKernel kernel, const void *k, const void *v, int64_t k_st, int64_t k_sh, int64_t v_st, int64_t v_sh,
+int launch_rows(const kv_plan *pl, RowParams &p, bool write, int format, bool pairs, const void *k, const void *v, int64_t k_st, int64_t k_sh, int64_t v_st, int64_t v_sh,
                 const int32_t *tok_seq, const int32_t *tok_slot, const int32_t *positions, int n_tok, void *hip_stream)
 {
     if (n_tok < 0 || k_st < 0 || k_sh < 0 || v_st < 0 || v_sh < 0 || ((k_st | k_sh | v_st | v_sh) & 7)) return KV_EINVAL;
@@ -182,7 +218,9 @@ int launch_rows(const kv_plan *pl, RowParams &p, RowKernel kernel, const void *k
     p.k_st = 2 * k_st; p.k_sh = 2 * k_sh; p.v_st = 2 * v_st; p.v_sh = 2 * v_sh;
     p.n_heads = pl->H;
     p.vectors = pl->D / 8;
-    const long long per_tok = (long long)p.n_heads * p.vectors;
+    const int heads = heads_per_thread(n_tok, p.n_heads, p.vectors), head_groups = (p.n_heads + heads - 1) / heads;
+    const RowKernel kernel = kernel_of(pl->dtype == KV_BF16, heads, write, format, pairs);
+    const long long per_tok = (long long)head_groups * p.vectors;
     const long long most = (1ll << 31) / per_tok;  // tokens of a launch: items are counted in 32 bits
     if (most < 1) return KV_ERANGE;
     for (long long t0 = 0; t0 < n_tok; t0 += most) {
@@ -193,6 +231,7 @@ int launch_rows(const kv_plan *pl, RowParams &p, RowKernel kernel, const void *k
         p.tok_slot = tok_slot + t0;
         p.positions = positions ? positions + t0 : nullptr;
         p.n_items = (unsigned)(n * per_tok);
+        p.n_rows = (int)n;
         (void)launch_kernel(kernel, dim3((p.n_items + kThreads - 1) / kThreads, 2), dim3(kThreads), (hipStream_t)hip_stream, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
@@ -282,7 +321,7 @@ extern "C" int kv_cache_write(const kv_plan_t *p, const kv_view_t *view, const k
         pairs = a->rope->style == KV_ROPE_PAIRS;
     }
     const int format = blocks ? blocks->format : KV_FORMAT_16;
-    return launch_rows(p, r, p->dtype == KV_BF16 ? write_kernel<true>(format, pairs) : write_kernel<false>(format, pairs), a->k, a->v, a->k_stride_t,
+    return launch_rows(p, r, true, format, pairs, a->k, a->v, a->k_stride_t,
                        a->k_stride_h, a->v_stride_t, a->v_stride_h, a->tok_seq, a->tok_slot, a->positions, a->n_tok, hip_stream);
 }
 
@@ -293,6 +332,6 @@ extern "C" int kv_cache_read(const kv_plan_t *p, const kv_view_t *view, const kv
     const int rc = cache_addr(p, view, blocks, layer, nullptr, nullptr, &r.c);
     if (rc != KV_OK) return rc;
     const int format = blocks ? blocks->format : KV_FORMAT_16;
-    return launch_rows(p, r, p->dtype == KV_BF16 ? read_kernel<true>(format) : read_kernel<false>(format), a->k, a->v, a->k_stride_t, a->k_stride_h,
+    return launch_rows(p, r, false, format, false, a->k, a->v, a->k_stride_t, a->k_stride_h,
                        a->v_stride_t, a->v_stride_h, a->tok_seq, a->tok_slot, nullptr, a->n_tok, hip_stream);
 }

@@ -137,7 +137,8 @@ extern "C" int kv_rope(const kv_rope_t *r, const kv_rope_args_t *a, void *hip_st
     p.x_st = 2 * a->x_stride_t; p.x_sh = 2 * a->x_stride_h; p.o_st = 2 * a->out_stride_t; p.o_sh = 2 * a->out_stride_h;
     p.sign = a->transposed ? -1.f : 1.f;
     p.n_pos = r->n_pos; p.rot = r->rot_dim; p.n_heads = a->n_heads; p.chunks = a->head_dim / 16;
-    const long long per_tok = (long long)a->n_heads * p.chunks;
+    const int heads = heads_per_thread(a->n_tok, a->n_heads, p.chunks);
+    const long long per_tok = (long long)((a->n_heads + heads - 1) / heads) * p.chunks;
     const long long most = (1ll << 31) / per_tok;  // tokens of a launch: items are counted in 32 bits
     if (most < 1) return KV_ERANGE;
     for (long long t0 = 0; t0 < a->n_tok; t0 += most) {
@@ -146,7 +147,8 @@ extern "C" int kv_rope(const kv_rope_t *r, const kv_rope_args_t *a, void *hip_st
         p.out = (char *)a->out + t0 * p.o_st;
         p.positions = a->positions + t0;
         p.n_items = (unsigned)(n * per_tok);
-        launch<1>(a->dtype == KV_BF16, r->style == KV_ROPE_PAIRS, dim3((p.n_items + kThreads - 1) / kThreads), (hipStream_t)hip_stream, p);
+        const dim3 grid((p.n_items + kThreads - 1) / kThreads);
+        (heads == 4 ? launch<4> : heads == 2 ? launch<2> : launch<1>)(a->dtype == KV_BF16, r->style == KV_ROPE_PAIRS, grid, (hipStream_t)hip_stream, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     }

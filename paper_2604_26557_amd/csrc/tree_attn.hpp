@@ -25,6 +25,7 @@ struct TreeParams {
     int ns, split_tokens, row_blocks;
     int bt_shift;                      // log2 of a block's tokens, or -1
     unsigned by_g, by_ns, by_h, by_row_blocks;  // 2^32 over G, ..., rounded up: x / G = x * by_g >> 32 as long as x * G < 2^32
+    int dense;                         // rows of a head lie side by side
     int grouped;                       // rows of context are looked up by groups of 16
 };
 
@@ -185,6 +186,23 @@ __device__ __forceinline__ void load_to_lds16(unsigned long long start, unsigned
     start = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)start) | (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(start >> 32)) << 32;
     if constexpr (NT) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(start), "s"(lds) : "memory");
     else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(start), "s"(lds) : "memory");
+}
+// N of them (1, 2 or 4) with both ends a kilobyte further each; the q-th's lane offset is offset ^ (q * TURN & MASK).
+template <bool NT, int N, int TURN, int MASK>
+__device__ __forceinline__ void load_run(unsigned long long start, unsigned offset, unsigned lds)
+{
+    start = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)start) | (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(start >> 32)) << 32;
+    const unsigned o1 = offset ^ (TURN & MASK), o2 = offset ^ (2 * TURN & MASK), o3 = offset ^ (3 * TURN & MASK);
+#define KV_LOAD(O, OFFSET, HINT) "\n\tglobal_load_lds_dwordx4 " O ", %0 offset:" OFFSET HINT
+#define KV_RUN(HINT)                                                                                                                                          \
+    if constexpr (N == 1) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0" KV_LOAD("%2", "0", HINT)::"s"(start), "s"(lds), "v"(offset) : "memory");                   \
+    else if constexpr (N == 2) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0" KV_LOAD("%2", "0", HINT) KV_LOAD("%3", "1024", HINT)::"s"(start), "s"(lds), "v"(offset), "v"(o1) : "memory"); \
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0" KV_LOAD("%2", "0", HINT) KV_LOAD("%3", "1024", HINT) KV_LOAD("%4", "2048", HINT) KV_LOAD("%5", "3072", HINT) \
+                      ::"s"(start), "s"(lds), "v"(offset), "v"(o1), "v"(o2), "v"(o3) : "memory");
+    if constexpr (NT) { KV_RUN(" nt") }
+    else { KV_RUN("") }
+#undef KV_RUN
+#undef KV_LOAD
 }
 // x as if it was new here: what follows from it is computed where it is used, and not kept in registers that the loop has none of.
 __device__ __forceinline__ int here(int x)
@@ -410,7 +428,15 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         const char *const rows = V ? p.c.v : p.c.k;
         const unsigned to = lds_at + stage * T::kStage + (V ? T::kKBytes : 0);
         const int l = here(lane), piece = l % T::kPieces, slot = l / T::kPieces;   // of a load
-        if (groups) {
+        if (groups && p.dense && T::kTokens <= 16) {
+            // rows side by side: what a load brings of a row is where the lane is, and both ends of the loads of 16 rows are a kilobyte apart
+            constexpr int kHalf = T::kRow / 64, kRun = kHalf < 4 ? kHalf : 4;   // loads of 16 rows, and of them with one start
+            constexpr int kTurn = V ? 0 : T::kPieces >= 16 ? 16 * T::kTokens : T::kPieces == 8 ? 64 : 0, kMask = 16 * (T::kPieces < 16 ? T::kPieces : 16) - 1;
+            const unsigned from = 16 * (V ? l : l ^ T::k_turn(slot));
+#pragma unroll
+            for (int q = 0; q < 2 * kHalf; q += kRun)
+                load_run<kNT, kRun, kTurn, kMask>((unsigned long long)rows + (q < kHalf ? at0 : at1) + q % kHalf * 1024, from ^ (q % kHalf * kTurn & kMask), to + q * 1024);
+        } else if (groups) {
             const unsigned lane_row = (unsigned)slot * (unsigned)p.c.ss;
 #pragma unroll
             for (int q = 0; q < T::kLoads; ++q) {

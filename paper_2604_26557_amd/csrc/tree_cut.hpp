@@ -10,21 +10,16 @@ constexpr int kMaxTreeSplits = 128;
 
 struct TreeShape {
     int D, H, G, bits, cus;  // bits of an element in the cache
+    bool paged;
 };
 struct TreeCut {
-    int nb;            // 16-row groups of a workgroup: 1, 2 or 4
+    int nb;            // 16-row groups of a workgroup: 1, 2 or 4 (at head_dim 256 no more than 2: four groups' sums do not fit the registers)
     int row_blocks;    // workgroups that share a KV head's rows of the sequence with the most
     int ns;            // splits of the longest sequence
     int split_tokens;  // a multiple of 32
 };
 
-// 16-row groups of a workgroup that has up to `rows` query rows of a KV head.  At head_dim 256 four groups' sums do not fit the registers.
-inline int tree_row_groups(int D, int rows) { return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4; }
-
-// Workgroups that the card holds at a time.
-inline int tree_slots(const TreeShape &s, int nb) { return s.cus; }
-
-// More splits than this are never made for n_tok drafted tokens: so many that each slot gets two workgroups.
+// No more splits than this for n_tok drafted tokens: so many that a compute unit gets about four workgroups of 64 rows.
 inline int tree_most_splits(const TreeShape &s, long long n_tok)
 {
     const long long blocks = std::max<long long>(1, (n_tok * s.G + 63) / 64) * s.H;
@@ -33,47 +28,70 @@ inline int tree_most_splits(const TreeShape &s, long long n_tok)
 
 inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (uint64_t)n_tok * s.H * s.G * (s.D + 2) * sizeof(float); }
 
+// Both choices go by an estimate of the time in us, fitted to what 15 shapes took with 3 row groups times 16 split counts each (head_dim 64 to 256, the three formats, 1 to
+// 64 drafted tokens, contexts of 256 to 32K):
+//   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on a compute unit adds 60 % of that;
+//   the whole cache through HBM once;  where there are splits a second launch, and partial results written and read.
+// Its choice was within 5 % of a shape's best on 9 of the 15 and within 12 % on all; 64 rows and 256 workgroups for every shape were up to 40 % off.
 inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *first, int n_splits, uint64_t ws_bytes)
 {
     int rows = 0, longest = 0;
+    bool uniform = true;
+    double blocks[3] = {0, 0, 0}, tokens[3] = {0, 0, 0}, context = 0;  // by row groups: workgroups without splits, and the tokens they go over
     for (int b = 0; b < B; ++b) {
-        const int t = first[b + 1] - first[b];
+        const int t = first[b + 1] - first[b], total = lens[b] + t;
         if (t == 0) continue;
+        uniform = uniform && (longest == 0 || longest == total);
         rows = std::max(rows, t * s.G);
-        longest = std::max(longest, lens[b] + t);
+        longest = std::max(longest, total);
+        context += total;
+        for (int k = 0; k < 3; ++k) {
+            const int n = (t * s.G + (16 << k) - 1) / (16 << k);
+            blocks[k] += n;
+            tokens[k] += (double)n * total;
+        }
     }
-    TreeCut c{};
-    c.nb = tree_row_groups(s.D, rows);
-    const int block = 16 * c.nb;
-    c.row_blocks = (rows + block - 1) / block;
-    double blocks = 0, tokens = 0;  // workgroups without splits, and the tokens they go over
-    for (int b = 0; b < B; ++b) {
-        const int t = first[b + 1] - first[b], n = (t * s.G + block - 1) / block;
-        blocks += n;
-        tokens += (double)n * (lens[b] + t);
-    }
-    blocks *= s.H;
-    tokens *= s.H;
     const long long n_tok = first[B];
     const int fit = (int)std::min<uint64_t>(kMaxTreeSplits, ws_bytes / tree_split_bytes(s, n_tok));
     const int most = std::max(1, std::min(fit, n_splits > 0 ? n_splits : tree_most_splits(s, n_tok)));
-    int best = most;
-    if (n_splits == 0) {
-        // us: what HBM needs for the whole, or the fullest slot for its workgroups (each 32 tokens of a wavefront, bytes or products), and the second launch
-        const int slots = tree_slots(s, c.nb);
-        const double row = 2.0 * s.D * s.bits / 8, hbm = tokens / std::max(1, c.row_blocks) * row / 6.0e6;
-        const double token = std::max(row / 50e3, 4.0 * block * s.D / 2.5e6) * (slots / s.cus);
-        double least = 1e30;
-        for (int ns = 1; ns <= most; ns = ns < 4 ? ns + 1 : ns + ns / 4) {
-            const int st = (longest + ns - 1) / ns;
-            const double items = ns == 1 ? blocks : tokens / st + 0.5 * blocks, turns = std::max(1.0, items / slots);
-            const double us = std::max(hbm, std::max(std::max<double>(st, 256) * token, turns * st * token)) + (ns > 1 ? 3.0 + 0.02 * ns : 0);
-            if (us < least) least = us, best = ns;
+    const double hbm = context * s.H * 2.0 * s.D * s.bits / 8 / 5.5e6, part = 2.0 * n_tok * s.H * s.G * s.D * 4 / 3.5e6;
+    constexpr int kCounted = 16;   // sequences whose workgroups are counted one by one: for more, and split, half a workgroup each is added
+    TreeCut best{};
+    double least = 1e30;
+    for (int k = 0; k < (s.D == 256 ? 2 : 3); ++k) {
+        const int nb = 1 << k;
+        if (k > 0 && rows <= 8 * nb) break;   // half of the rows would be none
+        const double per_row = 0.2 * nb * s.D / 128 * (s.D == 256 ? 1.5 : 1);
+        const double step = (s.D == 256 ? 1.2 : 0.85) + per_row + (s.bits < 16 ? 0.05 * nb : 0) + (s.paged ? 0.2 : 0), start = 3.2 + 1.3 * nb;
+        for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32) {
+            const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
+            double items = blocks[k];
+            if (ns > 1 && uniform) {
+                items *= (longest + st - 1) / st;
+            } else if (ns > 1 && B <= kCounted) {
+                items = 0;
+                for (int b = 0; b < B; ++b) {
+                    const int t = first[b + 1] - first[b];
+                    items += (t * s.G + 16 * nb - 1) / (16 * nb) * ((lens[b] + t + st - 1) / st);
+                }
+            } else if (ns > 1) {
+                items = tokens[k] / st + 0.5 * blocks[k];
+            }
+            items *= s.H;
+            double turns = std::max(1.0, items / s.cus);   // workgroups of the fullest compute unit
+            if (uniform) turns = (double)(long long)(turns + 0.9);
+            else if (turns > 1) turns += 0.25;
+            const double us = std::max(hbm + start / 2, (start + (st + 127) / 128 * step) * (1 + 0.6 * (turns - 1))) + (ns > 1 ? 3.0 + ns * (part + 0.05) : 0);
+            if (us < least) {
+                least = us;
+                best.nb = nb;
+                best.split_tokens = st;
+            }
         }
     }
-    c.split_tokens = ((longest + best - 1) / best + 31) / 32 * 32;
-    c.ns = std::max(1, (longest + c.split_tokens - 1) / std::max(1, c.split_tokens));
-    return c;
+    best.row_blocks = (rows + 16 * best.nb - 1) / (16 * best.nb);
+    best.ns = std::max(1, (longest + best.split_tokens - 1) / std::max(1, best.split_tokens));
+    return best;
 }
 
 }  // namespace kvb

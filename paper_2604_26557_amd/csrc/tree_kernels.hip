@@ -12,53 +12,71 @@ namespace {
 
 using namespace kvb;
 
-// A wavefront merges the splits of one query row.
+// A wavefront merges the splits of one query row: lane = split for the weights, which it takes from the lanes, and loads of a round of splits at a time.
 constexpr int kCombineWaves = 4;
 template <int D>
-__global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(TreeParams p, int n_rows)
+__global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(TreeParams p)
 {
-    constexpr int kLanes = D / 4, kTogether = 64 / kLanes;   // lanes of a row, splits at a time
-    const int row = blockIdx.x * kCombineWaves + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (row >= n_rows) return;
-    const int Hq = p.H * p.G, t = row / Hq, hq = row - t * Hq;
-    int lo = 0, hi = p.B - 1;   // the last sequence that starts at or before t
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (p.tok_first[mid] <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    const int drafted = min(p.tok_first[lo + 1] - p.tok_first[lo], KV_TREE_MAX);
-    const int total = max(0, min(p.seq_lens[lo], p.max_total - drafted)) + drafted;
+    constexpr int kLanes = D / 4, kTogether = 64 / kLanes, kRound = 8;   // lanes of a row; splits at a time; of them on their way
+    const int b = blockIdx.y, lane = threadIdx.x & 63, Hq = p.H * p.G;
+    const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * kCombineWaves + (int)(threadIdx.x >> 6));
+    const int first = load_uniform(p.tok_first + b), drafted = min(load_uniform(p.tok_first + b + 1) - first, KV_TREE_MAX);
+    const int total = max(0, min(load_uniform(p.seq_lens + b), p.max_total - drafted)) + drafted;
+    if (r >= drafted * Hq) return;
+    const int t = first + r / Hq, hq = r % Hq;
     const int ns = min(p.ns, (total + p.split_tokens - 1) / p.split_tokens);
-    const f32x2 *const ml = (const f32x2 *)p.part_ml + (long long)row * p.ns;
-    const float *const part = p.part_acc + (long long)row * p.ns * D;
+    const long long row = (long long)t * Hq + hq;
+    const f32x2 *const ml = (const f32x2 *)p.part_ml + row * p.ns;
     const int sub = lane / kLanes, d = lane % kLanes * 4;
-    float to = kNoScore;
-    for (int s = 0; s < ns; ++s) to = fmaxf(to, ml[s][0]);
-    float l = 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < ns; ++s) l += ml[s][1] == 0.f ? 0.f : ml[s][1] * __builtin_amdgcn_exp2f(ml[s][0] - to);
-    for (int s = sub; s < ns; s += kTogether) {
-        const float f = ml[s][1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(ml[s][0] - to), 1.0e-37f);   // an infinity stays one
-        const f32x4 y = *(const f32x4 *)&part[(long long)s * D + d];
+    const float *const part = p.part_acc + row * p.ns * D + d;
+    const f32x2 m0 = lane < ns ? ml[lane] : f32x2{kNoScore, 0.f}, m1 = 64 + lane < ns ? ml[64 + lane] : f32x2{kNoScore, 0.f};
+    f32x4 y[kRound];
+    auto load = [&](int s0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = fmaf(y[k], f, x[k]);
+        for (int k = 0; k < kRound; ++k) {
+            const int s = s0 + k * kTogether + sub;
+            if (s0 + k * kTogether < ns) y[k] = *(const f32x4 *)&part[(long long)(s < ns ? s : 0) * D];
+        }
+    };
+    load(0);
+    float to = fmaxf(m0[0], m1[0]);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) to = fmaxf(to, __shfl_xor(to, o));
+    // an infinity stays one: no weight of a split that has something is zero
+    const float w0 = m0[1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m0[0] - to), 1.0e-37f), w1 = m1[1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m1[0] - to), 1.0e-37f);
+    float l = m0[1] * w0 + m1[1] * w1;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) l += __shfl_xor(l, o);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < ns; s0 += kRound * kTogether) {
+        if (s0 > 0) load(s0);
+#pragma unroll
+        for (int k = 0; k < kRound; ++k) {
+            const int s = s0 + k * kTogether + sub;
+            if (s0 + k * kTogether >= ns) break;
+            const float f = __shfl(s0 < 64 ? w0 : w1, s & 63);
+            if (s < ns && f != 0.f) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = fmaf(y[k][e], f, x[e]);
+            }
+        }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        for (int o = kLanes; o < 64; o *= 2) x[k] += __shfl_xor(x[k], o);
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int o = kLanes; o < 64; o *= 2) x[e] += __shfl_xor(x[e], o);
     }
     if (sub == 0) store_four(p.out, t * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
 }
 
-TreeShape shape_of(const kv_plan *p, int bits)
+TreeShape shape_of(const kv_plan *p, int bits, bool paged)
 {
     static int cus = 0;
     if (cus == 0) {
         int dev = 0, n = 0;
         cus = hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0 ? n : 256;
     }
-    return TreeShape{p->D, p->H, p->Hq / p->H, bits, cus};
+    return TreeShape{p->D, p->H, p->Hq / p->H, bits, cus, paged};
 }
 
 }  // namespace
@@ -82,7 +100,7 @@ extern "C" int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t 
 extern "C" size_t kv_tree_attn_workspace(const kv_plan_t *p, int n_tok, int max_len)
 {
     if (!p || n_tok < 0 || max_len < 0) return 0;
-    const TreeShape s = shape_of(p, 16);
+    const TreeShape s = shape_of(p, 16, false);
     const int most = std::min(tree_most_splits(s, n_tok), (int)(((int64_t)max_len + KV_TREE_MAX + 31) / 32));
     return (size_t)std::max<uint64_t>(16, tree_split_bytes(s, n_tok) * most);
 }
@@ -97,13 +115,14 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     if (a->n_splits < 0 || a->n_splits > 128 || !std::isfinite(a->scale)) return KV_EINVAL;
     if (p->B > 65535 || p->Hq > 65535) return KV_EINVAL;
     if (a->tok_first_host[0] != 0) return KV_EINVAL;
-    int max_total = 0;
+    int max_total = 0, most_drafted = 0;
     for (int b = 0; b < p->B; ++b) {
         const int len = view->seq_lens_host[b], n = a->tok_first_host[b + 1] - a->tok_first_host[b];
         if (len < 0 || a->tok_first_host[b + 1] < a->tok_first_host[b]) return KV_EINVAL;
         if (n > KV_TREE_MAX || len > INT_MAX - KV_TREE_MAX) return KV_ERANGE;
         if (a->mask && n > 64ll * a->mask_words) return KV_ERANGE;
         max_total = std::max(max_total, len + n);
+        most_drafted = std::max(most_drafted, n);
     }
     TreeParams t{};
     const int rc = cache_addr(p, view, blocks, layer, view->seq_lens_host, a->tok_first_host, &t.c);
@@ -130,7 +149,7 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.out_mode = a->out_dtype == KV_OUT_F32 ? 0 : bf16 ? 2 : 1;
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;
-    const TreeCut cut = cut_tree(shape_of(p, format_bits(format)), p->B, view->seq_lens_host, a->tok_first_host, a->n_splits, ws_bytes);
+    const TreeCut cut = cut_tree(shape_of(p, format_bits(format), t.c.table != nullptr), p->B, view->seq_lens_host, a->tok_first_host, a->n_splits, ws_bytes);
     t.ns = cut.ns;
     t.split_tokens = cut.split_tokens;
     t.row_blocks = cut.row_blocks;
@@ -146,16 +165,15 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     const bool f32 = t.out_mode == 0;
     // offsets of a step's rows, and of a block, fit 32 bits; blocks hold whole groups of 16
     t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < 1ull << 16 : t.c.ss < 1ull << 26 && t.c.zs < 1ull << 26;
+    t.dense = t.c.ss == (uint64_t)p->D * format_bits(format) / 8;
     TreeKernel k = (format == KV_FORMAT_FP8 ? tree_kernel_fp8 : format == KV_FORMAT_FP4 ? tree_kernel_fp4 : tree_kernel_16)(p->D, bf16, f32, cut.nb);
     hipStream_t st = (hipStream_t)hip_stream;
     (void)launch_kernel(k, dim3((unsigned)groups), dim3(kTreeThreads), st, t);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     if (cut.ns == 1) return KV_OK;
-    const long long rows = (long long)n_tok * p->Hq;
-    const dim3 cgrid((unsigned)((rows + kCombineWaves - 1) / kCombineWaves));
-    (void)launch_kernel(p->D == 64 ? kv_tree_combine_kernel<64> : p->D == 128 ? kv_tree_combine_kernel<128> : kv_tree_combine_kernel<256>, cgrid,
-                        dim3(64 * kCombineWaves), st, t, (int)rows);
+    const dim3 cgrid((unsigned)(((long long)most_drafted * p->Hq + kCombineWaves - 1) / kCombineWaves), (unsigned)p->B);
+    (void)launch_kernel(p->D == 64 ? kv_tree_combine_kernel<64> : p->D == 128 ? kv_tree_combine_kernel<128> : kv_tree_combine_kernel<256>, cgrid, dim3(64 * kCombineWaves), st, t);
     e = hipGetLastError();
     if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     return KV_OK;
