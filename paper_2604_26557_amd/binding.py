@@ -258,6 +258,16 @@ class Plan:
     def __init__(self, handle: int):
         self.handle = C.c_void_p(handle)
         self.info = kv_plan_info(self)
+        self._shape = None
+
+    @property
+    def shape(self):
+        """(KV heads, query heads, head_dim, torch dtype, batch + 1): what the tensors of a layer's calls are compared with."""
+        if self._shape is None:
+            import torch
+            i = self.info
+            self._shape = (i.n_kv_heads, i.n_q_heads, i.head_dim, torch.float16 if i.dtype == KV_F16 else torch.bfloat16, i.batch + 1)
+        return self._shape
 
     def close(self):
         if self.handle:
@@ -527,13 +537,17 @@ def kv_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, scaling: int 
     return t
 
 
+_dtypes = {}   # torch dtype -> KV_F16 | KV_BF16, once torch is imported
+
+
 def _kv_dtype(t) -> int:
-    import torch
-    if t.dtype == torch.float16:
-        return KV_F16
-    if t.dtype == torch.bfloat16:
-        return KV_BF16
-    raise KVError(KV_EINVAL, f"rows of {t.dtype}")
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.float16: KV_F16, torch.bfloat16: KV_BF16})
+    d = _dtypes.get(t.dtype)
+    if d is None:
+        raise KVError(KV_EINVAL, f"rows of {t.dtype}")
+    return d
 
 
 def kv_rope(rope: Rope, positions, x, out, transposed: bool = False, stream=None) -> None:
@@ -549,27 +563,23 @@ def kv_rope(rope: Rope, positions, x, out, transposed: bool = False, stream=None
         raise KVError(rc, "kv_rope")
 
 
-def _row_pair(k, v, tok_seq, tok_slot, where):
-    (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
-    if kd != 1 or vd != 1 or k.shape != v.shape or k.dtype != v.dtype or tok_seq.numel() < k.shape[0] or tok_slot.numel() < k.shape[0]:
+def _row_strides(plan: Plan, k, v, tok_seq, tok_slot, where):
+    """Strides of K's and V's rows [n_tok, H, D], which have to be of the plan's shape and type, and their number."""
+    (n, h, d), (kt, kh, kd), (vt, vh, vd), shape = k.shape, k.stride(), v.stride(), plan.shape
+    if kd != 1 or vd != 1 or h != shape[0] or d != shape[2] or k.dtype != shape[3] or v.dtype != shape[3] or v.shape != k.shape \
+            or tok_seq.numel() < n or tok_slot.numel() < n:
         raise KVError(KV_EINVAL, where)
-    return kt, kh, vt, vh
-
-
-def _check_rows(plan: Plan, k, where):
-    if k.shape[1] != plan.info.n_kv_heads or k.shape[2] != plan.info.head_dim or _kv_dtype(k) != plan.info.dtype:
-        raise KVError(KV_EINVAL, where)
+    return kt, kh, vt, vh, n
 
 
 def kv_cache_write(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, k, v, tok_seq, tok_slot, rope: Optional[Rope] = None,
                    positions=None, stream=None) -> None:
     """k, v: [n_tok, H, D], the plan's dtype, last dim contiguous; tok_seq, tok_slot, positions: device int32 [n_tok]."""
-    strides = _row_pair(k, v, tok_seq, tok_slot, "kv_cache_write")
-    _check_rows(plan, k, "kv_cache_write")
-    if rope is not None and (positions is None or positions.numel() < k.shape[0]):
+    kt, kh, vt, vh, n = _row_strides(plan, k, v, tok_seq, tok_slot, "kv_cache_write")
+    if rope is not None and (positions is None or positions.numel() < n):
         raise KVError(KV_EINVAL, "kv_cache_write")
-    a = kv_write_args_t(k.data_ptr(), v.data_ptr(), *strides, tok_seq.data_ptr(), tok_slot.data_ptr(), rope._ptr if rope is not None else None,
-                        positions.data_ptr() if positions is not None else None, k.shape[0], 0)
+    a = kv_write_args_t(k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, tok_seq.data_ptr(), tok_slot.data_ptr(), rope._ptr if rope is not None else None,
+                        positions.data_ptr() if rope is not None else None, n, 0)
     rc = (_lib or lib()).kv_cache_write(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), _caller_stream(stream))
     if rc:
         raise KVError(rc, "kv_cache_write")
@@ -577,9 +587,8 @@ def kv_cache_write(plan: Plan, view: View, blocks: Optional[Blocks], layer: int,
 
 def kv_cache_read(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tok_seq, tok_slot, k_out, v_out, stream=None) -> None:
     """k_out, v_out: [n_tok, H, D], the plan's dtype, last dim contiguous; tok_seq, tok_slot: device int32 [n_tok]."""
-    strides = _row_pair(k_out, v_out, tok_seq, tok_slot, "kv_cache_read")
-    _check_rows(plan, k_out, "kv_cache_read")
-    a = kv_read_args_t(k_out.data_ptr(), v_out.data_ptr(), *strides, tok_seq.data_ptr(), tok_slot.data_ptr(), k_out.shape[0], 0)
+    kt, kh, vt, vh, n = _row_strides(plan, k_out, v_out, tok_seq, tok_slot, "kv_cache_read")
+    a = kv_read_args_t(k_out.data_ptr(), v_out.data_ptr(), kt, kh, vt, vh, tok_seq.data_ptr(), tok_slot.data_ptr(), n, 0)
     rc = (_lib or lib()).kv_cache_read(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), _caller_stream(stream))
     if rc:
         raise KVError(rc, "kv_cache_read")
@@ -622,10 +631,9 @@ def kv_tree_attn_workspace(plan: Plan, n_tok: int, max_len: int) -> int:
 def kv_tree_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tree: TreeBatch, q, out, out_dtype: int, n_splits: int, workspace,
                  scale: float = 0.0, stream=None) -> None:
     """q, out: [n_tok, H_q, D], last dim contiguous; q of the plan's dtype, out of that or fp32 (out_dtype)."""
-    (qt, qh, qd), (ot, oh, od) = q.stride(), out.stride()
-    info = plan.info
-    if qd != 1 or od != 1 or q.shape != out.shape or q.shape[0] < tree.n_tok or q.shape[1] != info.n_q_heads or q.shape[2] != info.head_dim \
-            or len(tree.first) != info.batch + 1 or _kv_dtype(q) != info.dtype or out.element_size() != (4 if out_dtype == KV_OUT_F32 else 2):
+    (n, hq, d), (qt, qh, qd), (ot, oh, od), shape = q.shape, q.stride(), out.stride(), plan.shape
+    if qd != 1 or od != 1 or n < tree.n_tok or hq != shape[1] or d != shape[2] or q.dtype != shape[3] or out.shape != q.shape \
+            or len(tree.first) != shape[4] or out.element_size() != (4 if out_dtype == KV_OUT_F32 else 2):
         raise KVError(KV_EINVAL, "kv_tree_attn")
     a = kv_tree_args_t(q.data_ptr(), out.data_ptr(), qt, qh, ot, oh, *tree._fixed, out_dtype, n_splits, scale)
     rc = (_lib or lib()).kv_tree_attn(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), workspace.data_ptr(),

@@ -489,24 +489,59 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     const u32x4 ones = BF16 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u} : u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 
     // Scores of 32 tokens: lane (n, group) gets those of tokens group, group + 4, ..., from each half four; rows n of K's operand are tokens n / 4 + 4 * (n % 4) (+ 16).
-    auto scores = [&](const char *stage, f32x4 (&s)[NB][2]) {
-        const char *const k = stage, *const z = stage + 2 * T::kKBytes;
+    struct KRead {
         u32x4 w[T::kKReads][2];
-        float scale[T::kKReads][2];
+        unsigned z[T::kBlocks ? T::kKReads : 1][2];
+    };
+    constexpr int kHalves = T::kVBytes == 32 ? 2 : 1, kPairs = kColumns / 2 / kHalves, kBytes = T::kVBytes / kHalves;
+    struct VRead {
+        unsigned w[kHalves][8][kBytes < 4 ? 1 : kBytes / 4];
+        unsigned z[T::kBlocks ? 8 : 1];
+    };
+    auto read_k = [&](const char *stage, KRead &x) {
+        const char *const k = stage, *const z = stage + 2 * T::kKBytes;
 #pragma unroll
         for (int r = 0; r < T::kKReads; ++r)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int token = (n >> 2) + 4 * (n & 3) + 16 * i;
                 if constexpr (T::kKPiece == 16) {
-                    w[r][i] = *(const u32x4 *)(k + token * T::kRow + 16 * ((4 * r + group) ^ T::k_turn(token)));
+                    x.w[r][i] = *(const u32x4 *)(k + token * T::kRow + 16 * ((4 * r + group) ^ T::k_turn(token)));
                 } else {
                     const u32x2 v = *(const u32x2 *)(k + token * T::kRow + 8 * group);
-                    w[r][i] = u32x4{v[0], v[1], 0, 0};
+                    x.w[r][i] = u32x4{v[0], v[1], 0, 0};
                 }
-                scale[r][i] = 1.f;
-                if constexpr (T::kBlocks) scale[r][i] = scale_operand((unsigned char)z[token * (D == 256 ? 8 : 4) + (4 * r + group) * T::kKElems / kBlockElems]);
+                if constexpr (T::kBlocks) x.z[r][i] = (unsigned char)z[token * (D == 256 ? 8 : 4) + (4 * r + group) * T::kKElems / kBlockElems];
             }
+    };
+    auto read_v = [&](const char *stage, VRead &x) {
+        const char *const v = stage + T::kKBytes, *const z = stage + 2 * T::kKBytes + (D == 256 ? 256 : 128);
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const char *const at = v + (group + 4 * j) * T::kRow + kBytes * n + half * 256;
+                unsigned *const w = x.w[half][j];
+                if constexpr (kBytes == 2) {
+                    w[0] = *(const unsigned short *)at;
+                } else if constexpr (kBytes == 4) {
+                    w[0] = *(const unsigned *)at;
+                } else if constexpr (kBytes == 8) {
+                    const u32x2 y = *(const u32x2 *)at;
+                    w[0] = y[0];
+                    w[1] = y[1];
+                } else {
+                    const u32x4 y = *(const u32x4 *)at;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = y[e];
+                }
+            }
+        if constexpr (T::kBlocks) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x.z[j] = (unsigned char)z[(group + 4 * j) * (D == 256 ? 8 : 4) + kColumns * n / kBlockElems];
+        }
+    };
+    auto scores = [&](const KRead &x, f32x4 (&s)[NB][2]) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
         constexpr int per = T::kKElems / 8;
@@ -523,17 +558,15 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     u32x4 a;
-                    if constexpr (!T::kBlocks) a = w[r][i];
-                    else if constexpr (FORMAT == KV_FORMAT_FP8) a = decode8<BF16, FORMAT>(u32x2{w[r][i][2 * e], w[r][i][2 * e + 1]}, scale[r][i]);
-                    else a = decode8<BF16, FORMAT>(u32x2{w[r][i][e], 0}, scale[r][i]);
+                    if constexpr (!T::kBlocks) a = x.w[r][i];
+                    else if constexpr (FORMAT == KV_FORMAT_FP8) a = decode8<BF16, FORMAT>(u32x2{x.w[r][i][2 * e], x.w[r][i][2 * e + 1]}, scale_operand(x.z[r][i]));
+                    else a = decode8<BF16, FORMAT>(u32x2{x.w[r][i][e], 0}, scale_operand(x.z[r][i]));
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) s[nb][i] = mfma32<BF16>(a, q[nb], s[nb][i]);
                 }
             }
     };
-    auto product = [&](const char *stage, const u32x4 (&pr)[NB][kP]) {
-        const char *const v = stage + T::kKBytes, *const z = stage + 2 * T::kKBytes + (D == 256 ? 256 : 128);
-        constexpr int kHalves = T::kVBytes == 32 ? 2 : 1, kPairs = kColumns / 2 / kHalves, kBytes = T::kVBytes / kHalves;
+    auto product = [&](const VRead &x, const u32x4 (&pr)[NB][kP]) {
 #pragma unroll
         for (int t = 0; t < kP; ++t)
 #pragma unroll
@@ -541,37 +574,20 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         float scale[8];
         if constexpr (T::kBlocks) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) scale[j] = scale_operand((unsigned char)z[(group + 4 * j) * (D == 256 ? 8 : 4) + kColumns * n / kBlockElems]);
+            for (int j = 0; j < 8; ++j) scale[j] = scale_operand(x.z[j]);
         }
 #pragma unroll
-        for (int half = 0; half < kHalves; ++half) {
-            unsigned w[8][kBytes < 4 ? 1 : kBytes / 4];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const char *const at = v + (group + 4 * j) * T::kRow + kBytes * n + half * 256;
-                if constexpr (kBytes == 2) {
-                    w[j][0] = *(const unsigned short *)at;
-                } else if constexpr (kBytes == 4) {
-                    w[j][0] = *(const unsigned *)at;
-                } else if constexpr (kBytes == 8) {
-                    const u32x2 x = *(const u32x2 *)at;
-                    w[j][0] = x[0];
-                    w[j][1] = x[1];
-                } else {
-                    const u32x4 x = *(const u32x4 *)at;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[j][e] = x[e];
-                }
-            }
+        for (int half = 0; half < kHalves; ++half)
 #pragma unroll
             for (int c = 0; c < kPairs; ++c) {
                 unsigned y[8];   // two columns of the eight tokens
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if constexpr (!T::kBlocks) y[j] = w[j][c];
-                    else if constexpr (FORMAT == KV_FORMAT_FP8) y[j] = c % 2 ? decode2<BF16, FORMAT, 1>(w[j][c / 2], scale[j]) : decode2<BF16, FORMAT, 0>(w[j][c / 2], scale[j]);
-                    else y[j] = c % 4 == 0 ? decode2<BF16, FORMAT, 0>(w[j][c / 4], scale[j]) : c % 4 == 1 ? decode2<BF16, FORMAT, 1>(w[j][c / 4], scale[j])
-                              : c % 4 == 2 ? decode2<BF16, FORMAT, 2>(w[j][c / 4], scale[j]) : decode2<BF16, FORMAT, 3>(w[j][c / 4], scale[j]);
+                    const unsigned *const w = x.w[half][j];
+                    if constexpr (!T::kBlocks) y[j] = w[c];
+                    else if constexpr (FORMAT == KV_FORMAT_FP8) y[j] = c % 2 ? decode2<BF16, FORMAT, 1>(w[c / 2], scale[j]) : decode2<BF16, FORMAT, 0>(w[c / 2], scale[j]);
+                    else y[j] = c % 4 == 0 ? decode2<BF16, FORMAT, 0>(w[c / 4], scale[j]) : c % 4 == 1 ? decode2<BF16, FORMAT, 1>(w[c / 4], scale[j])
+                              : c % 4 == 2 ? decode2<BF16, FORMAT, 2>(w[c / 4], scale[j]) : decode2<BF16, FORMAT, 3>(w[c / 4], scale[j]);
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -587,7 +603,6 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
                         }
                 }
             }
-        }
     };
     auto rescale = [&](int nb, float f) {
         sum[nb] *= f;
@@ -632,8 +647,9 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         for (int c = 0; c < kColumns; ++c) acc[nb][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // Steps.  A stage's K is loaded again as soon as its scores are formed, its V after its product.  Loads come back in order: all but those issued later are waited for.
+    // Steps.  Loads come back in order: all but those issued later are waited for.
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
+    constexpr bool kEarly = NB <= 2;
     unsigned there[kStages], stage = 0;
 #pragma unroll
     for (int m = 0; m < kStages; ++m) {
@@ -662,42 +678,55 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     for (int m = 0; m < mine; ++m) {
         const bool more = m + kStages < mine;
         if (more) where(m + kStages);
+        const char *const here_now = ring + stage * T::kStage;
+        const int j0 = s0 + 32 * (wave + m * kWaves);
         f32x4 s[NB][2];
+        VRead v;
+        // The stage is read and loaded again at once where K and V both fit the registers beside the sums; else each as it is needed.
+        if (m + kStages <= mine) wait_loads<kEarly ? (kStages - 1) * (kKIssues + kVIssues) : kVIssues + (kStages - 1) * (kKIssues + kVIssues)>();
+        else wait_loads<0>();
         {
-            const int j0 = s0 + 32 * (wave + m * kWaves);
-            if (m + kStages <= mine) wait_loads<kVIssues + (kStages - 1) * (kKIssues + kVIssues)>();
-            else wait_loads<0>();
-            scores(ring + stage * T::kStage, s);
-            if (j0 + 32 > len || there[0] != ~0u) {
-                // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
-                const int row = (int)rb * kRows + here(n);
+            KRead k;
+            read_k(here_now, k);
+            if constexpr (kEarly) read_v(here_now, v);
+            scores(k, s);
+        }
+        if (j0 + 32 > len || there[0] != ~0u) {
+            // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
+            const int row = (int)rb * kRows + here(n);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const unsigned seen = (there[0] & row_sees32(p, first, row + nb * 16, j0, len, total)) >> group;
+            for (int nb = 0; nb < NB; ++nb) {
+                const unsigned seen = (there[0] & row_sees32(p, first, row + nb * 16, j0, len, total)) >> group;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = seen >> 4 * j & 1 ? s[nb][j / 4][j % 4] : -INFINITY;
-                }
+                for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = seen >> 4 * j & 1 ? s[nb][j / 4][j % 4] : -INFINITY;
             }
         }
         __builtin_amdgcn_sched_barrier(0);   // a phase's registers at a time
         if (more) {
             wait_reads();
             issue_rows(stage, std::false_type{});
+            if constexpr (kEarly) {
+                issue_scales(stage);
+                issue_rows(stage, std::true_type{});
+            }
         }
-        {
-            u32x4 pr[NB][kP];
-            __builtin_amdgcn_sched_barrier(0);
-            softmax(s, pr);
-            __builtin_amdgcn_sched_barrier(0);
+        u32x4 pr[NB][kP];
+        __builtin_amdgcn_sched_barrier(0);
+        softmax(s, pr);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kEarly) {
             if (more) wait_loads<(kStages - 1) * (kKIssues + kVIssues) + T::kLoads>();
             else wait_loads<0>();
-            product(ring + stage * T::kStage, pr);
+            read_v(here_now, v);
         }
+        product(v, pr);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) {
-            wait_reads();
-            issue_scales(stage);
-            issue_rows(stage, std::true_type{});
+        if constexpr (!kEarly) {
+            if (more) {
+                wait_reads();
+                issue_scales(stage);
+                issue_rows(stage, std::true_type{});
+            }
         }
 #pragma unroll
         for (int k = 0; k + 1 < kStages; ++k) there[k] = there[k + 1];

@@ -30,9 +30,9 @@ inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (
 
 // Both choices go by an estimate of the time in us, fitted to what 15 shapes took with 3 row groups times 16 split counts each (head_dim 64 to 256, the three formats, 1 to
 // 64 drafted tokens, contexts of 256 to 32K):
-//   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on a compute unit adds 60 % of that;
+//   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on a compute unit adds 39 % of the one and 56 % of the other;
 //   the whole cache through HBM once;  where there are splits a second launch, and partial results written and read.
-// Its choice was within 5 % of a shape's best on 9 of the 15 and within 12 % on all; 64 rows and 256 workgroups for every shape were up to 40 % off.
+// Its choice was within 5 % of a shape's best on 11 of the 15 and within 20 % on all; 64 rows and 256 workgroups for every shape were up to 40 % off.
 inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *first, int n_splits, uint64_t ws_bytes)
 {
     int rows = 0, longest = 0;
@@ -54,15 +54,14 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
     const long long n_tok = first[B];
     const int fit = (int)std::min<uint64_t>(kMaxTreeSplits, ws_bytes / tree_split_bytes(s, n_tok));
     const int most = std::max(1, std::min(fit, n_splits > 0 ? n_splits : tree_most_splits(s, n_tok)));
-    const double hbm = context * s.H * 2.0 * s.D * s.bits / 8 / 5.5e6, part = 2.0 * n_tok * s.H * s.G * s.D * 4 / 3.5e6;
+    const double hbm = context * s.H * 2.0 * s.D * s.bits / 8 / 7.0e6, part = 2.0 * n_tok * s.H * s.G * s.D * 4 / 2.1e6;
     constexpr int kCounted = 16;   // sequences whose workgroups are counted one by one: for more, and split, half a workgroup each is added
     TreeCut best{};
     double least = 1e30;
     for (int k = 0; k < (s.D == 256 ? 2 : 3); ++k) {
         const int nb = 1 << k;
         if (k > 0 && rows <= 8 * nb) break;   // half of the rows would be none
-        const double per_row = 0.2 * nb * s.D / 128 * (s.D == 256 ? 1.5 : 1);
-        const double step = (s.D == 256 ? 1.2 : 0.85) + per_row + (s.bits < 16 ? 0.05 * nb : 0) + (s.paged ? 0.2 : 0), start = 3.2 + 1.3 * nb;
+        const double step = (s.D == 256 ? 0.75 : 0.9) + 0.19 * nb * s.D / 128 * (s.D == 256 ? 2.6 : 1) + (s.paged ? 0.25 : 0), start = 3.0 + 0.9 * nb;
         for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32) {
             const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
             double items = blocks[k];
@@ -81,7 +80,7 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
             double turns = std::max(1.0, items / s.cus);   // workgroups of the fullest compute unit
             if (uniform) turns = (double)(long long)(turns + 0.9);
             else if (turns > 1) turns += 0.25;
-            const double us = std::max(hbm + start / 2, (start + (st + 127) / 128 * step) * (1 + 0.6 * (turns - 1))) + (ns > 1 ? 3.0 + ns * (part + 0.05) : 0);
+            const double us = std::max(hbm + 0.8 * start, start * (1 + 0.39 * (turns - 1)) + (st + 127) / 128 * step * (1 + 0.56 * (turns - 1))) + (ns > 1 ? 4.4 + ns * (part + 0.01) : 0);
             if (us < least) {
                 least = us;
                 best.nb = nb;

@@ -519,3 +519,18 @@ def test_two_runs_give_the_same_bits():
     first = c.attend(q, parents)
     for _ in range(5):
         assert torch.equal(c.attend(q, parents), first)
+
+
+@pytest.mark.parametrize("fmt,share", [("fp8", 2), ("fp4", 4)])
+def test_example_of_a_serving_loop(fmt, share):
+    """The operators together: drafts verified, accepted rows kept, the cache offloaded and reloaded as codes and scales."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "tree_step.py")
+    spec = importlib.util.spec_from_file_location("tree_step", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    worst, moved, full = mod.main(layers=2, context=333, steps=4, fmt=fmt, say=lambda *a: None)
+    # probabilities and results are rounded to 8 bits, the 32-bit form's operands are the same: two roundings of at most 2^-8 each
+    assert worst <= 2 * 2.0 ** -8
+    assert full / share < moved < full / share * 1.2   # scales are 1/32 of fp8 codes, 1/16 of fp4's; whole sectors
