@@ -520,7 +520,7 @@ int kv_adapt_update(kv_adapt_t *a, const kv_pipe_stats_t *stats);
  * reloads the codes like any other cache).  Strides here are bytes; a row's head_dim/32 bytes lie side by side.
  * In KV_LAYOUT_PAGED stride_b goes from block to block (the view's table applies), stride_h from head to head, stride_s from token to token.
  * The calls below take the plan of the cache's real head_dim and dtype (the 16-bit type of rows written, read and attended with), and NULL in
- * place of a kv_blocks_t for KV_FORMAT_16.
+ * place of a kv_blocks_t for KV_FORMAT_16.  A view with seq_off arrays (rows that start later) is none of theirs: KV_EINVAL.
  */
 typedef struct kv_blocks {
     int32_t format;         /* KV_FORMAT_FP8 | KV_FORMAT_FP4 */
@@ -633,7 +633,10 @@ int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t *masks, int
  * sequence is plain decoding).  A row that sees nothing yields zeros; what a row does not see has no effect on it, infinities and NaNs included.
  * fp32 scores, maxima and sums; probabilities enter the product with V in parts whose sum is the fp32 value (out_dtype KV_OUT_F32), or rounded to the
  * plan's 16-bit type, and in that rounded form also their sum (KV_OUT_SAME: each output is rounded to that type anyway).
- * head_dim 64, 128 or 256.  q: the plan's dtype; q strides: elements, multiples of 8; out strides: elements; q and workspace 16-byte aligned.
+ * A row all of whose scores are -infinity yields zeros too; NaNs that a row sees spread as in the formula.
+ * head_dim 64, 128 or 256; at most 4095 query heads per KV head (KV_EINVAL) and 2^30 tokens of context (KV_ERANGE).  q: the plan's dtype; q strides: elements,
+ * multiples of 8; out strides: elements; q and workspace 16-byte aligned.  A row's scales are aligned to their number (head_dim/32 bytes).
+ * Fastest where a head's rows lie side by side and blocks of a pool hold a multiple of 16 tokens; everything else is looked up row by row.
  * workspace: at least kv_tree_attn_workspace() bytes lets the library split sequences as it likes; with less it splits less.
  */
 #define KV_TREE_MAX 256

@@ -380,9 +380,9 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     unsigned long long at0 = 0, at1 = 0, z0 = 0, z1 = 0;   // starts
     unsigned long long lane_at = 0, lane_z = 0;            // where not all rows exist, or they are looked up: the row of token lane % 32
     unsigned next_there = ~0u;                             // a bit for each token that the cache has
-    unsigned ids = 0;                                      // lane l: block of half l % 2 of the wavefront's step l / 2 (of 32 steps)
+    unsigned long long ids_at = 0, ids_z = 0, ids_there = 0;   // block pool, lane l: start of half l % 2 of the wavefront's step l / 2 (of 32 steps); whether it has one, by lanes
     bool groups = false;
-    auto where = [&](int m) {   // this wavefront's m-th step
+    auto where = [&](int m) {   // this wavefront's m-th step; called for each in turn
         const int j0 = s0 + 32 * (wave + m * kWaves), left = total - 1 - j0;
         groups = p.grouped && left >= 31;
         next_there = ~0u;
@@ -394,24 +394,36 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             return;
         }
         if (!p.c.table) {
-            at0 = base + (unsigned)j0 * p.c.ss;
+            // from one step to the next a sum, not a product
+            at0 = m == 0 ? base + (unsigned)j0 * p.c.ss : at0 + 32 * kWaves * (unsigned)p.c.ss;
             at1 = at0 + 16 * (unsigned)p.c.ss;
             if (T::kBlocks) {
-                z0 = zbase + (unsigned)j0 * p.c.zs;
+                z0 = m == 0 ? zbase + (unsigned)j0 * p.c.zs : z0 + 32 * kWaves * (unsigned)p.c.zs;
                 z1 = z0 + 16 * (unsigned)p.c.zs;
             }
         } else {
-            if (m % 32 == 0) ids = (unsigned)table[block_of(min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1))];
-            unsigned id0 = (unsigned)__builtin_amdgcn_readlane((int)ids, 2 * (m % 32)), id1 = (unsigned)__builtin_amdgcn_readlane((int)ids, 2 * (m % 32) + 1);
-            const unsigned in0 = j0 - block_of(j0) * p.c.bt, in1 = j0 + 16 - block_of(j0 + 16) * p.c.bt;
-            if (id0 >= (unsigned)p.c.n_pool) id0 = 0, next_there &= 0xffff0000u;
-            if (id1 >= (unsigned)p.c.n_pool) id1 = 0, next_there &= 0xffffu;
-            at0 = base + (unsigned long long)id0 * (unsigned)p.c.sb + in0 * (unsigned)p.c.ss;
-            at1 = base + (unsigned long long)id1 * (unsigned)p.c.sb + in1 * (unsigned)p.c.ss;
-            if (T::kBlocks) {
-                z0 = zbase + (unsigned long long)id0 * (unsigned)p.c.zb + in0 * (unsigned)p.c.zs;
-                z1 = zbase + (unsigned long long)id1 * (unsigned)p.c.zb + in1 * (unsigned)p.c.zs;
+            if (m % 32 == 0) {   // the starts of 32 steps at a time, a lane each
+                const int j = min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1) & ~15, at = block_of(j);
+                unsigned id = (unsigned)table[at];
+                const unsigned in = j - at * p.c.bt;
+                ids_there = __ballot(id < (unsigned)p.c.n_pool);
+                id = id < (unsigned)p.c.n_pool ? id : 0;
+                ids_at = base + (unsigned long long)id * (unsigned)p.c.sb + in * (unsigned)p.c.ss;
+                if (T::kBlocks) ids_z = zbase + (unsigned long long)id * (unsigned)p.c.zb + in * (unsigned)p.c.zs;
             }
+            const int l = 2 * (m % 32);
+            auto of_lane = [](unsigned long long x, int k) {
+                return (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, k) |
+                       (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(x >> 32), k) << 32;
+            };
+            at0 = of_lane(ids_at, l);
+            at1 = of_lane(ids_at, l + 1);
+            if (T::kBlocks) {
+                z0 = of_lane(ids_z, l);
+                z1 = of_lane(ids_z, l + 1);
+            }
+            const unsigned both = (unsigned)(ids_there >> l) & 3;
+            next_there = both == 3 ? ~0u : both == 2 ? 0xffff0000u : both == 1 ? 0xffffu : 0;
         }
         if (!groups) {
             const int t = min(lane & 31, left);

@@ -1,4 +1,5 @@
-// How a kv_tree_attn launch shares its work out: query rows per workgroup and token splits.  Host arithmetic only.
+// How a kv_tree_attn launch shares its work out: query rows per workgroup and token splits.  Host arithmetic only, for groups of at most 4095 heads and contexts of at
+// most 2^30 tokens.
 #pragma once
 
 #include <algorithm>
@@ -33,6 +34,7 @@ inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (
 //   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on a compute unit adds 39 % of the one and 56 % of the other;
 //   the whole cache through HBM once;  where there are splits a second launch, and partial results written and read.
 // Its choice was within 5 % of a shape's best on 11 of the 15 and within 20 % on all; 64 rows and 256 workgroups for every shape were up to 40 % off.
+// At least one token is drafted.
 inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *first, int n_splits, uint64_t ws_bytes)
 {
     int rows = 0, longest = 0;
@@ -66,12 +68,12 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
             const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
             double items = blocks[k];
             if (ns > 1 && uniform) {
-                items *= (longest + st - 1) / st;
+                items *= (longest - 1) / st + 1;
             } else if (ns > 1 && B <= kCounted) {
                 items = 0;
                 for (int b = 0; b < B; ++b) {
                     const int t = first[b + 1] - first[b];
-                    items += (t * s.G + 16 * nb - 1) / (16 * nb) * ((lens[b] + t + st - 1) / st);
+                    items += (double)((t * s.G + 16 * nb - 1) / (16 * nb)) * ((lens[b] + t - 1) / st + 1);
                 }
             } else if (ns > 1) {
                 items = tokens[k] / st + 0.5 * blocks[k];
@@ -89,7 +91,7 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
         }
     }
     best.row_blocks = (rows + 16 * best.nb - 1) / (16 * best.nb);
-    best.ns = std::max(1, (longest + best.split_tokens - 1) / std::max(1, best.split_tokens));
+    best.ns = (longest - 1) / best.split_tokens + 1;
     return best;
 }
 

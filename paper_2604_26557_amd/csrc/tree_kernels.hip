@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(Tre
     const int total = max(0, min(load_uniform(p.seq_lens + b), p.max_total - drafted)) + drafted;
     if (r >= drafted * Hq) return;
     const int t = first + r / Hq, hq = r % Hq;
-    const int ns = min(p.ns, (total + p.split_tokens - 1) / p.split_tokens);
+    const int ns = min(p.ns, (total - 1) / p.split_tokens + 1);
     const long long row = (long long)t * Hq + hq;
     const f32x2 *const ml = (const f32x2 *)p.part_ml + row * p.ns;
     const int sub = lane / kLanes, d = lane % kLanes * 4;
@@ -113,13 +113,13 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     if (!view->seq_lens_host || !view->seq_lens_dev || !a->tok_first_host || !a->tok_first_dev) return KV_EINVAL;
     if (a->out_dtype != KV_OUT_F32 && a->out_dtype != KV_OUT_SAME) return KV_EINVAL;
     if (a->n_splits < 0 || a->n_splits > 128 || !std::isfinite(a->scale)) return KV_EINVAL;
-    if (p->B > 65535 || p->Hq > 65535) return KV_EINVAL;
+    if (p->B > 65535 || p->Hq > 65535 || p->Hq / p->H > 4095) return KV_EINVAL;   // a row's number times the group is divided in 32 bits
     if (a->tok_first_host[0] != 0) return KV_EINVAL;
     int max_total = 0, most_drafted = 0;
     for (int b = 0; b < p->B; ++b) {
         const int len = view->seq_lens_host[b], n = a->tok_first_host[b + 1] - a->tok_first_host[b];
         if (len < 0 || a->tok_first_host[b + 1] < a->tok_first_host[b]) return KV_EINVAL;
-        if (n > KV_TREE_MAX || len > INT_MAX - KV_TREE_MAX) return KV_ERANGE;
+        if (n > KV_TREE_MAX || len > 1 << 30) return KV_ERANGE;   // the kernels look some thousand tokens past a sequence's end in 32 bits
         if (a->mask && n > 64ll * a->mask_words) return KV_ERANGE;
         max_total = std::max(max_total, len + n);
         most_drafted = std::max(most_drafted, n);
@@ -163,8 +163,9 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     auto over = [](int d) { return (unsigned)(((1ull << 32) + d - 1) / d); };
     t.by_g = over(t.G); t.by_ns = over(cut.ns); t.by_h = over(p->H); t.by_row_blocks = over(cut.row_blocks);
     const bool f32 = t.out_mode == 0;
-    // offsets of a step's rows, and of a block, fit 32 bits; blocks hold whole groups of 16
-    t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < 1ull << 16 : t.c.ss < 1ull << 26 && t.c.zs < 1ull << 26;
+    // offsets within a block, or from one of a wavefront's steps to the next (128 tokens), fit 32 bits; blocks hold whole groups of 16
+    t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < (1ull << 32) / (uint64_t)t.c.bt
+                          : t.c.ss < 1ull << 25 && t.c.zs < 1ull << 25;
     t.dense = t.c.ss == (uint64_t)p->D * format_bits(format) / 8;
     TreeKernel k = (format == KV_FORMAT_FP8 ? tree_kernel_fp8 : format == KV_FORMAT_FP4 ? tree_kernel_fp4 : tree_kernel_16)(p->D, bf16, f32, cut.nb);
     hipStream_t st = (hipStream_t)hip_stream;

@@ -534,3 +534,52 @@ def test_example_of_a_serving_loop(fmt, share):
     # probabilities and results are rounded to 8 bits, the 32-bit form's operands are the same: two roundings of at most 2^-8 each
     assert worst <= 2 * 2.0 ** -8
     assert full / share < moved < full / share * 1.2   # scales are 1/32 of fp8 codes, 1/16 of fp4's; whole sectors
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+@pytest.mark.parametrize("D,H,G,layout,bt,lens,trees", [
+    (128, 1, 40, "paged", 8, [90, 17], [7, 3]),           # blocks of half a group of 16 tokens, more heads than a row group
+    (64, 2, 3, "paged", 48, [333, 1500], [5, 33]),        # blocks that are no power of two
+    (256, 1, 8, "paged", 32, [4300], [30]),               # several rounds of a wavefront's look-ups: 32 steps of 128 tokens each
+    (64, 1, 4, "paged", 16, [9000, 4095, 4097], [1, 2, 3]),
+    (64, 3, 2, "bhsd", 0, [40 * i for i in range(20)], [1 + i % 5 for i in range(20)]),   # more sequences than the cut counts one by one
+    (128, 2, 16, "bhsd", 0, [64] * 18, [9] * 18)])
+def test_attention_blocks_groups_and_batches(fmt, D, H, G, layout, bt, lens, trees):
+    rng = np.random.default_rng(len(lens))
+    parents = [random_parents(rng, n) for n in trees]
+    c = Cache(lens, H, D, torch.float16, fmt, layout, bt=bt or 16, seed=len(lens), extra=max(trees), n_q_heads=H * G)
+    q = rows((sum(trees), H * G, D), torch.float16, 33).cuda()
+    for n_splits in (0, 1):
+        check(c, q, parents, c.attend(q, parents, kv.KV_OUT_F32, n_splits), True)
+
+
+@pytest.mark.parametrize("stride", [(1 << 25) - 64, 1 << 25])
+def test_tokens_as_far_apart_as_a_step_can_count(stride):
+    """Either side of the token stride from which rows are looked up one by one: several steps of each wavefront."""
+    D, n = 64, 300
+    buf = torch.empty(stride * n + 2 * D, dtype=torch.uint8, device="cuda")
+    c = Cache([n - 2], 1, D, torch.bfloat16, "fp8", seed=22, extra=2, n_q_heads=4)
+    q = rows((2, 4, D), torch.bfloat16, 34).cuda()
+    want = c.attend(q, [[-1, 0]], n_splits=1)
+    for kind, at in (("k", 0), ("v", D)):
+        far = buf[at:].as_strided((1, 1, n, D), (0, 0, stride, 1))
+        far[0] = c.dev[kind][0]
+        c.dev[kind] = far
+    c.remake()
+    assert torch.equal(c.attend(q, [[-1, 0]], n_splits=1), want)
+
+
+@pytest.mark.parametrize("stride", [(1 << 28) - 4, 1 << 28])
+def test_scales_of_a_block_as_far_apart_as_32_bits_count(stride):
+    """Scales by tokens over all blocks: either side of what a block's offset holds."""
+    D = 64
+    c = Cache([100], 1, D, torch.bfloat16, "fp8", "paged", seed=23, extra=2, n_q_heads=4)
+    q = rows((2, 4, D), torch.bfloat16, 35).cuda()
+    want = c.attend(q, [[-1, 0]], n_splits=1)
+    m, buf = c.dev["k_scale"].shape[0], torch.empty(stride * 16 + 4096, dtype=torch.uint8, device="cuda")
+    for kind, at in (("k_scale", 0), ("v_scale", 2048)):
+        far = buf[at:].as_strided((m, 1, 16, D // 32), (2, 2, stride, 1))
+        far[:] = c.dev[kind]
+        c.dev[kind] = far
+    c.remake()
+    assert torch.equal(c.attend(q, [[-1, 0]], n_splits=1), want)

@@ -247,3 +247,14 @@ def test_importing_the_binding_needs_no_torch():
     """What the binding did before: torch is imported when the library is loaded, not with the module."""
     code = "import sys; sys.path.insert(0, %r); from paper_2604_26557_amd import binding; print('torch' in sys.modules)" % ROOT
     assert subprocess.check_output([sys.executable, "-c", code], text=True).strip() == "False"
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_attention_refuses_groups_and_contexts_past_its_arithmetic(fmt):
+    """4095 query heads per KV head and 2^30 tokens are the most."""
+    def fake(Hq, n):
+        f = Fake(H=1, Hq=Hq, paged=True, fmt=fmt, max_blocks_per_seq=1 << 27)
+        f.lens[0] = n
+        return f.attn()
+    assert fake(4095, 50) == kv.KV_OK and fake(4096, 50) == kv.KV_EINVAL
+    assert fake(4, 1 << 30) == kv.KV_OK and fake(4, (1 << 30) + 1) == kv.KV_ERANGE
