@@ -24,7 +24,8 @@ struct TreeParams {
     int words, max_total, H, G, B, out_mode;  // out_mode: 0 fp32, 1 fp16, 2 bf16
     int ns, split_tokens, row_blocks;
     int bt_shift;                      // log2 of a block's tokens, or -1
-    unsigned by_g, by_ns, by_h, by_row_blocks;  // 2^32 over G, ..., rounded up: x / G = x * by_g >> 32 as long as x * G < 2^32
+    unsigned by_g, by_ns, by_h, by_row_blocks, by_split;  // 2^32 over G, ns, ..., rounded up (quotient)
+    int ragged;                        // at most 64 sequences, of which some have fewer splits or row blocks than others
     int dense;                         // rows of a head lie side by side
     int grouped;                       // rows of context are looked up by groups of 16
 };
@@ -233,7 +234,15 @@ __device__ __forceinline__ RowAt row_at(const CacheAddr &c, const int *table, un
     return RowAt{base + at * c.sb + r * c.ss, zbase + at * c.zb + r * c.zs, there};
 }
 
-// The drafted token of row r of a KV head's query rows.
+// x / d by 2^32 / d, rounded up: the product may be one too large.
+__device__ __forceinline__ unsigned quotient(unsigned x, unsigned d, unsigned by_d)
+{
+    if (d == 1) return x;
+    const unsigned q = __umulhi(x, by_d);
+    return q * d > x ? q - 1 : q;
+}
+
+// The drafted token of row r of a KV head's query rows: at most 256 G, so the product is never too large.
 __device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.by_g); }
 
 // A value that all lanes load, through the scalar cache: nothing writes it while the kernel runs.
@@ -342,24 +351,71 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = kParts<BF16, F32>, kWaves = T::kWaves, kStages = T::kStages;
     constexpr bool kNT = NB <= 2;   // with more rows other workgroups may read the same K and V out of L2
 
-    // Workgroups go round the eight XCDs: the row blocks of a split are eight apart, run at the same time on one XCD and share its L2.
-    unsigned unit = blockIdx.x, rb = 0;
-    if (p.row_blocks > 1) {
-        const unsigned turn = blockIdx.x / 8, eights = __umulhi(turn, p.by_row_blocks);
-        rb = turn - eights * (unsigned)p.row_blocks;
-        unit = eights * 8 + blockIdx.x % 8;
+    // The arguments' cache lines at once, not each where the first of its values is needed.
+    asm volatile("" ::"s"(p.c.k), "s"(p.c.kz), "s"(p.q), "s"(p.part_acc), "s"(p.scale_log2e), "s"(p.by_split));
+
+    // Which sequence, KV head, split and row block.  Workgroups go round the eight XCDs; the row blocks of a split are a multiple of eight apart: they run at about the same
+    // time on one XCD and share its L2.
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    unsigned b, h, split, rb = 0;
+    int first, drafted, len;
+    if (p.ragged) {
+        // Only what there is, sequence after sequence (a lane each): workgroups that have nothing to do would take places from others, which then share a compute unit
+        // while the next one is idle.
+        int f = 0, n = 0, l = 0;
+        unsigned units = 0;   // splits of heads, in eights where there may be row blocks
+        if (lane < p.B) {
+            f = p.tok_first[lane];
+            n = min(p.tok_first[lane + 1] - f, KV_TREE_MAX);
+            l = max(0, min(p.seq_lens[lane], p.max_total - n));
+            units = n <= 0 ? 0 : (quotient((unsigned)(l + n - 1), (unsigned)p.split_tokens, p.by_split) + 1) * (unsigned)p.H;
+            if (p.row_blocks > 1) units = (units + 7) & ~7u;
+        }
+        const unsigned all = units * ((unsigned)(n * p.G + kRows - 1) / kRows);
+        unsigned end = all;   // of the sequence's workgroups
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);   // sums over the lanes below: 1, 2, 4, 8 of a row of 16, then over rows
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
+        b = (unsigned)__popcll(__ballot(end <= blockIdx.x));
+        if (b >= (unsigned)p.B) return;
+        first = __builtin_amdgcn_readlane(f, (int)b);
+        drafted = __builtin_amdgcn_readlane(n, (int)b);
+        len = __builtin_amdgcn_readlane(l, (int)b);
+        units = (unsigned)__builtin_amdgcn_readlane((int)units, (int)b);
+        unsigned unit = blockIdx.x - (unsigned)__builtin_amdgcn_readlane((int)(end - all), (int)b);
+        if (unit >= units) {
+            rb = unit / units;
+            unit -= rb * units;
+        }
+        split = quotient(unit, (unsigned)p.H, p.by_h);
+        h = unit - split * (unsigned)p.H;
+    } else {
+        unsigned unit = blockIdx.x;
+        if (p.row_blocks > 1) {
+            const unsigned turn = blockIdx.x / 8, eights = quotient(turn, (unsigned)p.row_blocks, p.by_row_blocks);
+            rb = turn - eights * (unsigned)p.row_blocks;
+            unit = eights * 8 + blockIdx.x % 8;
+        }
+        const unsigned bh = quotient(unit, (unsigned)p.ns, p.by_ns);
+        split = unit - bh * (unsigned)p.ns;
+        b = quotient(bh, (unsigned)p.H, p.by_h);
+        h = bh - b * (unsigned)p.H;
+        if (b >= (unsigned)p.B) return;
+        const int next = load_uniform(p.tok_first + b + 1), l = load_uniform(p.seq_lens + b);
+        first = load_uniform(p.tok_first + b);
+        __builtin_amdgcn_sched_barrier(0);   // one wait for all three
+        drafted = min(next - first, KV_TREE_MAX);
+        len = max(0, min(l, p.max_total - drafted));
     }
-    const unsigned bh = p.ns == 1 ? unit : __umulhi(unit, p.by_ns), split = unit - bh * (unsigned)p.ns;
-    const unsigned b = p.H == 1 ? bh : __umulhi(bh, p.by_h), h = bh - b * (unsigned)p.H;
-    if (b >= (unsigned)p.B) return;
-    const int first = load_uniform(p.tok_first + b), drafted = min(load_uniform(p.tok_first + b + 1) - first, KV_TREE_MAX);
     const int n_rows = drafted * p.G - (int)rb * kRows;   // of this block: the first kRows of them
     if (n_rows <= 0) return;
-    const int len = max(0, min(load_uniform(p.seq_lens + b), p.max_total - drafted)), total = len + drafted;
+    const int total = len + drafted;
     const int s0 = (int)split * p.split_tokens, s1 = min(s0 + p.split_tokens, total);
     if (s0 >= total) return;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, group = lane >> 4;
     const unsigned long long base = p.c.table ? h * p.c.sh : b * p.c.sb + h * p.c.sh;
     const unsigned long long zbase = p.c.table ? h * p.c.zh : b * p.c.zb + h * p.c.zh;

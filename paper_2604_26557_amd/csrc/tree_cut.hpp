@@ -3,6 +3,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 namespace kvb {
@@ -29,21 +30,26 @@ inline int tree_most_splits(const TreeShape &s, long long n_tok)
 
 inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (uint64_t)n_tok * s.H * s.G * (s.D + 2) * sizeof(float); }
 
-// Both choices go by an estimate of the time in us, fitted to what 15 shapes took with 3 row groups times 16 split counts each (head_dim 64 to 256, the three formats, 1 to
-// 64 drafted tokens, contexts of 256 to 32K):
-//   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on a compute unit adds 39 % of the one and 56 % of the other;
-//   the whole cache through HBM once;  where there are splits a second launch, and partial results written and read.
-// Its choice was within 5 % of a shape's best on 11 of the 15 and within 20 % on all; 64 rows and 256 workgroups for every shape were up to 40 % off.
+// Sequences up to which a ragged batch's launch leaves out the workgroups that have nothing to do, and up to which they are counted one by one here: a lane of a wavefront each.
+constexpr int kCounted = 64;
+
+// Both choices go by an estimate of the time in us, fitted to what 36 shapes took with 3 row groups times 20 split counts each (head_dim 64 to 256, the three formats, 1 to
+// 48 sequences of equal or ragged lengths, 1 to 64 drafted tokens, contexts of 48 to 32K):
+//   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on the fullest compute unit adds 40 % of the one and 41 to 50 % of the other;
+//   the whole cache through HBM once, and again through L2 for further row blocks;
+//   where there are splits a second launch, and partial results written and read.
+// Its choice was 4 % from a shape's best on average, within 5 % on 28 of the 36, within 10 % on 31 and 63 % off on the worst (many short sequences of unequal length, whose
+// workgroups it takes for equals); the times themselves it gives to 13 % on average.
 // At least one token is drafted.
 inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *first, int n_splits, uint64_t ws_bytes)
 {
     int rows = 0, longest = 0;
-    bool uniform = true;
     double blocks[3] = {0, 0, 0}, tokens[3] = {0, 0, 0}, context = 0;  // by row groups: workgroups without splits, and the tokens they go over
+    float totals[kCounted], drafts[kCounted], groups[kCounted][3];     // of sequences that are counted
+    int counted = 0;
     for (int b = 0; b < B; ++b) {
         const int t = first[b + 1] - first[b], total = lens[b] + t;
         if (t == 0) continue;
-        uniform = uniform && (longest == 0 || longest == total);
         rows = std::max(rows, t * s.G);
         longest = std::max(longest, total);
         context += total;
@@ -51,38 +57,41 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
             const int n = (t * s.G + (16 << k) - 1) / (16 << k);
             blocks[k] += n;
             tokens[k] += (double)n * total;
+            if (counted < kCounted) groups[counted][k] = (float)n;
         }
+        if (counted < kCounted) {
+            totals[counted] = (float)(total - 1);
+            drafts[counted] = (float)t;
+        }
+        ++counted;
     }
     const long long n_tok = first[B];
     const int fit = (int)std::min<uint64_t>(kMaxTreeSplits, ws_bytes / tree_split_bytes(s, n_tok));
     const int most = std::max(1, std::min(fit, n_splits > 0 ? n_splits : tree_most_splits(s, n_tok)));
-    const double hbm = context * s.H * 2.0 * s.D * s.bits / 8 / 7.0e6, part = 2.0 * n_tok * s.H * s.G * s.D * 4 / 2.1e6;
-    constexpr int kCounted = 16;   // sequences whose workgroups are counted one by one: for more, and split, half a workgroup each is added
+    const double row = s.H * 2.0 * s.D * s.bits / 8, hbm = context * row / 7.4e6, part = 2.0 * s.H * s.G * s.D * 4 / 2.0e6;
     TreeCut best{};
     double least = 1e30;
-    for (int k = 0; k < (s.D == 256 ? 2 : 3); ++k) {
-        const int nb = 1 << k;
-        if (k > 0 && rows <= 8 * nb) break;   // half of the rows would be none
-        const double step = (s.D == 256 ? 0.75 : 0.9) + 0.19 * nb * s.D / 128 * (s.D == 256 ? 2.6 : 1) + (s.paged ? 0.25 : 0), start = 3.0 + 0.9 * nb;
-        for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32) {
-            const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
-            double items = blocks[k];
-            if (ns > 1 && uniform) {
-                items *= (longest - 1) / st + 1;
-            } else if (ns > 1 && B <= kCounted) {
-                items = 0;
-                for (int b = 0; b < B; ++b) {
-                    const int t = first[b + 1] - first[b];
-                    items += (double)((t * s.G + 16 * nb - 1) / (16 * nb)) * ((lens[b] + t - 1) / st + 1);
-                }
-            } else if (ns > 1) {
-                items = tokens[k] / st + 0.5 * blocks[k];
+    for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32) {
+        const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
+        float splits[3] = {0, 0, 0}, parts = 0;   // workgroups of a KV head, and partial results of a query head
+        if (counted <= kCounted) {
+            const float per = 1.f / (float)st;
+            for (int b = 0; b < counted; ++b) {
+                const float n = (float)((int)(totals[b] * per) + 1);
+                for (int k = 0; k < 3; ++k) splits[k] += groups[b][k] * n;
+                parts += drafts[b] * n;
             }
-            items *= s.H;
-            double turns = std::max(1.0, items / s.cus);   // workgroups of the fullest compute unit
-            if (uniform) turns = (double)(long long)(turns + 0.9);
-            else if (turns > 1) turns += 0.25;
-            const double us = std::max(hbm + 0.8 * start, start * (1 + 0.39 * (turns - 1)) + (st + 127) / 128 * step * (1 + 0.56 * (turns - 1))) + (ns > 1 ? 4.4 + ns * (part + 0.01) : 0);
+        } else {   // half a workgroup more each than their tokens fill
+            for (int k = 0; k < 3; ++k) splits[k] = (float)(ns > 1 ? tokens[k] / st + 0.5 * blocks[k] : blocks[k]);
+            parts = (float)n_tok * (float)ns;
+        }
+        for (int k = 0; k < (s.D == 256 ? 2 : 3); ++k) {
+            const int nb = 1 << k;
+            if (k > 0 && rows <= 8 * nb) break;   // half of the rows would be none
+            const double step = 0.95 + 0.18 * nb * s.D / 128 * (s.D == 256 ? 1.4 : 1) + (s.paged ? 0.05 : 0), start = 2.6 + 0.6 * nb;
+            const double further = std::max(0.0, std::ceil((double)splits[k] * s.H / s.cus) - 1);   // workgroups beside the first on the fullest compute unit
+            const double us = std::max(hbm + (tokens[k] - context) * row / 25e6 + 1.06 * start, start * (1 + 0.4 * further) + (st + 127) / 128 * step * (1 + (0.53 - 0.03 * nb) * further)) +
+                              (ns > 1 ? 3.9 + parts * part + 0.03 * ns : 0);
             if (us < least) {
                 least = us;
                 best.nb = nb;

@@ -158,10 +158,21 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.bt_shift = -1;
     if (t.c.table && (t.c.bt & (t.c.bt - 1)) == 0) t.bt_shift = __builtin_ctz((unsigned)t.c.bt);
     // units (a split of a KV head) go in eights where they have several row blocks (the kernel's note on XCDs)
-    const uint64_t units = (uint64_t)p->B * p->H * cut.ns, groups = cut.row_blocks > 1 ? (units + 7) / 8 * 8 * cut.row_blocks : units;
-    if ((groups + 8) * std::max(std::max(cut.ns, cut.row_blocks), p->H) >= 1ull << 32) return KV_ERANGE;   // what the divisions below allow
+    auto in_eights = [&](uint64_t units) { return cut.row_blocks > 1 ? (units + 7) / 8 * 8 : units; };
+    uint64_t groups = in_eights((uint64_t)p->B * p->H * cut.ns) * cut.row_blocks;
+    if (p->B > 1 && p->B <= kCounted) {   // without those that have nothing to do, if there are any
+        uint64_t some = 0;
+        for (int b = 0; b < p->B; ++b) {
+            const int n = a->tok_first_host[b + 1] - a->tok_first_host[b];
+            if (n > 0) some += in_eights((uint64_t)((view->seq_lens_host[b] + n - 1) / cut.split_tokens + 1) * p->H) * ((n * t.G + 16 * cut.nb - 1) / (16 * cut.nb));
+        }
+        t.ragged = some < groups;
+        if (t.ragged) groups = some;
+    }
+    if (groups * kTreeThreads >= 1ull << 32) return KV_ERANGE;   // threads of a launch
     auto over = [](int d) { return (unsigned)(((1ull << 32) + d - 1) / d); };
     t.by_g = over(t.G); t.by_ns = over(cut.ns); t.by_h = over(p->H); t.by_row_blocks = over(cut.row_blocks);
+    t.by_split = over(cut.split_tokens);
     const bool f32 = t.out_mode == 0;
     // offsets within a block, or from one of a wavefront's steps to the next (128 tokens), fit 32 bits; blocks hold whole groups of 16
     t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < (1ull << 32) / (uint64_t)t.c.bt

@@ -583,3 +583,17 @@ def test_scales_of_a_block_as_far_apart_as_32_bits_count(stride):
         c.dev[kind] = far
     c.remake()
     assert torch.equal(c.attend(q, [[-1, 0]], n_splits=1), want)
+
+
+@pytest.mark.parametrize("B", [63, 64, 65])
+def test_ragged_batches_as_wide_as_a_wavefront(B):
+    """Workgroups without work are left out of up to 64 sequences' launches, by sums over a wavefront's lanes."""
+    rng = np.random.default_rng(B)
+    lens, trees = rng.integers(0, 700, B).tolist(), rng.integers(0, 12, B).tolist()
+    trees[0] = trees[-1] = 11
+    trees[1] = trees[B // 2] = 0
+    parents = [random_parents(rng, n) for n in trees]
+    c = Cache(lens, 3, 64, torch.bfloat16, "fp8", "paged", seed=B, extra=12, n_q_heads=9)
+    q = rows((sum(trees), 9, 64), torch.bfloat16, 36).cuda()
+    for n_splits in (0, 1, 5):   # up to 33 rows: several row blocks
+        check(c, q, parents, c.attend(q, parents, kv.KV_OUT_F32, n_splits), True)
