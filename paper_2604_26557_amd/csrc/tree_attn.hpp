@@ -1,4 +1,27 @@
 // Kernels of kv_tree_attn, a translation unit for each cache format (tree_attn_16.hip, tree_attn_fp8.hip, tree_attn_fp4.hip).
+//
+// Mathematics.  A query row is one query head of one drafted token; the G query heads of a KV head share its K and V, so the rows of a sequence and KV head are
+// T * G.  Each row has out = sum_j p_j V_j / sum_j p_j with p_j = exp2((q . K_j) scale log2(e) - ref), in one pass over the tokens: ref is any number near the running
+// maximum, the same for all tokens that are added up, and sums are multiplied by exp2(old - new) when it moves.  Parts of the tokens with references of their own
+// (wavefronts, then workgroups) are joined by the same factors.
+//
+// Work.  A workgroup has a split of a KV head's tokens and 16, 32 or 64 of its rows (NB row groups); its four wavefronts take every fourth step of 32 tokens, each for
+// all the rows, so K and V are decoded once per workgroup, and join their sums at the end.  Both products are on the matrix cores (16 x 16 x 32): S^T = K q^T has K's
+// rows as its first operand and query rows as columns, so that a lane ends up with eight scores of one row, which as they lie are the second operand of V^T P^T: no score
+// changes lanes.  Sums of probabilities are one more product, with ones.
+//
+// What bounds it, and what was measured (MI355X, us per call, the second launch that joins splits included):
+//   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 51.8 = 5.4 TB/s;
+//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 27 %): 32K tokens x
+//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 62 = 555 TFLOP/s;
+//   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 15.4.
+// Why so:
+//   K and V go through LDS, loaded there without passing registers: 16 KiB of a wavefront are on their way while it computes, without spilling what holds the sums.  With loads into
+//   registers, when this was changed: 307 at the 32K case (88 through LDS), 91 at the 256-wide heads (73).
+//   64 rows per workgroup where there are as many: 32 rows take 72.7 and 16 rows 98.0 at the 32K case (64: 63.6); where there are but 16 (32K tokens, 16 bits, 4 drafted),
+//   16 take 29.6, 32 30.4 and 64 33.8.  Which, and how many splits: cut_tree.
+//   Four wavefronts, merged by halves: what one gives another goes through LDS twice (half, then a quarter of the sums), and two workgroups share a compute unit: one
+//   merges while the other reads.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -147,7 +170,8 @@ struct TreeTile {
     static constexpr int kStage = 2 * kKBytes + kZBytes;
     static constexpr int kQBytes = kQInLds ? NB * kSteps * 1024 : 0;
     static constexpr int kHalfLds = 80 * 1024;
-    // Steps on their way while one is worked on: up to 16 KiB of a wavefront, as long as two workgroups fit
+    // Steps on their way while one is worked on: up to 16 KiB of a wavefront, as long as two workgroups fit a compute unit's LDS.  A wavefront's reads have some 2 us of
+    // latency to cover.
     static constexpr int kStages = kWaves * 4 * kStage + kQBytes <= kHalfLds && kStage <= 4096 ? 4 : kWaves * 2 * kStage + kQBytes <= kHalfLds ? 2 : 1;
     static constexpr int kRing = kWaves * kStages * kStage;
     static constexpr int kMerge = kWaves * NB * kColumns / 2 * 1024, kStates = (2 * kWaves * kRows + kWaves) * 4;   // bytes
@@ -677,8 +701,11 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) acc[nb][c] *= f;
     };
-    // Probabilities against a reference that follows the running maximum lazily: only where a probability came out above 2^4 are maxima formed, sums
-    // rescaled and the probabilities formed again.
+    // Probabilities against a reference that follows the running maximum lazily: only where a probability came out above 2^4 are maxima formed over the lanes, sums
+    // rescaled and the probabilities formed again: most steps have no exchange between lanes and leave the sums alone.  What is added up stays below 2^4 times the number of
+    // tokens, far from where 32 bits end.
+    // Each probability is rounded to 16 bits where the result is; its sum is that of the rounded ones, so the weights add up to one.  A 32-bit result gets it in parts that
+    // add up to its 32 bits (bf16), or to all but 2^-22 of it (fp16).
     auto softmax = [&](f32x4 (&s)[NB][2], u32x4 (&pr)[NB][kP]) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -716,8 +743,12 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     }
 
     // Steps.  Loads come back in order: all but those issued later are waited for.
+    // Early: K and V of a step are read from LDS at once and its place loaded again before anything is computed; else V is read after the softmax.  Codes are few registers:
+    // 32K tokens x 8 heads x 128, 8 bits, 32 rows 27.0 us early, 27.8 late; 4 x 8K x 16 x 256, 8 bits, 16 rows 51.4-54.0, 54.7-55.7; 32 x 500-2000 x 8 x 128, paged, 25.1, 26.5.
+    // 16-bit rows, and more rows at 256 columns, leave too few for the sums: 32K tokens, 16 bits, 16 rows 31.2 early, 30.5 late; 16 x 4K, 32 rows 60.0, 57.8; 4 x 8K x 16 x 256,
+    // 8 bits, 32 rows 61.2, 59.8.
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
-    constexpr bool kEarly = NB <= 2;
+    constexpr bool kEarly = T::kBlocks && NB * D <= 256;
     unsigned there[kStages], stage = 0;
 #pragma unroll
     for (int m = 0; m < kStages; ++m) {
