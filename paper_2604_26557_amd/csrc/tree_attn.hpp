@@ -153,7 +153,7 @@ struct TreeTile {
     static constexpr int kColumns = D / 16;           // columns of V that a lane works on
     static constexpr int kSteps = D / 32;             // products of 16 tokens' q K^T
     static constexpr int kRows = 16 * NB;             // query rows of a workgroup
-    static constexpr bool kQInLds = NB * D > 256;     // more rows than their registers are worth
+    static constexpr bool kQStays = NB * D > 256;     // q is read from LDS at each step: more rows than their registers are worth
     static constexpr int kRow = D * kBits / 8;        // bytes of a token's row
     static constexpr int kPieces = kRow / 16;         // a row's pieces of 16 bytes: a lane's share of a load
     static constexpr int kTokens = 64 / kPieces;      // rows of a load (1 KiB)
@@ -168,7 +168,7 @@ struct TreeTile {
     static constexpr int kZLoads = !kBlocks ? 0 : D == 256 ? 2 : 1;
     static constexpr int kWaves = 4;                  // two workgroups and more on a compute unit: one merges while another reads
     static constexpr int kStage = 2 * kKBytes + kZBytes;
-    static constexpr int kQBytes = kQInLds ? NB * kSteps * 1024 : 0;
+    static constexpr int kQBytes = NB * kSteps * 1024;
     static constexpr int kHalfLds = 80 * 1024;
     // Steps on their way while one is worked on: up to 16 KiB of a wavefront, as long as two workgroups fit a compute unit's LDS.  A wavefront's reads have some 2 us of
     // latency to cover.
@@ -177,6 +177,7 @@ struct TreeTile {
     static constexpr int kMerge = kWaves * NB * kColumns / 2 * 1024, kStates = (2 * kWaves * kRows + kWaves) * 4;   // bytes
     static constexpr int kLds = kRing + kQBytes > kMerge + kStates ? kRing + kQBytes : kMerge + kStates;
     static_assert(kLds <= (D == 256 ? 2 : 1) * kHalfLds, "LDS of a compute unit");
+    static constexpr int kQIssues = (NB * kSteps + kWaves - 1) / kWaves;
     static constexpr int kPerCu = kLds <= 40 * 1024 ? 4 : kLds <= kHalfLds / 3 * 2 ? 3 : kLds <= kHalfLds ? 2 : 1;
 
     // The first of the eight elements of d that a lane contributes to product s: any order will do that q follows as well.
@@ -566,16 +567,19 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         }
     };
 
-    // Query rows: token-major, the G heads of a token side by side.  Rows past the last one are zeros.
+    // Query rows: token-major, the G heads of a token side by side.  Those past the last one are copies of it, whose results go nowhere.
     auto row_token = [&](int r) { return token_of(p, (int)rb * kRows + r); };
-    u32x4 *const q_lds = (u32x4 *)(lds + T::kRing);
-    u32x4 q_reg[T::kQInLds ? 1 : NB][kSteps];
-    auto load_q = [&](int nb, int s) {
-        const int r = nb * 16 + n;
-        if (r >= n_rows) return u32x4{0, 0, 0, 0};
-        const int t = row_token(r), g = (int)rb * kRows + r - t * p.G;
-        return *(const u32x4 *)(p.q + 2 * ((first + t) * p.q_st + ((int)h * p.G + g) * p.q_sh + T::q_at(s, group)));
+    const u32x4 *const q_lds = (const u32x4 *)(lds + T::kRing);
+    auto issue_q = [&] {   // a wavefront's share of them to LDS
+        const unsigned to = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char *)lds + T::kRing;
+#pragma unroll
+        for (int k = 0; k < T::kQIssues; ++k) {
+            const int i = wave + k * kWaves, nb = i / kSteps, s = i % kSteps;
+            const int r = min(nb * 16 + n, n_rows - 1), t = row_token(r), g = (int)rb * kRows + r - t * p.G;
+            if (i < NB * kSteps) load_to_lds<16, false>(p.q + 2 * ((first + t) * p.q_st + ((int)h * p.G + g) * p.q_sh + T::q_at(s, group)), to + i * 1024);
+        }
     };
+    u32x4 q_reg[T::kQStays ? 1 : NB][kSteps];
     f32x4 acc[NB][kColumns], sum[NB];
     float ref[NB];
     const u32x4 ones = BF16 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u} : u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
@@ -644,7 +648,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
                 u32x4 q[NB];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    if constexpr (T::kQInLds) q[nb] = q_lds[(nb * kSteps + r * per + e) * 64 + lane];
+                    if constexpr (T::kQStays) q[nb] = q_lds[(nb * kSteps + r * per + e) * 64 + lane];
                     else q[nb] = q_reg[nb][r * per + e];
                 }
 #pragma unroll
@@ -750,6 +754,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
     constexpr bool kEarly = T::kBlocks && NB * D <= 256;
     unsigned there[kStages], stage = 0;
+    issue_q();
 #pragma unroll
     for (int m = 0; m < kStages; ++m) {
         there[m] = ~0u;
@@ -760,17 +765,16 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         issue_rows(m, std::true_type{});
         there[m] = next_there;
     }
-    if constexpr (T::kQInLds) {
-        for (int i = wave; i < NB * kSteps; i += kWaves) q_lds[i * 64 + lane] = load_q(i / kSteps, i % kSteps);
-        __syncthreads();
-    } else {
+    // q is there once everybody's share is; the steps' loads go on
+    if (mine >= kStages) wait_loads<kStages * (kKIssues + kVIssues)>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if constexpr (!T::kQStays) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                q_reg[nb][s] = load_q(nb, s);
-                asm volatile("" : "+v"(q_reg[nb][s]));   // arrived: a wait for them within the loop would be one for every load
-            }
+            for (int s = 0; s < kSteps; ++s) q_reg[nb][s] = q_lds[(nb * kSteps + s) * 64 + lane];
     }
 
 #pragma unroll 1
