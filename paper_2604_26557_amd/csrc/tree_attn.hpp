@@ -270,6 +270,20 @@ __device__ __forceinline__ unsigned quotient(unsigned x, unsigned d, unsigned by
 // The drafted token of row r of a KV head's query rows: at most 256 G, so the product is never too large.
 __device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.by_g); }
 
+// The kernel's arguments, loaded where they are needed: what is only used now and then, or after the loop, takes no scalar registers in it (there are too few: the
+// others would be kept in lanes of a vector register and fetched from there at each step).
+__device__ __forceinline__ TreeParams arguments()
+{
+#if __HIP_DEVICE_COMPILE__
+    typedef const __attribute__((address_space(4))) TreeParams *Args;
+    unsigned long long at = (unsigned long long)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(Args)at;
+#else
+    return TreeParams{};   // the host's pass over this file knows no such address
+#endif
+}
+
 // A value that all lanes load, through the scalar cache: nothing writes it while the kernel runs.
 __device__ __forceinline__ int load_uniform(const int *at) { return *(const __attribute__((address_space(4))) int *)(unsigned long long)at; }
 
@@ -454,7 +468,6 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 
     const int n_steps = (s1 - s0 + 31) / 32;
     const int mine = (n_steps - wave + kWaves - 1) / kWaves;   // steps of this wavefront: wave, wave + kWaves, ...
-    auto block_of = [&](int j) { return p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt; };
 
     // Where a step's rows are.  16 rows lie stride by stride from a start that all lanes share, in a block pool from an id that some lane holds; blocks of other
     // sizes and rows far apart are looked up one by one.  A row past the end is the last one; what has no place in the cache is block 0 of the pool; neither is seen.
@@ -468,7 +481,8 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         groups = p.grouped && left >= 31;
         next_there = ~0u;
         if (!p.grouped) {
-            const RowAt r = row_at(p.c, table, base, zbase, j0 + min(lane & 31, left));
+            const CacheAddr c = arguments().c;
+            const RowAt r = row_at(c, table, base, zbase, j0 + min(lane & 31, left));
             lane_at = r.at;
             lane_z = r.z;
             next_there = (unsigned)__ballot(r.there);
@@ -484,7 +498,8 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             }
         } else {
             if (m % 32 == 0) {   // the starts of 32 steps at a time, a lane each
-                const int j = min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1) & ~15, at = block_of(j);
+                const TreeParams p = arguments();
+                const int j = min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1) & ~15, at = p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt;
                 unsigned id = (unsigned)table[at];
                 const unsigned in = j - at * p.c.bt;
                 ids_there = __ballot(id < (unsigned)p.c.n_pool);
@@ -796,6 +811,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         }
         if (j0 + 32 > len || there[0] != ~0u) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
+            const TreeParams p = arguments();
             const int row = (int)rb * kRows + here(n);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -854,6 +870,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 
     // Merge: the wavefronts' references and sums become factors of their accumulators; these are added by halves: a wavefront gives the one that is not in its keeping to
     // another and gets that one's half of what is, twice.  In the end each has a quarter of the sums of all four.
+    const TreeParams a = arguments();
     static_assert(kWaves == 4 && NB * kColumns % 4 == 0, "halves of halves");
     constexpr int kTiles = NB * kColumns;
     f32x4 *const give = (f32x4 *)lds;                                                                // [kWaves][kTiles / 2][64]
@@ -872,7 +889,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     __syncthreads();
     if ((bad_lds[0] + bad_lds[1]) + (bad_lds[2] + bad_lds[3]) != 0.f) {
         for (int r = wave; r < min(n_rows, kRows); r += kWaves)
-            plain_row<D, BF16, FORMAT>(p, table, base, zbase, h, first, (int)rb * kRows + r, len, total, s0, s1, split, lane);
+            plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, (int)rb * kRows + r, len, total, s0, s1, split, lane);
         return;
     }
     float to[NB], total_sum[NB];
@@ -890,7 +907,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) total_sum[nb] += l[w] == 0.f ? 0.f : l[w] * __builtin_amdgcn_exp2f(r[w] - to[nb]);
         float f = sum[nb][0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref[nb] - to[nb]);
-        if (p.ns == 1) f = total_sum[nb] == 0.f ? 0.f : f / total_sum[nb];
+        if (a.ns == 1) f = total_sum[nb] == 0.f ? 0.f : f / total_sum[nb];
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) tiles[nb * kColumns + c] = acc[nb][c] * f;
     }
@@ -919,16 +936,16 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     static_assert(kColumns % kShare == 0, "of one row group");
     const int nb = kShare * wave / kColumns, c0 = kShare * wave % kColumns, r = nb * 16 + n;
     if (r >= n_rows) return;
-    const int t = row_token(r), hq = (int)h * p.G + (int)rb * kRows + r - t * p.G;
-    const long long part = ((long long)(first + t) * (p.H * p.G) + hq) * p.ns + split, at = p.ns == 1 ? (first + t) * p.o_st + hq * p.o_sh : part * D;
-    if (p.ns > 1 && group == 0 && c0 == 0) {
+    const int t = token_of(a, (int)rb * kRows + r), hq = (int)h * a.G + (int)rb * kRows + r - t * a.G;
+    const long long part = ((long long)(first + t) * (a.H * a.G) + hq) * a.ns + split, at = a.ns == 1 ? (first + t) * a.o_st + hq * a.o_sh : part * D;
+    if (a.ns > 1 && group == 0 && c0 == 0) {
         float ml[2] = {to[0], total_sum[0]};
 #pragma unroll
         for (int k = 1; k < NB; ++k) {
             ml[0] = k == nb ? to[k] : ml[0];
             ml[1] = k == nb ? total_sum[k] : ml[1];
         }
-        *(f32x2 *)&p.part_ml[part * 2] = f32x2{ml[0] - kLiftLog2<BF16>, ml[1]};
+        *(f32x2 *)&a.part_ml[part * 2] = f32x2{ml[0] - kLiftLog2<BF16>, ml[1]};
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -936,8 +953,8 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         float x[kShare];
 #pragma unroll
         for (int c = 0; c < kShare; ++c) x[c] = mine_now[c][i];
-        if (p.ns > 1) store_columns<kShare>(p.part_acc, o, 0, x);
-        else store_columns<kShare>(p.out, o, p.out_mode, x);
+        if (a.ns > 1) store_columns<kShare>(a.part_acc, o, 0, x);
+        else store_columns<kShare>(a.out, o, a.out_mode, x);
     }
 }
 
