@@ -11,10 +11,10 @@
 // changes lanes.  Sums of probabilities are one more product, with ones.
 //
 // What bounds it, and what was measured (MI355X, us per call, the second launch that joins splits included):
-//   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 51.8 = 5.4 TB/s;
-//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 27 %): 32K tokens x
-//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 62 = 555 TFLOP/s;
-//   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 15.4.
+//   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 49.4 = 5.6 TB/s;
+//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 29 %): 32K tokens x
+//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 60 = 573 TFLOP/s;
+//   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 14.1.
 // Why so:
 //   K and V go through LDS, loaded there without passing registers: 16 KiB of a wavefront are on their way while it computes, without spilling what holds the sums.  With loads into
 //   registers, when this was changed: 307 at the 32K case (88 through LDS), 91 at the 256-wide heads (73).
@@ -271,7 +271,7 @@ __device__ __forceinline__ unsigned quotient(unsigned x, unsigned d, unsigned by
 __device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.by_g); }
 
 // The kernel's arguments, loaded where they are needed: what is only used now and then, or after the loop, takes no scalar registers in it (there are too few: the
-// others would be kept in lanes of a vector register and fetched from there at each step).
+// others would be kept in lanes of a vector register and fetched from there at each step: 4 sequences of 8K x 16 heads x 256, 8 bits, 51.8 us, now 49.0).
 __device__ __forceinline__ TreeParams arguments()
 {
 #if __HIP_DEVICE_COMPILE__
@@ -582,7 +582,8 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         }
     };
 
-    // Query rows: token-major, the G heads of a token side by side.  Those past the last one are copies of it, whose results go nowhere.
+    // Query rows: token-major, the G heads of a token side by side.  Those past the last one are copies of it, whose results go nowhere.  They go to LDS ahead of the steps'
+    // K and V: loaded into registers behind these, they were there only when all of these were (4K tokens, 16 drafted: 15.0 us, now 14.3; 48 single tokens 22.7, 21.6).
     auto row_token = [&](int r) { return token_of(p, (int)rb * kRows + r); };
     const u32x4 *const q_lds = (const u32x4 *)(lds + T::kRing);
     auto issue_q = [&] {   // a wavefront's share of them to LDS
