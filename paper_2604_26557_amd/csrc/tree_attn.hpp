@@ -12,8 +12,8 @@
 //
 // What bounds it, and what was measured (MI355X, us per call, the second launch that joins splits included):
 //   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 49.4 = 5.6 TB/s;
-//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 29 %): 32K tokens x
-//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 60 = 573 TFLOP/s;
+//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 32 %): 32K tokens x
+//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 56.3 = 611 TFLOP/s;
 //   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 14.1.
 // Why so:
 //   K and V go through LDS, loaded there without passing registers: 16 KiB of a wavefront are on their way while it computes, without spilling what holds the sums.  With loads into
@@ -769,6 +769,9 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     // 8 bits, 32 rows 61.2, 59.8.
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
     constexpr bool kEarly = T::kBlocks && NB * D <= 256;
+    // With 64 rows a wavefront goes ahead of the other one of its SIMD in its products, whose operands wait for conversions and permutes between them: 32K tokens x 8 heads x 128,
+    // 64 drafted, in 8 bits 66.9 -> 63.4 us (64.4 with the second product alone), in 16 bits, where K needs no conversion, 63.0 -> 60.3 with the second alone (62.2 with both).
+    constexpr bool kFirst = NB == 4, kFirstK = kFirst && T::kBlocks;
     unsigned there[kStages], stage = 0;
     issue_q();
 #pragma unroll
@@ -808,7 +811,9 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             KRead k;
             read_k(here_now, k);
             if constexpr (kEarly) read_v(here_now, v);
+            if constexpr (kFirstK) __builtin_amdgcn_s_setprio(1);
             scores(k, s);
+            if constexpr (kFirstK) __builtin_amdgcn_s_setprio(0);
         }
         if (j0 + 32 > len || there[0] != ~0u) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
@@ -839,7 +844,9 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             else wait_loads<0>();
             read_v(here_now, v);
         }
+        if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
         product(v, pr);
+        if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (!kEarly) {
             if (more) {
