@@ -769,9 +769,10 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     // 8 bits, 32 rows 61.2, 59.8.
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
     constexpr bool kEarly = T::kBlocks && NB * D <= 256;
-    // With 64 rows a wavefront goes ahead of the other one of its SIMD in its products, whose operands wait for conversions and permutes between them: 32K tokens x 8 heads x 128,
-    // 64 drafted, in 8 bits 66.9 -> 63.4 us (64.4 with the second product alone), in 16 bits, where K needs no conversion, 63.0 -> 60.3 with the second alone (62.2 with both).
-    constexpr bool kFirst = NB == 4, kFirstK = kFirst && T::kBlocks;
+    // From 32 rows on a wavefront goes ahead of the other one of its SIMD in its products, whose operands wait for conversions and permutes between them: 32K tokens x 8 heads x 128,
+    // 64 drafted, in 8 bits 66.9 -> 63.4 us (64.4 with the second product alone), in 16 bits, where K needs no conversion, 63.0 -> 60.3 with the second alone (62.2 with both);
+    // 32 rows of a ragged 8-bit batch 37.8 -> 36.0.  With 16 rows it is as often slower (32 x 500-2000 tokens 23.2 -> 23.7) as faster (48 single tokens 21.5 -> 21.0).
+    constexpr bool kFirst = NB >= 2, kFirstK = kFirst && T::kBlocks;
     unsigned there[kStages], stage = 0;
     issue_q();
 #pragma unroll
