@@ -631,8 +631,8 @@ int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t *masks, int
  *   out[t,hq,:] = softmax_j(q[t,hq,:] . K[b,h,j,:] * scale) V[b,h,j,:],  h = hq / (H_q/H),
  * over the context j < len_b and those j = len_b + m whose bit m is set in mask[t] (without a mask: m <= i, a causal chain; a single token per
  * sequence is plain decoding).  A row that sees nothing yields zeros; what a row does not see has no effect on it, infinities and NaNs included.
- * fp32 scores, maxima and sums; probabilities enter the product with V in parts whose sum is the fp32 value (out_dtype KV_OUT_F32), or rounded to the
- * plan's 16-bit type, and in that rounded form also their sum (KV_OUT_SAME: each output is rounded to that type anyway).
+ * fp32 scores, maxima and sums; probabilities enter the product with V, and their sum, in parts that add up to the fp32 value: exactly (bf16, KV_OUT_F32), to
+ * within 2^-22 of it (fp16) or 2^-16 (bf16, KV_OUT_SAME: results that are rounded to 2^-8).
  * A row all of whose scores are -infinity yields zeros too; NaNs that a row sees spread as in the formula.
  * head_dim 64, 128 or 256; at most 4095 query heads per KV head (KV_EINVAL) and 2^30 tokens of context (KV_ERANGE).  q: the plan's dtype; q strides: elements,
  * multiples of 8; out strides: elements; q and workspace 16-byte aligned.  A row's scales are aligned to their number (head_dim/32 bytes).

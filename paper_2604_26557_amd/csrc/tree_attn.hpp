@@ -116,20 +116,23 @@ constexpr float kLargeRef = 1048576.f;  // beyond it the rounding of a reference
 // fp16 probabilities are taken of 2^11 times themselves (at most 2^15): what is lost lies below 2^-36 of the largest
 template <bool BF16> constexpr float kLiftLog2 = BF16 ? 0.f : 11.f;
 template <bool BF16> constexpr float kMostProbability = BF16 ? 16.f : 32768.f;   // 2^(4 + kLiftLog2)
-template <bool BF16, bool F32> constexpr int kParts = F32 ? (BF16 ? 3 : 2) : 1;
+// Probabilities as 16-bit operands: parts whose sum is the 32-bit value up to 2^-22 (fp16, two parts) or 2^-16 (bf16, two), or that value (bf16, three).  Two in bf16 go with
+// bf16 results, whose own rounding, to 2^-8, is 256 times as coarse.  One part, rounded, would make the error of a 16-bit result 1.4 times that of its own rounding, for 56.2 instead of 67.3 us
+// with 64 drafted tokens over 32K x 8 heads x 128 in 8 bits, 48.2 instead of 49.9 in a ragged batch of 8, 49.5 either way where HBM is the limit.
+template <bool BF16, bool F32> constexpr int kParts = BF16 && F32 ? 3 : 2;
 
-// Probabilities as 16-bit operands: rounded once, or as parts whose sum is the 32-bit value (bf16) or that value up to 2^-22 (fp16).
 template <bool BF16, int N>
 __device__ __forceinline__ void split_pair(float x, float y, unsigned (&out)[N])
 {
-    if constexpr (BF16 && N == 3) {
+    if constexpr (BF16) {
 #pragma unroll
-        for (int t = 0; t < 3; ++t) {
+        for (int t = 0; t + 1 < N; ++t) {   // cut off, which takes one instruction for two
             const unsigned a = __float_as_uint(x), b = __float_as_uint(y);
             out[t] = __builtin_amdgcn_perm(b, a, 0x07060302u);
             x -= __uint_as_float(a & 0xffff0000u);
             y -= __uint_as_float(b & 0xffff0000u);
         }
+        out[N - 1] = pack2<BF16>(x, y);
     } else {
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -724,8 +727,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     // Probabilities against a reference that follows the running maximum lazily: only where a probability came out above 2^4 are maxima formed over the lanes, sums
     // rescaled and the probabilities formed again: most steps have no exchange between lanes and leave the sums alone.  What is added up stays below 2^4 times the number of
     // tokens, far from where 32 bits end.
-    // Each probability is rounded to 16 bits where the result is; its sum is that of the rounded ones, so the weights add up to one.  A 32-bit result gets it in parts that
-    // add up to its 32 bits (bf16), or to all but 2^-22 of it (fp16).
+    // Their sum is that of their parts, so the weights add up to one.
     auto softmax = [&](f32x4 (&s)[NB][2], u32x4 (&pr)[NB][kP]) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -971,8 +973,7 @@ typedef void (*TreeKernel)(TreeParams);
 template <int FORMAT, int D, int NB>
 TreeKernel tree_kernel_of(bool bf16, bool f32)
 {
-    return bf16 ? (f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true> : kv_tree_partial_kernel<D, true, FORMAT, NB, false>)
-                : (f32 ? kv_tree_partial_kernel<D, false, FORMAT, NB, true> : kv_tree_partial_kernel<D, false, FORMAT, NB, false>);
+    return !bf16 ? kv_tree_partial_kernel<D, false, FORMAT, NB, false> : f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true> : kv_tree_partial_kernel<D, true, FORMAT, NB, false>;
 }
 template <int FORMAT>
 TreeKernel tree_kernel_for(int D, bool bf16, bool f32, int nb)
