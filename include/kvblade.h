@@ -551,7 +551,8 @@ typedef struct kv_rope {
 #define KV_ROPE_BASE 2       /* the base grows so that the longest wave is factor times as long: base * factor^(rot_dim/(rot_dim-2)) */
 #define KV_ROPE_WAVELENGTH 3 /* by the number of turns t = trained_pos * frequency_d / 2 pi within the trained context: frequencies with t <= low are
                                 divided by factor, with t >= high kept, in between a mixture that is linear in t */
-#define KV_ROPE_INDEX 4      /* the same, the mixture linear in d: it ends at the (rounded) d at which t = high and t = low */
+#define KV_ROPE_INDEX 4      /* the same, the mixture linear in d: it ends at the d at which t = high (rounded down) and t = low (rounded up), each moved into
+                                0 .. rot_dim - 1: past rot_dim/2 - 1 no pair is stretched in full */
 typedef struct kv_rope_desc {
     int32_t n_pos;
     int32_t rot_dim;

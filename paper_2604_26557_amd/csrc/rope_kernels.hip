@@ -98,10 +98,10 @@ extern "C" int kv_rope_table(const kv_rope_desc_t *d, float *table, size_t bytes
     if (bytes / sizeof(float) / d->rot_dim < (size_t)d->n_pos) return KV_ENOSPC;
     const double two_pi = 6.283185307179586476925, magnitude = d->magnitude == 0 ? 1 : d->magnitude;
     const double base = d->scaling == KV_ROPE_BASE ? d->base * std::pow(d->factor, d->rot_dim / (d->rot_dim - 2.0)) : d->base;
-    // INDEX: the pair at which a frequency makes t turns within the trained context
+    // INDEX: the pair at which a frequency makes t turns within the trained context; there need be none of that number
     auto pair_of = [&](double t) { return half * std::log(d->trained_pos / (t * two_pi)) / std::log(base); };
-    const double first = mixed ? std::min<double>(std::max(std::floor(pair_of(d->high)), 0.0), half - 1) : 0;
-    const double last = mixed ? std::min<double>(std::max(std::ceil(pair_of(d->low)), 0.0), half - 1) : 0;
+    auto end_of = [&](double i) { return std::min(std::max(i, 0.0), d->rot_dim - 1.0); };
+    const double first = mixed ? end_of(std::floor(pair_of(d->high))) : 0, last = mixed ? end_of(std::ceil(pair_of(d->low))) : 0;
     for (int i = 0; i < half; ++i) {
         double f = std::pow(base, -(double)i / half);
         if (d->scaling == KV_ROPE_LINEAR) f /= d->factor;
