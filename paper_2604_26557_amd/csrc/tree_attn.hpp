@@ -455,8 +455,8 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     const int n_rows = drafted * p.G - (int)rb * kRows;   // of this block: the first kRows of them
     if (n_rows <= 0) return;
     const int total = len + drafted;
+    if (!split_has_tokens(split, p.split_tokens, total)) return;
     const int s0 = (int)split * p.split_tokens, s1 = min(s0 + p.split_tokens, total);
-    if (s0 >= total) return;
 
     const int n = lane & 15, group = lane >> 4;
     const unsigned long long base = p.c.table ? h * p.c.sh : b * p.c.sb + h * p.c.sh;

@@ -33,6 +33,10 @@ inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (
 // Sequences up to which a ragged batch's launch leaves out the workgroups that have nothing to do, and up to which they are counted one by one here: a lane of a wavefront each.
 constexpr int kCounted = 64;
 
+// Whether a split has any of a sequence's tokens.  Where units go in eights a workgroup's split may be up to 7 past the last one: with tokens of a split as many as a context's, that
+// passes 32 bits.
+constexpr bool split_has_tokens(unsigned split, int split_tokens, int total) { return (uint64_t)split * (unsigned)split_tokens < (uint64_t)total; }
+
 // Both choices go by an estimate of the time in us, fitted to what 36 shapes took with 3 row groups times 20 split counts each (head_dim 64 to 256, the three formats, 1 to
 // 48 sequences of equal or ragged lengths, 1 to 64 drafted tokens, contexts of 48 to 32K):
 //   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on the fullest compute unit adds 40 % of the one and 41 to 50 % of the other;

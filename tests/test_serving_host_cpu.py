@@ -1,9 +1,13 @@
 """The serving step's host side where it is easily got wrong: ends of schedules, sizes, kinds of tensors."""
 import math
+import os
+import random
+import subprocess
 
 import numpy as np
 import pytest
 
+from conftest import ROOT
 from paper_2604_26557_amd import binding as kv
 
 
@@ -26,3 +30,36 @@ def test_rope_table_by_index_past_the_last_pair(base, trained, ends):
     assert np.abs(got - np.stack([np.cos(a), np.sin(a)], -1)).max() <= 2.0 ** -24 + 1e-13
     # and the last pair's angle by itself: sines of small angles, relative to a rounding
     assert np.abs(np.arcsin(got[1, 63, 1]) / f[63] - 1) <= 2.0 ** -22
+
+
+@pytest.fixture(scope="module")
+def units(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("units") / "tree_units_harness")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I",
+                           os.path.join(ROOT, "paper_2604_26557_amd", "csrc"), os.path.join(ROOT, "tests", "tree_units_harness.cpp"), "-o", exe])
+
+    def run(cases):
+        """cases: (D, H, G, n_splits, ws_splits, lens, drafted)"""
+        text = "".join(f"{D} {H} {G} {n} {ws} {len(lens)} {' '.join(map(str, lens))} {' '.join(map(str, drafted))}\n" for D, H, G, n, ws, lens, drafted in cases)
+        out = subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.splitlines()
+        assert len(out) == len(cases)
+        return [tuple(map(int, line.split())) for line in out]
+    return run
+
+
+def test_workgroups_past_the_last_split_have_no_tokens(units):
+    """Every token of a sequence is gone over once per head and row block, also where the numbers of splits that do not exist times their tokens pass 32 bits."""
+    rnd = random.Random(3)
+    cases = [(128, 1, 40, 1, 1, [n, 5], [4, 3]) for n in (1, 1000, 1 << 28, 306783379, 306783380, 1 << 29, (1 << 30) - 1, 1 << 30)]
+    cases += [(128, 1, 40, 0, 0, [1 << 30] * 3, [2, 1, 200])]
+    for _ in range(300):
+        B = rnd.randint(2, 64)
+        cases.append((rnd.choice([64, 128, 256]), rnd.choice([1, 2, 3, 5, 8]), rnd.choice([1, 4, 20, 40]), rnd.choice([0, 0, 1, 3]), rnd.choice([0, 1, 4, 128]),
+                      [rnd.choice([0, 40, 5000, rnd.randrange(1 << 30), 1 << 30]) for _ in range(B)], [rnd.choice([1, 2, 9, 256]) for _ in range(B)]))
+    past = 0
+    for (D, H, G, n, ws, lens, drafted), (groups, idle, tokens, nb, split_tokens) in zip(cases, units(cases)):
+        blocks = [-(-t * G // (16 * nb)) for t in drafted]
+        assert tokens == H * sum((a + t) * k for a, t, k in zip(lens, drafted, blocks))
+        assert groups - idle == H * sum(-(-(a + t) // split_tokens) * k for a, t, k in zip(lens, drafted, blocks))
+        past += idle > 0 and 7 * split_tokens >= 1 << 31
+    assert past > 50   # such launches are among them
