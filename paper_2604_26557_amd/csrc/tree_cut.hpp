@@ -30,6 +30,24 @@ inline int tree_most_splits(const TreeShape &s, long long n_tok)
 
 inline uint64_t tree_split_bytes(const TreeShape &s, long long n_tok) { return (uint64_t)n_tok * s.H * s.G * (s.D + 2) * sizeof(float); }
 
+// The numbers of splits that are considered.
+constexpr int next_splits(int ns) { return ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32; }
+
+// Room for whatever is chosen for up to n_tok drafted tokens over up to `tokens` of a sequence, drafted ones included.  Fewer tokens may be split more often: the most is wanted by n_tok or by
+// as many as just fill some number of 64-row blocks.
+inline uint64_t tree_workspace_bytes(const TreeShape &s, long long n_tok, long long tokens)
+{
+    int cap = 1;
+    while (cap < (tokens + 31) / 32 && cap < kMaxTreeSplits) cap = next_splits(cap);
+    auto room = [&](long long n) { return tree_split_bytes(s, n) * (uint64_t)std::min(tree_most_splits(s, n), cap); };
+    uint64_t most = room(n_tok);
+    for (long long blocks = 1, n = 0; (n = 64 * blocks / s.G) < n_tok; ++blocks) {
+        if (n > 0) most = std::max(most, room(n));
+        if (n > 0 && tree_most_splits(s, n) == 1) break;   // from there on more tokens take more room
+    }
+    return most;
+}
+
 // Sequences up to which a ragged batch's launch leaves out the workgroups that have nothing to do, and up to which they are counted one by one here: a lane of a wavefront each.
 constexpr int kCounted = 64;
 
@@ -75,7 +93,7 @@ inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *f
     const double row = s.H * 2.0 * s.D * s.bits / 8, hbm = context * row / 7.4e6, part = 2.0 * s.H * s.G * s.D * 4 / 2.0e6;
     TreeCut best{};
     double least = 1e30;
-    for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = ns < 8 ? ns + 1 : ns < 16 ? ns + 2 : ns < 32 ? ns + 4 : ns < 64 ? ns + 8 : ns + 32) {
+    for (int ns = n_splits > 0 ? most : 1; ns <= most; ns = next_splits(ns)) {
         const int st = ((longest + ns - 1) / ns + 31) / 32 * 32;
         float splits[3] = {0, 0, 0}, parts = 0;   // workgroups of a KV head, and partial results of a query head
         if (counted <= kCounted) {

@@ -102,9 +102,7 @@ extern "C" int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t 
 extern "C" size_t kv_tree_attn_workspace(const kv_plan_t *p, int n_tok, int max_len)
 {
     if (!p || n_tok < 0 || max_len < 0) return 0;
-    const TreeShape s = shape_of(p, 16, false);
-    const int most = std::min(tree_most_splits(s, n_tok), (int)(((int64_t)max_len + KV_TREE_MAX + 31) / 32));
-    return (size_t)std::max<uint64_t>(16, tree_split_bytes(s, n_tok) * most);
+    return (size_t)std::max<uint64_t>(16, tree_workspace_bytes(shape_of(p, 16, false), n_tok, (long long)max_len + KV_TREE_MAX));
 }
 
 extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *a, void *workspace,

@@ -9,6 +9,7 @@ import pytest
 
 from conftest import ROOT
 from paper_2604_26557_amd import binding as kv
+from test_tree_cut_cpu import cut  # noqa: F401
 
 
 @pytest.mark.parametrize("base,trained,ends", [(10000.0, 65536, (40, 65)), (10000.0, 131072, (45, 70)), (10000.0, 4096, (20, 46)), (1.0e6, 32768, (23, 40)),
@@ -63,3 +64,26 @@ def test_workgroups_past_the_last_split_have_no_tokens(units):
         assert groups - idle == H * sum(-(-(a + t) // split_tokens) * k for a, t, k in zip(lens, drafted, blocks))
         past += idle > 0 and 7 * split_tokens >= 1 << 31
     assert past > 50   # such launches are among them
+
+
+@pytest.mark.parametrize("D,H,G", [(128, 8, 4), (64, 16, 7), (64, 4, 7), (256, 2, 3), (128, 1, 40), (64, 1, 33), (128, 1, 1), (64, 2, 100), (128, 32, 1)])
+def test_a_workspace_serves_fewer_tokens_as_well(cut, D, H, G):
+    """Sized for n_tok drafted tokens and max_len of context, it holds what is chosen for fewer of either: the size does not fall as they grow, and the cut is the one that
+    unlimited room gives.  A call with fewer tokens may want more splits of them."""
+    plan = kv.kv_layout_plan(1, H, H * G, D, [16], kv.KV_F16, 512, 4096, kv.KV_PER_SEQ)
+    tokens = list(range(1, 140)) + [200, 256]
+    for max_len in (0, 40, 700, 2000, 32768):
+        size = [kv.kv_tree_attn_workspace(plan, n, max_len) for n in tokens]
+        assert size == sorted(size)
+    assert kv.kv_tree_attn_workspace(plan, 64, 700) <= kv.kv_tree_attn_workspace(plan, 64, 2000) <= kv.kv_tree_attn_workspace(plan, 64, 32768)
+    rnd = random.Random(D + H + G)
+    limited, free = [], []
+    for _ in range(300):
+        n_max, max_len = rnd.choice([16, 17, 48, 64, 65, 256]), rnd.choice([40, 700, 1100, 2080, 4000, 32768, 131072])
+        n, length = rnd.randint(1, n_max), rnd.randint(max_len // 2, max_len)
+        case = (D, H, G, rnd.choice([16, 8, 4]), rnd.random() < 0.5, 0)
+        room = kv.kv_tree_attn_workspace(plan, n_max, max_len) // (n * H * G * (D + 2) * 4)
+        limited.append(case + (room, [length], [n]))
+        free.append(case + (1000, [length], [n]))
+    for case, a, b in zip(limited, cut(limited), cut(free)):
+        assert a == b, case
