@@ -262,11 +262,12 @@ class Plan:
 
     @property
     def shape(self):
-        """(KV heads, query heads, head_dim, torch dtype, batch + 1): what the tensors of a layer's calls are compared with."""
+        """(KV heads, query heads, head_dim, torch dtype, batch + 1, torch.float32): what the tensors of a layer's calls are compared with."""
         if self._shape is None:
             import torch
             i = self.info
-            self._shape = (i.n_kv_heads, i.n_q_heads, i.head_dim, torch.float16 if i.dtype == KV_F16 else torch.bfloat16, i.batch + 1)
+            self._shape = (i.n_kv_heads, i.n_q_heads, i.head_dim, torch.float16 if i.dtype == KV_F16 else torch.bfloat16, i.batch + 1,
+                           torch.float32)
         return self._shape
 
     def close(self):
@@ -550,12 +551,24 @@ def _kv_dtype(t) -> int:
     return d
 
 
+_int32 = None   # torch.int32, once torch is imported
+
+
+def _are_indices(t, n: int) -> bool:
+    """n int32 numbers side by side, as the kernels read them."""
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    return t.dtype is _int32 and t.numel() >= n and t.is_contiguous()
+
+
 def kv_rope(rope: Rope, positions, x, out, transposed: bool = False, stream=None) -> None:
     """x, out: [n_tok, heads, head_dim], last dim contiguous; positions: device int32 [n_tok].  out may be x."""
     n, h, d = x.shape
     xt, xh, xd = x.stride()
     ot, oh, od = out.stride()
-    if xd != 1 or od != 1 or out.shape != x.shape or out.dtype != x.dtype or positions.numel() < n:
+    if xd != 1 or od != 1 or out.shape != x.shape or out.dtype != x.dtype or not _are_indices(positions, n):
         raise KVError(KV_EINVAL, "kv_rope")
     a = kv_rope_args_t(x.data_ptr(), out.data_ptr(), xt, xh, ot, oh, positions.data_ptr(), n, h, d, _kv_dtype(x), 1 if transposed else 0, 0)
     rc = (_lib or lib()).kv_rope(rope._ref, C.byref(a), _caller_stream(stream))
@@ -567,7 +580,7 @@ def _row_strides(plan: Plan, k, v, tok_seq, tok_slot, where):
     """Strides of K's and V's rows [n_tok, H, D], which have to be of the plan's shape and type, and their number."""
     (n, h, d), (kt, kh, kd), (vt, vh, vd), shape = k.shape, k.stride(), v.stride(), plan.shape
     if kd != 1 or vd != 1 or h != shape[0] or d != shape[2] or k.dtype != shape[3] or v.dtype != shape[3] or v.shape != k.shape \
-            or tok_seq.numel() < n or tok_slot.numel() < n:
+            or not _are_indices(tok_seq, n) or not _are_indices(tok_slot, n):
         raise KVError(KV_EINVAL, where)
     return kt, kh, vt, vh, n
 
@@ -576,7 +589,7 @@ def kv_cache_write(plan: Plan, view: View, blocks: Optional[Blocks], layer: int,
                    positions=None, stream=None) -> None:
     """k, v: [n_tok, H, D], the plan's dtype, last dim contiguous; tok_seq, tok_slot, positions: device int32 [n_tok]."""
     kt, kh, vt, vh, n = _row_strides(plan, k, v, tok_seq, tok_slot, "kv_cache_write")
-    if rope is not None and (positions is None or positions.numel() < n):
+    if rope is not None and (positions is None or not _are_indices(positions, n)):
         raise KVError(KV_EINVAL, "kv_cache_write")
     a = kv_write_args_t(k.data_ptr(), v.data_ptr(), kt, kh, vt, vh, tok_seq.data_ptr(), tok_slot.data_ptr(), rope._ptr if rope is not None else None,
                         positions.data_ptr() if rope is not None else None, n, 0)
@@ -618,8 +631,10 @@ def tree_batch(tok_first: Sequence[int], tok_first_dev, mask=None) -> TreeBatch:
     """tok_first (host) and tok_first_dev (device int32), both [B + 1]: sequence b's drafted tokens are rows tok_first[b] ..
     tok_first[b + 1] - 1.  mask: device int64 [n_tok, words] (kv_tree_masks of every sequence, one after the other); None: each token follows the
     one before it."""
+    import torch
     first = (C.c_int32 * len(tok_first))(*[int(x) for x in tok_first])
-    if tok_first_dev.numel() != len(tok_first) or (mask is not None and (mask.dim() != 2 or not mask.is_contiguous() or mask.shape[0] < tok_first[-1])):
+    if tok_first_dev.numel() != len(tok_first) or not _are_indices(tok_first_dev, len(tok_first)) or \
+            (mask is not None and (mask.dim() != 2 or mask.dtype != torch.int64 or not mask.is_contiguous() or mask.shape[0] < tok_first[-1])):
         raise KVError(KV_EINVAL, "tree_batch")
     return TreeBatch(first, tok_first_dev, mask)
 
@@ -633,7 +648,7 @@ def kv_tree_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, t
     """q, out: [n_tok, H_q, D], last dim contiguous; q of the plan's dtype, out of that or fp32 (out_dtype)."""
     (n, hq, d), (qt, qh, qd), (ot, oh, od), shape = q.shape, q.stride(), out.stride(), plan.shape
     if qd != 1 or od != 1 or n < tree.n_tok or hq != shape[1] or d != shape[2] or q.dtype != shape[3] or out.shape != q.shape \
-            or len(tree.first) != shape[4] or out.element_size() != (4 if out_dtype == KV_OUT_F32 else 2):
+            or len(tree.first) != shape[4] or out.dtype != shape[5 if out_dtype == KV_OUT_F32 else 3]:
         raise KVError(KV_EINVAL, "kv_tree_attn")
     a = kv_tree_args_t(q.data_ptr(), out.data_ptr(), qt, qh, ot, oh, *tree._fixed, out_dtype, n_splits, scale)
     rc = (_lib or lib()).kv_tree_attn(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), workspace.data_ptr(),

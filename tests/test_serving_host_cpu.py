@@ -6,6 +6,7 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
 from conftest import ROOT
 from paper_2604_26557_amd import binding as kv
@@ -87,3 +88,37 @@ def test_a_workspace_serves_fewer_tokens_as_well(cut, D, H, G):
         free.append(case + (1000, [length], [n]))
     for case, a, b in zip(limited, cut(limited), cut(free)):
         assert a == b, case
+
+
+def refused(call):
+    with pytest.raises(kv.KVError) as e:
+        call()
+    return e.value.code == kv.KV_EINVAL
+
+
+def test_binding_refuses_numbers_of_another_type_or_order():
+    """Indices are read as int32 side by side, masks as 64-bit words, results written as what they are asked to be: tensors of another kind would be read past
+    their end, or as other tokens' numbers.  torch's default is int64."""
+    plan = kv.kv_layout_plan(1, 2, 4, 64, [32], kv.KV_F16, 512, 4096, kv.KV_PER_SEQ)
+    k = torch.zeros((1, 2, 32, 64), dtype=torch.float16)
+    view = kv.bhsd_view([k], [k], [20], torch.zeros(1, dtype=torch.int32))
+    i = torch.arange(4, dtype=torch.int32)
+    rows = torch.zeros((4, 2, 64), dtype=torch.float16)
+    r = kv.Rope(torch.zeros((8, 16, 2)))
+    for bad in (i.long(), i.short(), i.float(), torch.arange(8, dtype=torch.int32)[::2], torch.zeros(1, dtype=torch.int32).expand(4), torch.zeros((4, 2), dtype=torch.int32)[:, 0]):
+        assert refused(lambda: kv.kv_rope(r, bad, rows, rows))
+        assert refused(lambda: kv.kv_cache_write(plan, view, None, 0, rows, rows, bad, i))
+        assert refused(lambda: kv.kv_cache_write(plan, view, None, 0, rows, rows, i, bad))
+        assert refused(lambda: kv.kv_cache_write(plan, view, None, 0, rows, rows, i, i, r, bad))
+        assert refused(lambda: kv.kv_cache_read(plan, view, None, 0, bad, i, rows, rows))
+        assert refused(lambda: kv.kv_cache_read(plan, view, None, 0, i, bad, rows, rows))
+        assert refused(lambda: kv.tree_batch([0, 1, 2, 4], bad))
+    for bad in (torch.int32, torch.float64, torch.bool, torch.uint8):
+        assert refused(lambda: kv.tree_batch([0, 4], i[:2], torch.zeros((4, 1), dtype=bad)))
+    assert refused(lambda: kv.tree_batch([0, 4], i[:2], torch.zeros((4, 2), dtype=torch.int64)[:, :1]))
+    kv.tree_batch([0, 4], i[:2], torch.zeros((4, 1), dtype=torch.int64))
+    tree = kv.tree_batch([0, 4], i[:2])
+    q, ws = torch.zeros((4, 4, 64), dtype=torch.float16), torch.zeros(16, dtype=torch.uint8)
+    for out, kind in ((torch.bfloat16, kv.KV_OUT_SAME), (torch.int16, kv.KV_OUT_SAME), (torch.float32, kv.KV_OUT_SAME), (torch.int32, kv.KV_OUT_F32), (torch.float16, kv.KV_OUT_F32),
+                      (torch.float64, kv.KV_OUT_F32)):
+        assert refused(lambda: kv.kv_tree_attn(plan, view, None, 0, tree, q, q.to(out), kind, 0, ws))
