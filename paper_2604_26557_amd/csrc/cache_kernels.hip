@@ -249,7 +249,7 @@ int launch_rows(const kv_plan *pl, RowParams &p, bool write, int format, bool pa
 int kvb::cache_addr(const kv_plan *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const int *lens, const int *first, CacheAddr *c)
 {
     *c = CacheAddr{};
-    if (!view->k_layers || !view->v_layers) return KV_EINVAL;
+    if (!view->k_layers || !view->v_layers || view->seq_off_host || view->seq_off_dev) return KV_EINVAL;
     if (layer < 0 || layer >= p->L || layer >= view->n_layers) return KV_ERANGE;
     const int format = blocks ? blocks->format : KV_FORMAT_16;
     if (blocks) {
@@ -278,7 +278,6 @@ int kvb::cache_addr(const kv_plan *p, const kv_view_t *view, const kv_blocks_t *
     if (view->layout == KV_LAYOUT_BHSD) {
         if (view->stride_b < 0 || view->stride_h < 0 || view->stride_s < 0 || view->s_alloc < 0) return KV_EINVAL;
         if ((view->stride_b | view->stride_h | view->stride_s) & 7) return KV_EINVAL;
-        if (view->seq_off_host || view->seq_off_dev) return KV_EINVAL;
         c->sb = 2 * (uint64_t)view->stride_b; c->sh = 2 * (uint64_t)view->stride_h; c->ss = 2 * (uint64_t)view->stride_s;
         c->rows = view->s_alloc;
         for (int b = 0; b < p->B; ++b) {

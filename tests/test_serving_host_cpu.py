@@ -1,4 +1,5 @@
 """The serving step's host side where it is easily got wrong: ends of schedules, sizes, kinds of tensors."""
+import ctypes as C
 import math
 import os
 import random
@@ -10,6 +11,7 @@ import torch
 
 from conftest import ROOT
 from paper_2604_26557_amd import binding as kv
+from test_serving_cpu import P, Fake
 from test_tree_cut_cpu import cut  # noqa: F401
 
 
@@ -122,3 +124,15 @@ def test_binding_refuses_numbers_of_another_type_or_order():
     for out, kind in ((torch.bfloat16, kv.KV_OUT_SAME), (torch.int16, kv.KV_OUT_SAME), (torch.float32, kv.KV_OUT_SAME), (torch.int32, kv.KV_OUT_F32), (torch.float16, kv.KV_OUT_F32),
                       (torch.float64, kv.KV_OUT_F32)):
         assert refused(lambda: kv.kv_tree_attn(plan, view, None, 0, tree, q, q.to(out), kind, 0, ws))
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+@pytest.mark.parametrize("which", ["seq_off_host", "seq_off_dev"])
+def test_views_whose_rows_start_later_are_refused(paged, fmt, which):
+    """The calls do not know such rows, in either layout."""
+    off = (C.c_int64 * 2)(0, 0)
+    ok = Fake(paged=paged, fmt=fmt)
+    assert ok.attn() == ok.rows_call("kv_cache_write") == ok.rows_call("kv_cache_read") == kv.KV_OK
+    setattr(ok.view, which, C.cast(off, type(getattr(ok.view, which))) if which == "seq_off_host" else P)
+    assert ok.attn() == ok.rows_call("kv_cache_write") == ok.rows_call("kv_cache_read") == kv.KV_EINVAL
