@@ -110,7 +110,7 @@ __device__ __forceinline__ void store_columns(void *out, long long i, int mode, 
     }
 }
 
-constexpr float kNoScore = -1.0e30f;    // reference of a row that has seen no score
+constexpr float kNoScore = -3.402823466e38f;   // reference of a row that has seen no score: no number is less
 // A reference follows the running maximum when a probability passes 2^4 of it.
 constexpr float kLargeRef = 1048576.f;  // beyond it the rounding of a reference would leave the range of the probabilities
 // fp16 probabilities are taken of 2^11 times themselves (at most 2^15): what is lost lies below 2^-36 of the largest

@@ -38,3 +38,36 @@ def test_16_bit_results_are_rounded_once(dtype, fmt, D, H, G, lens, trees):
     q = rows((sum(trees), H * G, D), dtype, 41).cuda()
     for n_splits in (0, 1, 3):
         check_same(c, q, parents, c.attend(q, parents, kv.KV_OUT_SAME, n_splits))
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("size", [1.0e15, 1.0e16, 1.0e18])
+@pytest.mark.parametrize("n_splits", [0, 1, 3])
+def test_scores_far_below_any_reference(fmt, size, n_splits):
+    """Rows all of whose scores are finite, but below -1e30: the largest of them takes all.  Only a row that sees nothing yields zeros."""
+    H, G, D, n = 1, 2, 64, 5
+    c = Cache([300], H, D, torch.bfloat16, fmt, seed=42, extra=n, n_q_heads=G)
+    level = 1 + np.arange(c.rows) % 7   # the first element of K is -level times `size`, the others are zero; level 1 is that of every seventh token
+    for j in range(c.rows):
+        for d in range(D):
+            c.values["k"][0, :, j, d] = 0
+        c.values["k"][0, :, j, 0] = -float(level[j]) * float(torch.tensor(size, dtype=torch.bfloat16))
+    k = torch.from_numpy(c.values["k"].astype(np.float32)).to(torch.bfloat16)
+    if fmt == "16":
+        c.dev["k"][:] = k.cuda()
+    else:
+        i = torch.arange(c.rows, dtype=torch.int32, device="cuda")
+        v = torch.zeros((c.rows, H, D), dtype=torch.bfloat16, device="cuda")
+        keep = c.dev["v"].clone(), c.dev["v_scale"].clone()
+        kv.kv_cache_write(c.plan, c.view, c.blocks, 0, k[0].transpose(0, 1).contiguous().cuda(), v, torch.zeros_like(i), i)
+        c.dev["v"][:], c.dev["v_scale"][:] = keep
+    q = torch.zeros((n, G, D), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0e17
+    got = c.attend(q, [[-1, 0, 1, 2, 3]], n_splits=n_splits).double().cpu().numpy()
+    if fmt != "16":   # the codes round 5 and 7 to neighbours in 4 bits: levels stay apart from 1
+        assert (level == 1).sum() > 40
+    for t in range(n):
+        best = np.flatnonzero(level[:300 + t + 1] == 1)
+        want = c.values["v"][0, 0, best].mean(0)
+        # 44 values added up in 32 bits, each sum off by a unit of at most 44 times the largest, and a division
+        assert np.abs(got[t] - want).max() <= 64 * 2.0 ** -24 * np.abs(c.values["v"]).max() * 44
