@@ -16,6 +16,7 @@ using namespace kvb;
 // exponentials take one instruction for the row, and the sums of up to 8 * 64 / (D / 4) splits are loaded at once, ahead of the weights.  Bound by its launch and two dependent reads: 3.9 us for 7
 // splits of 512 rows, 5.9 for 16 of 2048 (17 MB).
 constexpr int kCombineWaves = 4;
+constexpr float kNothing = -1.f;   // weight of a split without anything
 template <int D>
 __global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(TreeParams p)
 {
@@ -44,25 +45,29 @@ __global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(Tre
     float to = fmaxf(m0[0], m1[0]);
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) to = fmaxf(to, __shfl_xor(to, o));
-    // an infinity stays one: no weight of a split that has something is zero
-    const float w0 = m0[1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m0[0] - to), 1.0e-37f), w1 = m1[1] == 0.f ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m1[0] - to), 1.0e-37f);
+    const float w0 = m0[1] == 0.f ? kNothing : __builtin_amdgcn_exp2f(m0[0] - to), w1 = m1[1] == 0.f ? kNothing : __builtin_amdgcn_exp2f(m1[0] - to);
     float l = m0[1] * w0 + m1[1] * w1;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) l += __shfl_xor(l, o);
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < ns; s0 += kRound * kTogether) {
-        if (s0 > 0) load(s0);
+    auto add = [&](auto some_are_zero) {
+        for (int s0 = 0; s0 < ns; s0 += kRound * kTogether) {
+            if (s0 > 0) load(s0);
 #pragma unroll
-        for (int k = 0; k < kRound; ++k) {
-            const int s = s0 + k * kTogether + sub;
-            if (s0 + k * kTogether >= ns) break;
-            const float f = __shfl(s0 < 64 ? w0 : w1, s & 63);
-            if (s < ns && f != 0.f) {
+            for (int k = 0; k < kRound; ++k) {
+                const int s = s0 + k * kTogether + sub;
+                if (s0 + k * kTogether >= ns) break;
+                const float f = __shfl(s0 < 64 ? w0 : w1, s & 63);
+                if (s < ns && f != kNothing) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = fmaf(y[k][e], f, x[e]);
+                    for (int e = 0; e < 4; ++e)   // a weight too small for 32 bits still counts against an infinity
+                        x[e] = fmaf(y[k][e], decltype(some_are_zero)::value && f == 0.f && !__builtin_isfinite(y[k][e]) ? 1.0e-37f : f, x[e]);
+                }
             }
         }
-    }
+    };
+    if (__any(w0 == 0.f || w1 == 0.f)) add(std::true_type{});
+    else add(std::false_type{});
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
 #pragma unroll

@@ -71,3 +71,45 @@ def test_scores_far_below_any_reference(fmt, size, n_splits):
         want = c.values["v"][0, 0, best].mean(0)
         # 44 values added up in 32 bits, each sum off by a unit of at most 44 times the largest, and a division
         assert np.abs(got[t] - want).max() <= 64 * 2.0 ** -24 * np.abs(c.values["v"]).max() * 44
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n_splits", [1, 2, 4, 9])
+@pytest.mark.parametrize("far", [100.0, 300.0, 2000.0])
+def test_splits_that_weigh_nothing_add_nothing(D, n_splits, far):
+    """Values of 1e36 in tokens whose weight is exp(-far): what is finite there counts for its weight and no more, in whatever split it is."""
+    c = Cache([320], 1, D, torch.bfloat16, "16", seed=43, extra=1, n_q_heads=2)
+    big = float(torch.tensor(1.0e36, dtype=torch.bfloat16))
+    for kind in "kv":
+        t = c.dev[kind].cpu()
+        if kind == "k":
+            t[0, :, :, 0] = 0
+            t[0, :, :64, 0] = -float(torch.tensor(far, dtype=torch.bfloat16))   # as good as sure to be far below all others
+            t[0, :, :, 1:] = t[0, :, :, 1:] * 2.0 ** -3
+        else:
+            t[0, :, :64] = big
+        c.dev[kind] = t.cuda()
+        c.values[kind] = t.double().numpy()
+    c.remake()
+    q = rows((1, 2, D), torch.bfloat16, 44)
+    q[..., 0] = D ** 0.5
+    q = q.cuda()
+    out, weight, spread = c.expected(q, [[-1]])
+    got = c.attend(q, [[-1]], n_splits=n_splits).double().cpu().numpy()
+    if far == 100.0:   # weights of 1e-44 times 1e36: next to nothing, by the formula as well
+        assert weight.max() < 10
+    tol = attention_bound(out, weight, spread, 600, c.dtype, True)
+    assert (np.abs(got - out) <= tol).all(), np.abs(got - out).max()
+
+
+@pytest.mark.parametrize("n_splits", [1, 2, 4])
+def test_an_infinity_of_little_weight_stays_one(n_splits):
+    """A weight that is no number of 32 bits any more is still not zero."""
+    c = Cache([320], 1, 64, torch.bfloat16, "16", seed=45, extra=1, n_q_heads=2)
+    c.dev["k"][0, :, :, 0] = 0
+    c.dev["k"][0, :, :64, 0] = -300
+    c.dev["v"][0, :, 20, 7] = float("-inf")
+    q = rows((1, 2, 64), torch.bfloat16, 46)
+    q[..., 0] = 8
+    got = c.attend(q.cuda(), [[-1]], n_splits=n_splits)
+    assert (got[..., 7] == float("-inf")).all() and torch.isfinite(got[..., :7]).all() and torch.isfinite(got[..., 8:]).all()
