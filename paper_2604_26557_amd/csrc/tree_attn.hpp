@@ -43,7 +43,8 @@ struct TreeParams {
     const int *seq_lens, *tok_first;
     const unsigned long long *mask;    // null: a chain
     float *part_acc, *part_ml;         // [n_tok * Hq, ns, D] and [n_tok * Hq, ns, 2]; not read where ns = 1
-    float scale_log2e;
+    float scale_log2e;                 // without its sign
+    unsigned q_sign;                   // the scale's, for the two halves of a word of q
     int words, max_total, H, G, B, out_mode;  // out_mode: 0 fp32, 1 fp16, 2 bf16
     int ns, split_tokens, row_blocks;
     int bt_shift;                      // log2 of a block's tokens, or -1
@@ -342,7 +343,7 @@ __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table,
 {
     const int t = token_of(p, r), hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
     const u32x2 qw = *(const u32x2 *)(p.q + 2 * ((first + t) * p.q_st + hq * p.q_sh + 4 * at));
-    const f32x2 q0 = unpack2<BF16>(qw[0]), q1 = unpack2<BF16>(qw[1]);
+    const f32x2 q0 = unpack2<BF16>(qw[0] ^ p.q_sign), q1 = unpack2<BF16>(qw[1] ^ p.q_sign);
     auto row = [&](const char *rows, const char *scales, int j, bool *there) {
         const RowAt x = row_at(p.c, table, base, zbase, j);
         *there = x.there;
@@ -792,6 +793,15 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     else wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    // A negative scale turns q's signs here: references and masks are those of a positive one.
+    if (const unsigned sign = arguments().q_sign; sign != 0) {
+#pragma unroll
+        for (int k = 0; k < T::kQIssues; ++k) {
+            const int i = wave + k * kWaves;
+            if (i < NB * kSteps) ((u32x4 *)(lds + T::kRing))[i * 64 + lane] ^= sign;
+        }
+        __syncthreads();
+    }
     if constexpr (!T::kQStays) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)

@@ -150,7 +150,8 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.words = a->mask_words;
     t.max_total = max_total;
     t.H = p->H; t.G = p->Hq / p->H; t.B = p->B;
-    t.scale_log2e = (float)(1.4426950408889634 * (a->scale == 0.f ? 1 / std::sqrt((double)p->D) : (double)a->scale));
+    t.scale_log2e = (float)(1.4426950408889634 * (a->scale == 0.f ? 1 / std::sqrt((double)p->D) : std::fabs((double)a->scale)));
+    t.q_sign = a->scale < 0.f ? 0x80008000u : 0;
     t.out_mode = a->out_dtype == KV_OUT_F32 ? 0 : bf16 ? 2 : 1;
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;

@@ -113,3 +113,28 @@ def test_an_infinity_of_little_weight_stays_one(n_splits):
     q[..., 0] = 8
     got = c.attend(q.cuda(), [[-1]], n_splits=n_splits)
     assert (got[..., 7] == float("-inf")).all() and torch.isfinite(got[..., :7]).all() and torch.isfinite(got[..., 8:]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("G,lens,trees", [(4, [70, 0], [9, 40]), (1, [300, 41], [1, 3])])
+def test_a_negative_scale_is_that_of_negated_queries(dtype, fmt, G, lens, trees):
+    """Bit for bit, where scores are whole numbers (the order and rounding of their sums is nothing then): masks and references know the sign, so
+    the same arithmetic is done."""
+    parents = [random_parents(np.random.default_rng(47), n) for n in trees]
+    c = Cache(lens, 2, 64, dtype, fmt, seed=47, extra=max(trees), n_q_heads=2 * G)
+    rng = np.random.default_rng(48)
+    i = torch.arange(2 * c.rows, dtype=torch.int32, device="cuda")
+    k = torch.from_numpy(rng.integers(-2, 3, (2 * c.rows, 2, 64)).astype(np.float32)).to(dtype)   # numbers of every format
+    keep = {name: t.clone() for name, t in c.dev.items() if name[0] == "v"}
+    kv.kv_cache_write(c.plan, c.view, c.blocks, 0, k.cuda(), torch.zeros_like(k).cuda(), i // c.rows, i % c.rows)
+    for name, t in keep.items():
+        c.dev[name][:] = t
+    c.values["k"] = k.double().numpy().reshape(2, c.rows, 2, 64).transpose(0, 2, 1, 3)
+    q = torch.from_numpy(rng.integers(-3, 4, (sum(trees), 2 * G, 64)).astype(np.float32)).to(dtype).cuda()
+    for n_splits in (0, 1, 2):
+        got = c.attend(q, parents, n_splits=n_splits, scale=-0.125)
+        assert torch.equal(got, c.attend(-q, parents, n_splits=n_splits, scale=0.125))
+        out, weight, spread = c.expected(-q, parents, scale=0.125)
+        tol = attention_bound(out, weight, spread, max(lens) + 256, dtype, True)
+        assert (np.abs(got.double().cpu().numpy() - out) <= tol).all()
