@@ -13,6 +13,7 @@ from conftest import ROOT
 from paper_2604_26557_amd import binding as kv
 from test_serving_cpu import P, Fake
 from test_tree_cut_cpu import cut  # noqa: F401
+from treeshapes import SHAPES, without_a_context
 
 
 @pytest.mark.parametrize("base,trained,ends", [(10000.0, 65536, (40, 65)), (10000.0, 131072, (45, 70)), (10000.0, 4096, (20, 46)), (1.0e6, 32768, (23, 40)),
@@ -136,3 +137,33 @@ def test_views_whose_rows_start_later_are_refused(paged, fmt, which):
     assert ok.attn() == ok.rows_call("kv_cache_write") == ok.rows_call("kv_cache_read") == kv.KV_OK
     setattr(ok.view, which, C.cast(off, type(getattr(ok.view, which))) if which == "seq_off_host" else P)
     assert ok.attn() == ok.rows_call("kv_cache_write") == ok.rows_call("kv_cache_read") == kv.KV_EINVAL
+
+
+@pytest.mark.parametrize("D,nb", list(SHAPES))
+def test_batches_for_wide_kernels_take_them(cut, D, nb):
+    """What the GPU tests of 32 and 64 rows a workgroup go by: in every format and layout, with the workspace that they have."""
+    cases = []
+    for H, G, lens, drafted, splits in SHAPES[D, nb] + [without_a_context(SHAPES[D, nb][2])[0]]:
+        plan = kv.kv_layout_plan(1, H, H * G, D, [16], kv.KV_F16, 512, 4096, kv.KV_PER_SEQ)
+        room = kv.kv_tree_attn_workspace(plan, sum(drafted), max(lens) + 256) // (sum(drafted) * H * G * (D + 2) * 4)
+        cases += [(D, H, G, bits, paged, n, room, lens, drafted) for n in splits for bits in (16, 8, 4) for paged in (False, True)]
+    got = cut(cases)
+    assert [c["nb"] for c in got] == [nb] * len(cases)
+    assert max(c["ns"] for c in got) > 1 and max(c["row_blocks"] for c in got) > 1 and max(c["split_tokens"] for c in got) >= 576
+
+
+def test_more_sequences_than_are_counted_one_by_one(cut):
+    """From 65 sequences on workgroups are estimated from sums: the cut still covers everything, and equal batches on either side are cut alike."""
+    rnd = random.Random(9)
+    cases = []
+    for _ in range(200):
+        B = rnd.choice([64, 65, 66, 100, 300])
+        cases.append((rnd.choice([64, 128, 256]), rnd.choice([1, 4, 8]), rnd.choice([1, 4, 7]), rnd.choice([16, 8, 4]), rnd.random() < 0.5, rnd.choice([0, 0, 2]), -1,
+                      [rnd.choice([0, 31, 700, 4096, rnd.randrange(1, 40000)]) for _ in range(B)], [rnd.choice([1, 1, 5, 64]) for _ in range(B)]))
+    for (D, H, G, bits, paged, n, ws, lens, drafted), c in zip(cases, cut(cases)):
+        rows, longest = max(drafted) * G, max(a + t for a, t in zip(lens, drafted))
+        assert 16 * c["nb"] * c["row_blocks"] >= rows > 16 * c["nb"] * (c["row_blocks"] - 1)
+        assert c["split_tokens"] % 32 == 0 and c["ns"] * c["split_tokens"] >= longest > (c["ns"] - 1) * c["split_tokens"]
+    for n, t in ((300, 1), (4096, 4), (2000, 16)):
+        a, b = cut([(128, 8, 4, 8, True, 0, -1, [n] * B, [t] * B) for B in (64, 65)])
+        assert a["nb"] == b["nb"] and abs(a["ns"] - b["ns"]) <= 1
