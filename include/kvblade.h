@@ -634,7 +634,9 @@ int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t *masks, int
  * sequence is plain decoding).  A row that sees nothing yields zeros; what a row does not see has no effect on it, infinities and NaNs included.
  * fp32 scores, maxima and sums; probabilities enter the product with V, and their sum, in parts that add up to the fp32 value: exactly (bf16, KV_OUT_F32), to
  * within 2^-22 of it (fp16) or 2^-16 (bf16, KV_OUT_SAME: results that are rounded to 2^-8).
- * A row all of whose scores are -infinity yields zeros too; NaNs that a row sees spread as in the formula.
+ * A row all of whose scores are -infinity yields zeros too; NaNs that a row sees spread as in the formula.  Scores are held times log2(e), and sums are divided in the end: what
+ * passes fp32 in these is an infinity (bf16 alone gets there).  A value that is not finite, seen or not, sends the splits that hold it to a form that goes row by row: some hundred times slower.
+ * scale may be negative.
  * head_dim 64, 128 or 256; at most 4095 query heads per KV head (KV_EINVAL) and 2^30 tokens of context (KV_ERANGE).  q: the plan's dtype; q strides: elements,
  * multiples of 8; out strides: elements; q and workspace 16-byte aligned.  A row's scales are aligned to their number (head_dim/32 bytes).
  * Fastest where a head's rows lie side by side and blocks of a pool hold a multiple of 16 tokens; everything else is looked up row by row.

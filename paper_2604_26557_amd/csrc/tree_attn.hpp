@@ -11,15 +11,16 @@
 // changes lanes.  Sums of probabilities are one more product, with ones.
 //
 // What bounds it, and what was measured (MI355X, us per call, the second launch that joins splits included):
-//   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 49.4 = 5.6 TB/s;
-//   the vector ALU, where rows are many (an exponential for every row and token, a conversion for every element of K and V, beside the matrix cores at 32 %): 32K tokens x
-//   8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 56.3 = 611 TFLOP/s;
-//   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 14.1.
+//   the bytes of K and V, where rows are few: 4 sequences of 8K x 16 heads x 256, 8-bit, 6 rows per head: 278 MB in 49.2 = 5.6 TB/s;
+//   the vector ALU, where rows are many (an exponential for every row and token and its two parts, a conversion for every element of K and V, beside the matrix cores at 39 %): 32K
+//   tokens x 8 heads x 128, 8-bit, 256 rows per head: 34.4 GFLOP in 67.4 = 510 TFLOP/s;
+//   the start of a workgroup, its merge (3 to 5 us) and the second launch (4), where the call is short: 4K tokens x 8 heads x 128, 64 rows per head: 14.2.
 // Why so:
-//   K and V go through LDS, loaded there without passing registers: 16 KiB of a wavefront are on their way while it computes, without spilling what holds the sums.  With loads into
-//   registers, when this was changed: 307 at the 32K case (88 through LDS), 91 at the 256-wide heads (73).
-//   64 rows per workgroup where there are as many: 32 rows take 72.7 and 16 rows 98.0 at the 32K case (64: 63.6); where there are but 16 (32K tokens, 16 bits, 4 drafted),
-//   16 take 29.6, 32 30.4 and 64 33.8.  Which, and how many splits: cut_tree.
+//   K and V go through LDS, loaded there without passing registers: 16 KiB of a wavefront are on their way while it computes, without spilling what holds the sums.  When this was
+//   changed: 307 -> 88 at the 32K case, 91 -> 73 at the 256-wide heads.
+//   64 rows per workgroup where there are as many: the 32K case takes 68.6 with 64, 74.5 with 32 and 103.9 with 16, in 16 bits 66.9, 87.3 and 135.5, each with its best number of splits; where
+//   there are but 16 (32K tokens, 16 bits, 4 drafted), 16 take 27.8, 32 28.9 and 64 33.1.  Which, and how many splits: cut_tree.  With 32-bit results of bf16 three instances of 64 rows spill
+//   (D = 128; 8-bit rows most: 48 registers): 91 in the loop in which 16-bit results take 76.
 //   Four wavefronts, merged by halves: what one gives another goes through LDS twice (half, then a quarter of the sums), and two workgroups share a compute unit: one
 //   merges while the other reads.
 #pragma once
@@ -182,7 +183,6 @@ struct TreeTile {
     static constexpr int kLds = kRing + kQBytes > kMerge + kStates ? kRing + kQBytes : kMerge + kStates;
     static_assert(kLds <= (D == 256 ? 2 : 1) * kHalfLds, "LDS of a compute unit");
     static constexpr int kQIssues = (NB * kSteps + kWaves - 1) / kWaves;
-    static constexpr int kPerCu = kLds <= 40 * 1024 ? 4 : kLds <= kHalfLds / 3 * 2 ? 3 : kLds <= kHalfLds ? 2 : 1;
 
     // The first of the eight elements of d that a lane contributes to product s: any order will do that q follows as well.
     static __device__ __forceinline__ int q_at(int s, int group)
@@ -275,7 +275,7 @@ __device__ __forceinline__ unsigned quotient(unsigned x, unsigned d, unsigned by
 __device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G == 1 ? r : (int)__umulhi((unsigned)r, p.by_g); }
 
 // The kernel's arguments, loaded where they are needed: what is only used now and then, or after the loop, takes no scalar registers in it (there are too few: the
-// others would be kept in lanes of a vector register and fetched from there at each step: 4 sequences of 8K x 16 heads x 256, 8 bits, 51.8 us, now 49.0).
+// others would be kept in lanes of a vector register and fetched from there at each step: when this was changed, 4 sequences of 8K x 16 heads x 256 of 8 bits went from 51.8 to 49.0 us).
 __device__ __forceinline__ TreeParams arguments()
 {
 #if __HIP_DEVICE_COMPILE__
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     };
 
     // Query rows: token-major, the G heads of a token side by side.  Those past the last one are copies of it, whose results go nowhere.  They go to LDS ahead of the steps'
-    // K and V: loaded into registers behind these, they were there only when all of these were (4K tokens, 16 drafted: 15.0 us, now 14.3; 48 single tokens 22.7, 21.6).
+    // K and V: loaded into registers behind these, they were there only when all of these were (when this was changed: 4K tokens, 16 drafted 15.0 -> 14.3 us; 48 single tokens 22.7 -> 21.6).
     auto row_token = [&](int r) { return token_of(p, (int)rb * kRows + r); };
     const u32x4 *const q_lds = (const u32x4 *)(lds + T::kRing);
     auto issue_q = [&] {   // a wavefront's share of them to LDS
@@ -767,14 +767,14 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 
     // Steps.  Loads come back in order: all but those issued later are waited for.
     // Early: K and V of a step are read from LDS at once and its place loaded again before anything is computed; else V is read after the softmax.  Codes are few registers:
-    // 32K tokens x 8 heads x 128, 8 bits, 32 rows 27.0 us early, 27.8 late; 4 x 8K x 16 x 256, 8 bits, 16 rows 51.4-54.0, 54.7-55.7; 32 x 500-2000 x 8 x 128, paged, 25.1, 26.5.
-    // 16-bit rows, and more rows at 256 columns, leave too few for the sums: 32K tokens, 16 bits, 16 rows 31.2 early, 30.5 late; 16 x 4K, 32 rows 60.0, 57.8; 4 x 8K x 16 x 256,
-    // 8 bits, 32 rows 61.2, 59.8.
+    // early and late, us, 4 x 8K x 16 x 256, 8 bits, 16 rows 49.2, 51.8; a ragged step of 32 rows, 8 bits 47.3, 48.1; 48 single tokens, 4 bits 21.4, 21.6; 32 x 500-2000 x 8 x 128 24.6, 25.8.
+    // 16-bit rows, and more rows at 256 columns, leave too few for the sums: 16 x 4K, 16 bits, 32 rows 60.5, 59.0; 4 x 8K x 16 x 256, 8 bits, 32 rows 59.9, 58.2; 64 rows spill: 32K tokens,
+    // 8 bits 107, 67.4; a ragged batch of 16 bits 61.4, 50.4.  (32K tokens, 16 bits, 16 rows: 29.8 both ways.)
     constexpr int kKIssues = T::kLoads + T::kZLoads, kVIssues = T::kLoads;
     constexpr bool kEarly = T::kBlocks && NB * D <= 256;
-    // From 32 rows on a wavefront goes ahead of the other one of its SIMD in its products, whose operands wait for conversions and permutes between them: 32K tokens x 8 heads x 128,
-    // 64 drafted, in 8 bits 66.9 -> 63.4 us (64.4 with the second product alone), in 16 bits, where K needs no conversion, 63.0 -> 60.3 with the second alone (62.2 with both);
-    // 32 rows of a ragged 8-bit batch 37.8 -> 36.0.  With 16 rows it is as often slower (32 x 500-2000 tokens 23.2 -> 23.7) as faster (48 single tokens 21.5 -> 21.0).
+    // From 32 rows on a wavefront goes ahead of the other one of its SIMD in its products, whose operands wait for conversions and permutes between them: neither product, the second, both, us:
+    // 32K tokens x 8 heads x 128, 64 drafted, in 8 bits 70.1, 68.5, 67.4; in 16 bits, where K needs no conversion, 70.9, 68.7, 72.2; 32 rows of a ragged 8-bit step 49.8, 48.6, 47.4.  With 16 rows it
+    // is as often slower (32 x 500-2000 tokens 24.7 -> 25.3) as faster (48 single tokens 21.4 -> 20.9).
     constexpr bool kFirst = NB >= 2, kFirstK = kFirst && T::kBlocks;
     unsigned there[kStages], stage = 0;
     issue_q();

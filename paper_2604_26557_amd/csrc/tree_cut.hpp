@@ -60,8 +60,8 @@ constexpr bool split_has_tokens(unsigned split, int split_tokens, int total) { r
 //   a workgroup's start and merge, and its wavefronts' steps of 32 tokens; every further workgroup on the fullest compute unit adds 40 % of the one and 41 to 50 % of the other;
 //   the whole cache through HBM once, and again through L2 for further row blocks;
 //   where there are splits a second launch, and partial results written and read.
-// Its choice was 4 % from a shape's best on average, within 5 % on 28 of the 36, within 10 % on 31 and 63 % off on the worst (many short sequences of unequal length, whose
-// workgroups it takes for equals); the times themselves it gives to 13 % on average.
+// The fit was to kernels with one part to a probability of a 16-bit result.  With the present ones its choice is 7 % from a shape's best on average, within 5 % on 26 of the 36, within 10 %
+// on 28 and 70 % off on the worst (many short sequences of unequal length, whose workgroups it takes for equals), where it was 6 %, 26, 28 and 70 %; the times themselves it gives to 13 % on average.
 // At least one token is drafted.
 inline TreeCut cut_tree(const TreeShape &s, int B, const int *lens, const int *first, int n_splits, uint64_t ws_bytes)
 {

@@ -13,8 +13,8 @@ namespace {
 using namespace kvb;
 
 // A wavefront joins the splits of one query row: out = sum_s 2^(ref_s - max) acc_s / sum_s 2^(ref_s - max) l_s.  A lane has the weight of a split (of two, beyond 64), so the
-// exponentials take one instruction for the row, and the sums of up to 8 * 64 / (D / 4) splits are loaded at once, ahead of the weights.  Bound by its launch and two dependent reads: 3.9 us for 7
-// splits of 512 rows, 5.9 for 16 of 2048 (17 MB).
+// exponentials take one instruction for the row, and the sums of up to 8 * 64 / (D / 4) splits are loaded at once, ahead of the weights.  Bound by its launch and two dependent reads: 4.0 us for 7
+// splits of 512 rows, 5.8 for 16 of 2048 (17 MB).
 constexpr int kCombineWaves = 4;
 constexpr float kNothing = -1.f;   // weight of a split without anything
 template <int D>
