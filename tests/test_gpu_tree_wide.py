@@ -127,3 +127,22 @@ def test_wide_runs_give_the_same_bits():
     first = run(c, q, masks, kv.KV_OUT_SAME, 2)
     for _ in range(5):
         assert torch.equal(run(c, q, masks, kv.KV_OUT_SAME, 2), first)
+
+
+@pytest.mark.parametrize("od", OUTS)
+@pytest.mark.parametrize("pad", [1, 2, 3, 4])
+@pytest.mark.parametrize("D,nb", list(SHAPES) + [(64, 1), (128, 1), (256, 1)])
+def test_results_at_any_stride(D, nb, pad, od):
+    """Results whose rows start at odd elements have the bits of those side by side, and nothing between them is written."""
+    if nb == 1:
+        c = WideCache([300, 40, 0], 2, D, 3, torch.bfloat16, "fp8", LAYOUTS[1], 5, 19)
+        masks, splits = [sees(random_parents(np.random.default_rng(n), n)) for n in (5, 1, 3)], (1, 2)
+        q = torch.from_numpy(np.random.default_rng(3).standard_normal((9, 6, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    else:
+        c, q, masks, splits = make(D, nb, 2, "fp8", torch.bfloat16, LAYOUTS[1], "tree", 19)
+    words, parents = words_of(masks), [[-1] * len(m) for m in masks]
+    for n in splits + (1,):
+        want = c.attend(q, parents, od, n, mask=words)
+        wide = torch.full((len(q), q.shape[1], D + pad), 7, dtype=want.dtype, device="cuda")
+        c.attend(q, parents, od, n, mask=words, out=wide[..., :D])
+        assert torch.equal(wide[..., :D], want) and (wide[..., D:] == 7).all()
