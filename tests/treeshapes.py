@@ -3,7 +3,7 @@ import numpy as np
 import torch
 
 from paper_2604_26557_amd import binding as kv
-from servecase import FORMATS, Cache
+from servecase import Cache
 
 # (head_dim, row groups of 16): (KV heads, query heads of each, contexts, drafted tokens, numbers of splits to ask for).  On 256 compute units the cut takes that many row groups for each, in every
 # format and layout and whatever the results' type.  Last row blocks of 1 to 64 rows, sequences without context or drafted tokens, several steps of each wavefront.
