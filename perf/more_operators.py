@@ -363,7 +363,7 @@ def _handles(s, c):
     s["shared"] = kv.prefix_groups(first, _dev(first), shared, _dev(shared)) if shared else None
     s["scores"] = None
     if c["cap"] or c["slopes"] or s["from"] is not None or s["to"] is not None:
-        s["scores"] = kv.scores(softcap=c["cap"], slopes=s["slope"], positions=s["pos"] if c["slopes"] and c["tree"] else None, sees_from=s["from"], sees_to=s["to"])
+        s["scores"] = kv.scores(softcap=c["cap"], slopes=s["slope"], positions=s["pos"] if c["slopes"] else None, sees_from=s["from"], sees_to=s["to"])
     s["ws"] = torch.empty(kv.kv_group_attn_workspace(s["plan"], s["first"][-1], s["total"]), dtype=torch.uint8, device="cuda")
 
 
