@@ -661,13 +661,127 @@ int kv_tree_attn(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t
 size_t kv_tree_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
 
 /* ------------------------------------------------------------------------------------------ */
+/* A serving step of a batch of requests: its tables, attention over shared prefixes and of   */
+/* capped, biased or bounded scores, sampling (stream-ordered, no blocking, no allocation)    */
+/* ------------------------------------------------------------------------------------------ */
+
+/*
+ * kv_step_tables -- a step's block tables and slot maps, built on the GPU from the lengths of its requests.
+ * Sequence b has seq_lens[b] cached tokens and new_lens[b] to come, whose blocks have to be there; new_lens[b] < 0: the request has ended.  Its row of the block table holds
+ * held[b] blocks, the next entries are -1.  With n = seq_lens[b] + new_lens[b] (0 if it has ended) and need = ceil(n / block_tokens):
+ *   entries shared[b] .. held[b] - 1 of an ended request go back to the free blocks, its row becomes -1 and held_out 0;
+ *   entries held[b] .. need - 1 of another are filled: those below shared[b] with the same entries of leader[b]'s row (a prefix that is in the cache once; what leader[b]'s row holds after
+ *   this call, except what it would itself take from a leader in this call), the others with free blocks.  held_out = max(held, need): blocks of tokens that were given up
+ *   stay with their sequence.
+ * leader[b] outside [0, batch) or b itself: none, and shared[b] counts as 0.  Shared entries belong to the leader, which has to end after those that follow it.
+ * free_ids[0 .. n_free) is a stack: what ends is pushed in the order of sequences and entries, then blocks are taken from its top in that order.
+ * If there are too few of them, or need exceeds max_blocks somewhere, nothing is handed out (requests that ended are released all the same) and held_out = held for the others:
+ * status[0] = blocks missing, status[1] = sequences that do not fit their row, both 0 otherwise.
+ * tok_first, tok_seq, tok_slot: the step's new tokens in order of sequences, token i of sequence b at row tok_first[b] + i, place seq_lens[b] + i (kv_cache_write's maps, and positions
+ * of a chain); written whatever the status is.  Rows of the maps past the last token, up to n_tok, become -1 (kv_cache_write skips them), tokens past n_tok have no row.
+ * held_out, n_free_out and block_table_out are the inputs themselves (all three: the step's changes are written in place) or other arrays (all three: rows are copied, the old ones stay
+ * as they were for work still to read them; the work is spread over the card).
+ * Values out of range do no harm: lengths count as 0 at least, held and n_free as within their arrays.  batch at most 8192.
+ */
+typedef struct kv_tables_args {
+    int32_t batch, block_tokens;
+    int32_t max_blocks;      /* entries of a row */
+    int32_t n_pool;          /* entries of free_ids */
+    int32_t n_tok;           /* rows of tok_seq and tok_slot */
+    int32_t reserved;
+    const int32_t *seq_lens, *new_lens; /* device [batch] */
+    const int32_t *leader, *shared;     /* device [batch], both or neither */
+    const int32_t *held;                /* device [batch] */
+    const int32_t *n_free;              /* device [1] */
+    const int32_t *block_table;         /* device [batch, max_blocks] */
+    int32_t *free_ids;                  /* device [n_pool] */
+    int32_t *held_out, *n_free_out, *block_table_out;
+    int32_t *tok_first;                 /* device [batch + 1] */
+    int32_t *tok_seq, *tok_slot;        /* device [n_tok] */
+    int32_t *status;                    /* device [2] */
+} kv_tables_args_t;
+int kv_step_tables(const kv_tables_args_t *args, void *hip_stream);
+
+/*
+ * Sequences that share a prefix.  Group g are sequences first[g] .. first[g + 1] - 1; tokens 0 .. prefix[g] - 1 of all of them are those of sequence first[g], in whose
+ * place in the cache alone they are read (the others' rows or blocks of them are not).  Every sequence of a group holds at least prefix[g] tokens of context.
+ * Sequences outside first[0] .. first[n_groups] - 1 share nothing.
+ */
+typedef struct kv_groups {
+    int32_t n_groups;
+    int32_t reserved;
+    const int32_t *first_host, *first_dev;   /* host, device [n_groups + 1], ascending, the same values */
+    const int32_t *prefix_host, *prefix_dev; /* host, device [n_groups], the same values */
+} kv_groups_t;
+
+/*
+ * What becomes of a score x = q . K * scale before the softmax, and what a new token sees.
+ *   softcap c > 0:  x -> c tanh(x / c)
+ *   slopes:         x -> x - slopes[hq] |p_t - p_j|, with positions: a token of the context is at position j, new token t at positions[t]
+ *   sees_from:      only tokens j >= sees_from[t] of the sequence are seen (a window, the start of a document)
+ *   sees_to:        tokens j < sees_to[t] are seen as well, new ones that the mask or chain leaves out included (a prefix whose tokens see each other both ways)
+ */
+typedef struct kv_scores {
+    float softcap;            /* 0 = none */
+    int32_t reserved;
+    const float *slopes;      /* device [H_q], nullable */
+    const int32_t *positions; /* device [n_tok]; with slopes */
+    const int32_t *sees_from; /* device [n_tok], nullable */
+    const int32_t *sees_to;   /* device [n_tok], nullable */
+} kv_scores_t;
+
+/*
+ * kv_group_attn -- attention of new tokens over one layer of a cache, as kv_tree_attn, for sequences that may share prefixes (groups, nullable) and scores that may be capped,
+ * biased or bounded (scores, nullable); without a mask a sequence may have any number of new tokens (a prompt, or a chunk of one): a chain.
+ * The K and V of a group's prefix are read once for all of its sequences' query rows, those of a sequence's own tokens once for it; workgroups whose rows see none of their tokens leave out
+ * what they would read.  args, types, layouts, formats and limits are kv_tree_attn's otherwise: head_dim 64, 128 or 256; with a mask at most KV_TREE_MAX new tokens per sequence.
+ * A row that sees nothing yields zeros.  workspace: at least kv_group_attn_workspace() bytes lets the library split as it likes; with less it splits less.
+ * Two calls that overlap in time need a workspace each.
+ */
+int kv_group_attn(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *args, const kv_groups_t *groups,
+                  const kv_scores_t *scores, void *workspace, size_t ws_bytes, void *hip_stream);
+/* Bytes of workspace with which kv_group_attn splits up to n_tok new tokens of the batch over contexts of up to max_len tokens as it likes. */
+size_t kv_group_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
+
+/*
+ * kv_sample -- the next token of every row of logits, from given random numbers.  With l = a row's logits, T its temperature, w_i = exp((l_i - max l) / T) and the
+ * tokens ordered by l from the largest down (equal ones by index), what is kept is the shortest of
+ *   the first top_k tokens (top_k <= 0: all);
+ *   the fewest first tokens whose sum of w is at least top_p times that of the first top_k (at least one; top_p >= 1: all);
+ *   those with w_i >= min_p (the largest always);
+ * and tokens[row] is the smallest index i with (sum of w_j over kept j <= i) > u * (sum over all kept).  probs[row] = w of it / sum over all kept.
+ * Not T > 0: the largest (the first of equal ones), probability 1.  Infinities of -1 are never drawn.  A row with a NaN or an infinity of +1, or without
+ * any finite logit, yields token -1 and probability 0.  u is taken as within [0, 1).
+ * Sums are of w held as integers, units of 2^-s with s = 62 - log2(n_vocab) rounded up (45 for 128K), so that they do not depend on an order; w is computed in double precision.
+ * workspace: device, 16-byte aligned, >= kv_sample_workspace() bytes (else KV_ENOSPC); nothing in it has to start at zero.
+ */
+#define KV_F32 2 /* logits only */
+typedef struct kv_sample_args {
+    const void *logits;       /* device [n_rows, n_vocab], a row's values side by side */
+    int64_t stride;           /* elements from row to row */
+    int32_t n_rows, n_vocab;
+    int32_t dtype;            /* KV_F16 | KV_BF16 | KV_F32 */
+    int32_t reserved;
+    const float *temperature; /* device [n_rows], nullable: 1 */
+    const int32_t *top_k;     /* device [n_rows], nullable: all */
+    const float *top_p;       /* device [n_rows], nullable: 1 */
+    const float *min_p;       /* device [n_rows], nullable: 0 */
+    const float *u;           /* device [n_rows] */
+    int32_t *tokens;          /* device [n_rows] */
+    float *probs;             /* device [n_rows], nullable */
+} kv_sample_args_t;
+int kv_sample(const kv_sample_args_t *args, void *workspace, size_t ws_bytes, void *hip_stream);
+size_t kv_sample_workspace(int n_rows, int n_vocab);
+
+/* ------------------------------------------------------------------------------------------ */
 int kv_last_hip_error(void);       /* hipError_t of the last KV_EHIP on this thread, else 0 */
 const char *kv_strerror(int code); /* static string */
 int kv_abi_version(void);
 /* sizeof of the ABI struct number `which` as this library was compiled (0 kv_plan_desc_t, 1 kv_plan_info_t,
  * 2 kv_extent_t, 3 kv_cmd_t, 4 kv_view_t, 5 kv_attn_args_t, 6 kv_pipe_opts_t, 7 kv_pipe_stats_t,
  * 8 kv_append_stats_t, 9 kv_adapt_t, 10 kv_chunk_trace_t, 11 kv_blocks_t, 12 kv_rope_t, 13 kv_rope_desc_t, 14 kv_rope_args_t,
- * 15 kv_write_args_t, 16 kv_read_args_t, 17 kv_tree_args_t; 0 for any other number): lets a binding verify its own
+ * 15 kv_write_args_t, 16 kv_read_args_t, 17 kv_tree_args_t, 18 kv_tables_args_t, 19 kv_groups_t, 20 kv_scores_t,
+ * 21 kv_sample_args_t; 0 for any other number): lets a binding verify its own
  * layouts. */
 size_t kv_abi_sizeof(int which);
 

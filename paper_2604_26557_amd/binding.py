@@ -16,7 +16,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("KVBLADE_LIB") or os.path.join(_PKG, "libkvblade.so")
 
 KV_OK, KV_EINVAL, KV_EALIGN, KV_ERANGE, KV_ENOSPC, KV_EHIP = 0, -1, -2, -3, -4, -5
-KV_F16, KV_BF16 = 0, 1
+KV_F16, KV_BF16, KV_F32 = 0, 1, 2
 KV_TOKEN_MAJOR, KV_PER_SEQ = 0, 1
 KV_PATH_DIRECT, KV_PATH_PAGECACHE = 0, 1
 KV_K, KV_V, KV_KV = 0, 1, 2
@@ -45,7 +45,7 @@ EXPORTS = [
     "kv_append_tokens", "kv_budget", "kv_plan_trim", "kv_adapt_init", "kv_adapt_order", "kv_adapt_update",
     "kv_abi_sizeof", "kv_budget_sample", "kv_decode_attn_static", "kv_offload_pack_layers", "kv_reload_unpack_layers",
     "kv_decode_attn_splits", "kv_rope_table", "kv_rope", "kv_cache_write", "kv_cache_read", "kv_tree_masks", "kv_tree_attn",
-    "kv_tree_attn_workspace",
+    "kv_tree_attn_workspace", "kv_step_tables", "kv_group_attn", "kv_group_attn_workspace", "kv_sample", "kv_sample_workspace",
 ]
 
 
@@ -166,6 +166,27 @@ class kv_tree_args_t(C.Structure):
                 ("n_splits", C.c_int32), ("scale", C.c_float)]
 
 
+class kv_tables_args_t(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "block_tokens", "max_blocks", "n_pool", "n_tok", "reserved")] + \
+               [(n, C.c_void_p) for n in ("seq_lens", "new_lens", "leader", "shared", "held", "n_free", "block_table", "free_ids", "held_out",
+                                          "n_free_out", "block_table_out", "tok_first", "tok_seq", "tok_slot", "status")]
+
+
+class kv_groups_t(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("reserved", C.c_int32), ("first_host", C.POINTER(C.c_int32)), ("first_dev", C.c_void_p),
+                ("prefix_host", C.POINTER(C.c_int32)), ("prefix_dev", C.c_void_p)]
+
+
+class kv_scores_t(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("reserved", C.c_int32), ("slopes", C.c_void_p), ("positions", C.c_void_p), ("sees_from", C.c_void_p),
+                ("sees_to", C.c_void_p)]
+
+
+class kv_sample_args_t(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("stride", C.c_int64), ("n_rows", C.c_int32), ("n_vocab", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "u", "tokens", "probs")]
+
+
 _lib = None
 
 
@@ -220,6 +241,13 @@ def lib() -> C.CDLL:
         L.kv_tree_attn.argtypes = [vp, vp, vp, i, C.POINTER(kv_tree_args_t), vp, C.c_size_t, vp]
         L.kv_tree_attn_workspace.argtypes = [vp, i, i]
         L.kv_tree_attn_workspace.restype = C.c_size_t
+        L.kv_step_tables.argtypes = [vp, vp]
+        L.kv_group_attn.argtypes = [vp, vp, vp, i, C.POINTER(kv_tree_args_t), vp, vp, vp, C.c_size_t, vp]
+        L.kv_group_attn_workspace.argtypes = [vp, i, i]
+        L.kv_group_attn_workspace.restype = C.c_size_t
+        L.kv_sample.argtypes = [C.POINTER(kv_sample_args_t), vp, C.c_size_t, vp]
+        L.kv_sample_workspace.argtypes = [i, i]
+        L.kv_sample_workspace.restype = C.c_size_t
         L.kv_strerror.restype = C.c_char_p
         L.kv_strerror.argtypes = [i]
         L.kv_abi_sizeof.argtypes = [i]
@@ -230,7 +258,8 @@ def lib() -> C.CDLL:
         for which, t in enumerate((kv_plan_desc_t, kv_plan_info_t, kv_extent_t, kv_cmd_t, kv_view_t, kv_attn_args_t,
                                    kv_pipe_opts_t, kv_pipe_stats_t, kv_append_stats_t, kv_adapt_t,
                                    kv_chunk_trace_t, kv_blocks_t, kv_rope_t, kv_rope_desc_t, kv_rope_args_t,
-                                   kv_write_args_t, kv_read_args_t, kv_tree_args_t)):
+                                   kv_write_args_t, kv_read_args_t, kv_tree_args_t, kv_tables_args_t, kv_groups_t, kv_scores_t,
+                                   kv_sample_args_t)):
             if L.kv_abi_sizeof(which) != C.sizeof(t):
                 raise RuntimeError(f"{t.__name__}: binding has {C.sizeof(t)} bytes, library {L.kv_abi_sizeof(which)}")
         _lib = L
@@ -655,6 +684,131 @@ def kv_tree_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, t
                                       workspace.nbytes, _caller_stream(stream))
     if rc:
         raise KVError(rc, "kv_tree_attn")
+
+
+# ------------------------------------------------------------------------------------------ a batch's step: tables, shared prefixes, sampling
+class StepTables:
+    """kv_tables_args_t plus the device tensors that it points to."""
+
+    def __init__(self, struct: kv_tables_args_t, keep):
+        self.struct, self._keep = struct, keep
+        self._ref = C.byref(struct)
+
+
+def _all_indices(where, *tensors) -> None:
+    """int32 tensors side by side, of at least so many numbers each."""
+    for t, n in tensors:
+        if t is not None and not _are_indices(t, n):
+            raise KVError(KV_EINVAL, where)
+
+
+def step_tables(block_tokens: int, seq_lens, new_lens, held, free_ids, n_free, block_table, tok_first, tok_seq, tok_slot, status, leader=None, shared=None,
+                held_out=None, n_free_out=None, block_table_out=None) -> StepTables:
+    """What kv_step_tables reads and writes, device int32 tensors all: seq_lens, new_lens, leader, shared, held [B], free_ids [pool], n_free [1], block_table [B, max_blocks],
+    tok_first [B + 1], tok_seq and tok_slot [rows], status [2].  Without held_out, n_free_out and block_table_out the step is written in place."""
+    b, rows = seq_lens.numel(), tok_seq.numel()
+    outs = (held_out, n_free_out, block_table_out)
+    if any(x is None for x in outs) != all(x is None for x in outs) or block_table.dim() != 2 or block_table.shape[0] != b or tok_slot.numel() != rows:
+        raise KVError(KV_EINVAL, "step_tables")
+    held_out, n_free_out, block_table_out = (y if x is None else x for x, y in zip(outs, (held, n_free, block_table)))
+    if block_table_out.shape != block_table.shape:
+        raise KVError(KV_EINVAL, "step_tables")
+    _all_indices("step_tables", (seq_lens, b), (new_lens, b), (leader, b), (shared, b), (held, b), (held_out, b), (n_free, 1), (n_free_out, 1), (block_table, 0),
+                 (block_table_out, 0), (free_ids, 0), (tok_first, b + 1), (tok_seq, 0), (tok_slot, 0), (status, 2))
+    p = [t.data_ptr() if t is not None else None for t in (seq_lens, new_lens, leader, shared, held, n_free, block_table, free_ids, held_out, n_free_out, block_table_out,
+                                                           tok_first, tok_seq, tok_slot, status)]
+    return StepTables(kv_tables_args_t(b, block_tokens, block_table.shape[1], free_ids.numel(), rows, 0, *p),
+                      (seq_lens, new_lens, leader, shared, held, n_free, block_table, free_ids, *outs, tok_first, tok_seq, tok_slot, status))
+
+
+def kv_step_tables(tables: StepTables, stream=None) -> None:
+    """Block tables and slot maps of a step from the lengths that the tensors hold now."""
+    rc = (_lib or lib()).kv_step_tables(tables._ref, _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_step_tables")
+
+
+class Groups:
+    """kv_groups_t plus what it points to."""
+
+    def __init__(self, struct: kv_groups_t, keep):
+        self.struct, self._keep = struct, keep
+        self._ref = C.byref(struct)
+
+
+def prefix_groups(first: Sequence[int], first_dev, prefix: Sequence[int], prefix_dev) -> Groups:
+    """Sequences first[g] .. first[g + 1] - 1 share prefix[g] tokens, which lie in the first one's place of the cache.  first [n + 1] and prefix [n] (host), and the same as
+    device int32 tensors."""
+    n = len(prefix)
+    if len(first) != n + 1 or not _are_indices(first_dev, n + 1) or not _are_indices(prefix_dev, n):
+        raise KVError(KV_EINVAL, "prefix_groups")
+    f, p = (C.c_int32 * (n + 1))(*[int(x) for x in first]), (C.c_int32 * max(1, n))(*[int(x) for x in prefix])
+    return Groups(kv_groups_t(n, 0, f, first_dev.data_ptr(), p, prefix_dev.data_ptr()), (f, p, first_dev, prefix_dev))
+
+
+class Scores:
+    """kv_scores_t plus the device tensors that it points to."""
+
+    def __init__(self, struct: kv_scores_t, keep, n_heads, n_tok):
+        self.struct, self._keep, self.n_heads, self.n_tok = struct, keep, n_heads, n_tok
+        self._ref = C.byref(struct)
+
+
+def scores(softcap: float = 0.0, slopes=None, positions=None, sees_from=None, sees_to=None) -> Scores:
+    """softcap c: c tanh(x / c); slopes (device float32 [H_q]): x - slope * distance, between positions (device int32 [n_tok]) of new tokens; sees_from, sees_to (device int32
+    [n_tok]): the first token that is seen, and up to which the others are in any case."""
+    import torch
+    rows = [t for t in (positions, sees_from, sees_to) if t is not None]
+    if (slopes is not None and (slopes.dtype != torch.float32 or slopes.dim() != 1 or not slopes.is_contiguous())) or any(not _are_indices(t, 0) for t in rows):
+        raise KVError(KV_EINVAL, "scores")
+    ptr = [t.data_ptr() if t is not None else None for t in (slopes, positions, sees_from, sees_to)]
+    return Scores(kv_scores_t(softcap, 0, *ptr), (slopes, positions, sees_from, sees_to), slopes.numel() if slopes is not None else None,
+                  min([t.numel() for t in rows], default=None))
+
+
+def kv_group_attn_workspace(plan: Plan, n_tok: int, max_len: int) -> int:
+    return int(lib().kv_group_attn_workspace(plan.handle, n_tok, max_len))
+
+
+def kv_group_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tree: TreeBatch, q, out, out_dtype: int, n_splits: int, workspace,
+                  groups: Optional[Groups] = None, scores: Optional[Scores] = None, scale: float = 0.0, stream=None) -> None:
+    """kv_tree_attn for sequences that share prefixes (groups) and scores that are capped, biased or bounded (scores), and for prompts.  q, out: [n_tok, H_q, D], last dim
+    contiguous; q of the plan's dtype, out of that or fp32 (out_dtype)."""
+    (n, hq, d), (qt, qh, qd), (ot, oh, od), shape = q.shape, q.stride(), out.stride(), plan.shape
+    if qd != 1 or od != 1 or n < tree.n_tok or hq != shape[1] or d != shape[2] or q.dtype != shape[3] or out.shape != q.shape \
+            or len(tree.first) != shape[4] or out.dtype != shape[5 if out_dtype == KV_OUT_F32 else 3]:
+        raise KVError(KV_EINVAL, "kv_group_attn")
+    if scores is not None and ((scores.n_heads is not None and scores.n_heads != hq) or (scores.n_tok is not None and scores.n_tok < tree.n_tok)):
+        raise KVError(KV_EINVAL, "kv_group_attn")
+    a = kv_tree_args_t(q.data_ptr(), out.data_ptr(), qt, qh, ot, oh, *tree._fixed, out_dtype, n_splits, scale)
+    rc = (_lib or lib()).kv_group_attn(plan.handle, view._ref, blocks._ref if blocks is not None else None, layer, C.byref(a), groups._ref if groups is not None else None,
+                                       scores._ref if scores is not None else None, workspace.data_ptr(), workspace.nbytes, _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_group_attn")
+
+
+_logit_dtypes = {}   # torch dtype -> KV_F16 | KV_BF16 | KV_F32, once torch is imported
+
+
+def kv_sample_workspace(n_rows: int, n_vocab: int) -> int:
+    return int(lib().kv_sample_workspace(n_rows, n_vocab))
+
+
+def kv_sample(logits, u, tokens, workspace, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, stream=None) -> None:
+    """logits: [rows, vocabulary] fp16, bf16 or fp32, last dim contiguous; temperature, top_p, min_p, u, probs: device float32 [rows]; top_k, tokens: device int32 [rows]."""
+    if not _logit_dtypes:
+        import torch
+        _logit_dtypes.update({torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float32: KV_F32})
+    (n, v), (st, sv), d = logits.shape, logits.stride(), _logit_dtypes.get(logits.dtype)
+    if d is None or (sv != 1 and v > 1) or not _are_indices(tokens, n) or (top_k is not None and not _are_indices(top_k, n)):
+        raise KVError(KV_EINVAL, "kv_sample")
+    for t in (u, temperature, top_p, min_p, probs):
+        if t is not None and (_logit_dtypes.get(t.dtype) != KV_F32 or t.numel() < n or not t.is_contiguous()):
+            raise KVError(KV_EINVAL, "kv_sample")
+    a = kv_sample_args_t(logits.data_ptr(), st, n, v, d, 0, *[t.data_ptr() if t is not None else None for t in (temperature, top_k, top_p, min_p, u, tokens, probs)])
+    rc = (_lib or lib()).kv_sample(C.byref(a), workspace.data_ptr(), workspace.nbytes, _caller_stream(stream))
+    if rc:
+        raise KVError(rc, "kv_sample")
 
 
 # ------------------------------------------------------------------------------------------ pipeline

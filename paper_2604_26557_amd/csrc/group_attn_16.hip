@@ -1,0 +1,3 @@
+#include "tree_attn.hpp"
+
+kvb::GroupKernel kvb::group_kernel_16(int D, bool bf16, bool f32, int nb) { return TreeKernelOf<true>::choose<KV_FORMAT_16>(D, bf16, f32, nb); }

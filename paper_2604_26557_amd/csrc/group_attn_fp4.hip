@@ -1,0 +1,3 @@
+#include "tree_attn.hpp"
+
+kvb::GroupKernel kvb::group_kernel_fp4(int D, bool bf16, bool f32, int nb) { return TreeKernelOf<true>::choose<KV_FORMAT_FP4>(D, bf16, f32, nb); }

@@ -453,6 +453,10 @@ extern "C" size_t kv_abi_sizeof(int which)
     case 15: return sizeof(kv_write_args_t);
     case 16: return sizeof(kv_read_args_t);
     case 17: return sizeof(kv_tree_args_t);
+    case 18: return sizeof(kv_tables_args_t);
+    case 19: return sizeof(kv_groups_t);
+    case 20: return sizeof(kv_scores_t);
+    case 21: return sizeof(kv_sample_args_t);
     default: return 0;
     }
 }

@@ -27,6 +27,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -53,6 +54,19 @@ struct TreeParams {
     int ragged;                        // at most 64 sequences, of which some have fewer splits or row blocks than others
     int dense;                         // rows of a head lie side by side
     int grouped;                       // rows of context are looked up by groups of 16
+};
+
+// What kv_group_attn has beside that. A unit of work is a group's prefix (all new tokens of its sequences over the prefix, in its first sequence's place) or a sequence (its new tokens over its
+// own tokens); partial results of a row are those of its prefix' splits, then those of its own.
+struct GroupParams : TreeParams {
+    const int *group_first, *prefix;   // [n_groups + 1], [n_groups]
+    int n_groups, prefix_ns;           // partial results of a row that are of its prefix
+    int prefix_tokens;                 // of a split of a prefix, a multiple of 32
+    unsigned by_prefix;
+    int shaped;                        // scores are capped or biased: the softmax takes them as they are then, scale_log2e = log2(e)
+    float scale, cap, cap_in;          // cap 0: none; cap_in = scale / cap
+    const float *slopes;
+    const int *positions, *from, *to;
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -276,15 +290,16 @@ __device__ __forceinline__ int token_of(const TreeParams &p, int r) { return p.G
 
 // The kernel's arguments, loaded where they are needed: what is only used now and then, or after the loop, takes no scalar registers in it (there are too few: the
 // others would be kept in lanes of a vector register and fetched from there at each step: when this was changed, 4 sequences of 8K x 16 heads x 256 of 8 bits went from 51.8 to 49.0 us).
-__device__ __forceinline__ TreeParams arguments()
+template <typename P>
+__device__ __forceinline__ P arguments()
 {
 #if __HIP_DEVICE_COMPILE__
-    typedef const __attribute__((address_space(4))) TreeParams *Args;
+    typedef const __attribute__((address_space(4))) P *Args;
     unsigned long long at = (unsigned long long)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(at));
     return *(Args)at;
 #else
-    return TreeParams{};   // the host's pass over this file knows no such address
+    return P{};   // the host's pass over this file knows no such address
 #endif
 }
 
@@ -299,6 +314,49 @@ __device__ __forceinline__ bool row_sees(const TreeParams &p, int first, int r, 
     const int t = token_of(p, r), i = j - len;
     if (!p.mask) return i <= t;
     return (bool)(p.mask[(long long)(first + t) * p.words + (i >> 6)] >> (i & 63) & 1);
+}
+
+// tanh of |y| <= 8.5, to 3e-7 of its value: y P(y^2) / Q(y^2), fitted by least squares of the relative error, reweighted until it was even (2^-24.8 before rounding). Through exponentials it takes as
+// long, and near zero loses what a cap multiplies again.
+__device__ __forceinline__ float tanh_within(float y)
+{
+    const float z = y * y;
+    const float num = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.072381503e-11f, -1.371888647e-08f), 9.573725038e-06f), 2.953875810e-03f), 1.294988990e-01f), 9.999999404e-01f);
+    const float den = fmaf(z, fmaf(z, fmaf(z, 2.327029943e-04f, 2.389829233e-02f), 4.628319144e-01f), 1.f);
+    return y * num * __builtin_amdgcn_rcpf(den);
+}
+// Beyond, tanh is 1 in 32 bits. A NaN stays one.
+__device__ __forceinline__ float tanh_of(float y) { return tanh_within(fabsf(y) > 8.5f ? copysignf(8.5f, y) : y); }
+// The same for what is finite; anything else becomes a NaN (one instruction instead of three).
+__device__ __forceinline__ float tanh_of_finite(float y) { return fmaf(y, 0.f, tanh_within(__builtin_amdgcn_fmed3f(y, -8.5f, 8.5f))); }
+
+// Query rows of a unit of kv_group_attn: which of 32 tokens from j on row r sees, as bits. Tokens before `begin` are another unit's; from len on they are new ones.
+struct GroupRows {
+    int first, tokens, begin, len, total;   // the rows' tokens; where the unit's tokens begin, the new ones begin, and they end
+};
+__device__ __forceinline__ unsigned group_sees32(const GroupParams &p, const GroupRows &u, int r, int j)
+{
+    auto below = [](int x) { return x >= 32 ? ~0u : (1u << max(x, 0)) - 1u; };
+    const int t = min((int)quotient((unsigned)r, (unsigned)p.G, p.by_g), u.tokens - 1), at = u.first + t;
+    unsigned seen = below(u.len - j);
+    const unsigned drafted = below(u.total - j) & ~seen;
+    if (drafted != 0) {
+        const int i = j - u.len;   // > -32
+        unsigned bits;
+        if (!p.mask) {
+            bits = below(t + 1 - i);
+        } else {
+            const unsigned long long *const row = p.mask + (long long)at * p.words;
+            const int w = max(i, 0) >> 6, shift = max(i, 0) & 63;
+            unsigned long long x = w < p.words ? row[w] >> shift : 0;
+            if (shift > 32 && w + 1 < p.words) x |= row[w + 1] << (64 - shift);
+            if (i < 0) x <<= -i;
+            bits = (unsigned)x;
+        }
+        if (p.to) bits |= below(max(p.to[at], 0) - j);
+        seen |= drafted & bits;
+    }
+    return seen & ~below(max(u.begin, p.from ? p.from[at] : 0) - j);
 }
 
 // The same of 32 tokens from j on, as bits.
@@ -323,13 +381,12 @@ __device__ __forceinline__ unsigned row_sees32(const TreeParams &p, int first, i
 
 // Four columns of a query row's sums: the result, or the partial result of a split.
 template <int D>
-__device__ __forceinline__ void store_sums(const TreeParams &p, unsigned h, int first, int r, unsigned split, int d, f32x4 x, float ref, float l)
+__device__ __forceinline__ void store_sums(const TreeParams &p, int token, int hq, unsigned split, int d, f32x4 x, float ref, float l)
 {
-    const int t = token_of(p, r), hq = (int)h * p.G + r - t * p.G;
     if (p.ns == 1) {
-        store_four(p.out, (first + t) * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
+        store_four(p.out, token * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
     } else {
-        const long long at = ((long long)(first + t) * (p.H * p.G) + hq) * p.ns + split;
+        const long long at = ((long long)token * (p.H * p.G) + hq) * p.ns + split;
         *(f32x4 *)&p.part_acc[at * D + d] = x;
         if (d == 0) *(f32x2 *)&p.part_ml[at * 2] = f32x2{ref, l};
     }
@@ -337,11 +394,12 @@ __device__ __forceinline__ void store_sums(const TreeParams &p, unsigned h, int 
 
 // One query row over a split on the vector ALU, a token at a time: its largest score, then its sums.  Whatever the cache holds, nothing but what the row sees
 // enters them.  A lane has four columns (of which several lanes may have the same).
-template <int D, bool BF16, int FORMAT>
-__device__ __forceinline__ void plain_row(const TreeParams &p, const int *table, unsigned long long base, unsigned long long zbase, unsigned h, int first, int r,
-                                       int len, int total, int s0, int s1, unsigned split, int lane)
+// sees(j): does it see token j; shaped(x, j): its score times log2(e), from its product with K.
+template <int D, bool BF16, int FORMAT, typename Sees, typename Shaped>
+__device__ __forceinline__ void plain_row(const TreeParams &p, const int *table, unsigned long long base, unsigned long long zbase, unsigned h, int first, int r, int t,
+                                       int s0, int s1, unsigned split, int lane, const Sees &sees, const Shaped &shaped)
 {
-    const int t = token_of(p, r), hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
+    const int hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
     const u32x2 qw = *(const u32x2 *)(p.q + 2 * ((first + t) * p.q_st + hq * p.q_sh + 4 * at));
     const f32x2 q0 = unpack2<BF16>(qw[0] ^ p.q_sign), q1 = unpack2<BF16>(qw[1] ^ p.q_sign);
     auto row = [&](const char *rows, const char *scales, int j, bool *there) {
@@ -366,14 +424,14 @@ __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table,
         float s = fmaf(q0[0], k[0], fmaf(q0[1], k[1], fmaf(q1[0], k[2], q1[1] * k[3])));
 #pragma unroll
         for (int o = 1; o < D / 4; o *= 2) s += __shfl_xor(s, o);
-        return there ? s * p.scale_log2e : -INFINITY;
+        return there ? shaped(s, j) : -INFINITY;
     };
     float top = -INFINITY, l = 0.f;
     for (int j = s0; j < s1; ++j)
-        if (row_sees(p, first, r, j, len, total)) top = fmaxf(top, score(j));
+        if (sees(j)) top = fmaxf(top, score(j));
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     for (int j = s0; j < s1; ++j) {
-        if (!row_sees(p, first, r, j, len, total)) continue;
+        if (!sees(j)) continue;
         const float s = score(j);
         if (s == -INFINITY) continue;
         const float w = __builtin_amdgcn_exp2f(s - top);
@@ -384,12 +442,14 @@ __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table,
         for (int k = 0; k < 4; ++k)   // a probability too small for 32 bits still counts against an infinity
             x[k] = fmaf(w == 0.f && !__builtin_isfinite(v[k]) ? 1.0e-37f : w, v[k], x[k]);
     }
-    if (lane < D / 4) store_sums<D>(p, h, first, r, split, 4 * at, x, top == -INFINITY ? kNoScore : top, l);
+    if (lane < D / 4) store_sums<D>(p, first + t, hq, split, 4 * at, x, top == -INFINITY ? kNoScore : top, l);
 }
 
-template <int D, bool BF16, int FORMAT, int NB, bool F32>
-__global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1)) kv_tree_partial_kernel(TreeParams p)
+template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
+__global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1))
+    kv_tree_partial_kernel(typename std::conditional<GROUP, GroupParams, TreeParams>::type p)
 {
+    using P = typename std::conditional<GROUP, GroupParams, TreeParams>::type;
     using T = TreeTile<D, FORMAT, NB>;
     constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = kParts<BF16, F32>, kWaves = T::kWaves, kStages = T::kStages;
     constexpr bool kNT = NB <= 2;   // with more rows other workgroups may read the same K and V out of L2
@@ -402,7 +462,80 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     unsigned b, h, split, rb = 0;
     int first, drafted, len;
-    if (p.ragged) {
+    [[maybe_unused]] int begin = 0, end_of_rows = 0;   // of the unit's tokens; past the last that a row of this workgroup sees
+    [[maybe_unused]] unsigned slot = 0;                // of the first split's partial result
+    if constexpr (GROUP) {
+        // Units, a lane each: groups, then sequences by 64. What a group's lane knows of it is asked for by the sequences' lanes.
+        unsigned at = blockIdx.x;
+        int group_first = 0, group_end = 0, shared = 0;
+        if (lane < p.n_groups) {
+            group_first = p.group_first[lane];
+            group_end = p.group_first[lane + 1];
+            shared = p.prefix[lane];
+        }
+        bool found = false;
+        for (int b0 = p.n_groups > 0 ? -1 : 0; b0 < p.B; b0 = b0 < 0 ? 0 : b0 + 64) {
+            const bool is_group = b0 < 0;
+            int f = 0, n = 0, l = 0, from = 0, kb = 0;   // first token, their number, context, where the unit's tokens begin, sequence in whose place they are
+            if (is_group) {
+                if (lane < p.n_groups && shared > 0) {
+                    f = p.tok_first[group_first];
+                    n = p.tok_first[group_end] - f;
+                    l = shared;
+                    kb = group_first;
+                }
+            } else {
+                kb = b0 + lane;
+                for (int g = 0; g < p.n_groups; ++g) {
+                    const int x = __builtin_amdgcn_readlane(group_first, g), y = __builtin_amdgcn_readlane(group_end, g), z = __builtin_amdgcn_readlane(shared, g);
+                    from = kb >= x && kb < y ? z : from;
+                }
+                if (kb < p.B) {
+                    f = p.tok_first[kb];
+                    n = p.tok_first[kb + 1] - f;
+                    l = max(from, min(p.seq_lens[kb], p.max_total - n));
+                }
+            }
+            const int st = is_group ? p.prefix_tokens : p.split_tokens;
+            unsigned units = 0;
+            if (n > 0) {
+                const int span = is_group ? l : l + n - (from & ~31);
+                units = (quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1) * (unsigned)p.H;
+                if (n * (long long)p.G > kRows) units = (units + 7) & ~7u;
+            }
+            const unsigned all = units * (unsigned)(((long long)n * p.G + kRows - 1) / kRows);
+            unsigned end = all;
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
+            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
+            const int which = __popcll(__ballot(end <= at));
+            if (which >= 64) {
+                at -= (unsigned)__builtin_amdgcn_readlane((int)end, 63);
+                continue;
+            }
+            first = __builtin_amdgcn_readlane(f, which);
+            drafted = __builtin_amdgcn_readlane(n, which);
+            len = __builtin_amdgcn_readlane(l, which);
+            begin = __builtin_amdgcn_readlane(from, which);
+            b = (unsigned)__builtin_amdgcn_readlane(kb, which);
+            units = (unsigned)__builtin_amdgcn_readlane((int)units, which);
+            unsigned unit = at - (unsigned)__builtin_amdgcn_readlane((int)(end - all), which);
+            if (unit >= units) {
+                rb = unit / units;
+                unit -= rb * units;
+            }
+            split = quotient(unit, (unsigned)p.H, p.by_h);
+            h = unit - split * (unsigned)p.H;
+            slot = is_group ? 0 : (unsigned)p.prefix_ns;
+            end_of_rows = is_group ? len : len + drafted;
+            found = true;
+            break;
+        }
+        if (!found) return;
+    } else if (p.ragged) {
         // Only what there is, sequence after sequence (a lane each): workgroups that have nothing to do would take places from others, which then share a compute unit
         // while the next one is idle.
         int f = 0, n = 0, l = 0;
@@ -455,9 +588,47 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     }
     const int n_rows = drafted * p.G - (int)rb * kRows;   // of this block: the first kRows of them
     if (n_rows <= 0) return;
-    const int total = len + drafted;
-    if (!split_has_tokens(split, p.split_tokens, total)) return;
-    const int s0 = (int)split * p.split_tokens, s1 = min(s0 + p.split_tokens, total);
+    const int total = GROUP ? end_of_rows : len + drafted;
+    int s0, s1;
+    [[maybe_unused]] int from_most = begin, pos_least = INT_MAX, origin = len;   // all rows see what is between from_most and the context's end; none of their positions is below pos_least
+    [[maybe_unused]] bool by_row = false;   // positions too far from one origin for 32 bits
+    if constexpr (GROUP) {
+        const int st = total == len ? p.prefix_tokens : p.split_tokens, start = begin & ~31;
+        if (!split_has_tokens(split, st, total - start)) return;
+        s0 = start + (int)split * st;
+        s1 = min(s0 + st, total);
+        int from_least = begin;
+        if (total > len && !p.mask) end_of_rows = len + 1 + (int)quotient((unsigned)((int)rb * kRows + min(n_rows, kRows) - 1), (unsigned)p.G, p.by_g);
+        if (p.from || p.to || p.slopes) {
+            const int r = (int)rb * kRows + min(lane, min(n_rows, kRows) - 1), t = first + (int)quotient((unsigned)r, (unsigned)p.G, p.by_g);
+            int lo = max(begin, p.from ? p.from[t] : 0), most = lo, up = p.to ? p.to[t] : 0, least = p.slopes ? p.positions[t] : 0, far = least;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                lo = min(lo, __shfl_xor(lo, o));
+                most = max(most, __shfl_xor(most, o));
+                up = max(up, __shfl_xor(up, o));
+                least = min(least, __shfl_xor(least, o));
+                far = max(far, __shfl_xor(far, o));
+            }
+            from_least = __builtin_amdgcn_readfirstlane(lo);
+            from_most = __builtin_amdgcn_readfirstlane(most);
+            if (total > len) end_of_rows = max(end_of_rows, min(__builtin_amdgcn_readfirstlane(up), total));
+            if (p.slopes) {
+                pos_least = __builtin_amdgcn_readfirstlane(least);
+                if (total > len) origin = __builtin_amdgcn_readfirstlane(far);
+                by_row = total > len ? (long long)origin - pos_least > 1024 : pos_least < len;
+                if (by_row) pos_least = INT_MIN;
+            }
+        }
+        // tokens that none of the rows sees are left out
+        s1 = min(s1, end_of_rows);
+        s0 = max(s0, min(from_least & ~31, s1 & ~31));
+        s1 = max(s0, s1);
+    } else {
+        if (!split_has_tokens(split, p.split_tokens, total)) return;
+        s0 = (int)split * p.split_tokens;
+        s1 = min(s0 + p.split_tokens, total);
+    }
 
     const int n = lane & 15, group = lane >> 4;
     const unsigned long long base = p.c.table ? h * p.c.sh : b * p.c.sb + h * p.c.sh;
@@ -482,11 +653,12 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     bool groups = false;
     auto where = [&](int m) {   // this wavefront's m-th step; called for each in turn
         const int j0 = s0 + 32 * (wave + m * kWaves), left = total - 1 - j0;
-        groups = p.grouped && left >= 31;
+        const int lowest = GROUP ? max(0, begin - j0) : 0;   // before it rows are another sequence's
+        groups = p.grouped && left >= 31 && lowest == 0;
         next_there = ~0u;
         if (!p.grouped) {
-            const CacheAddr c = arguments().c;
-            const RowAt r = row_at(c, table, base, zbase, j0 + min(lane & 31, left));
+            const CacheAddr c = arguments<P>().c;
+            const RowAt r = row_at(c, table, base, zbase, j0 + max(min(lane & 31, left), lowest));
             lane_at = r.at;
             lane_z = r.z;
             next_there = (unsigned)__ballot(r.there);
@@ -502,7 +674,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             }
         } else {
             if (m % 32 == 0) {   // the starts of 32 steps at a time, a lane each
-                const TreeParams p = arguments();
+                const P p = arguments<P>();
                 const int j = min(j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1) & ~15, at = p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt;
                 unsigned id = (unsigned)table[at];
                 const unsigned in = j - at * p.c.bt;
@@ -526,7 +698,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             next_there = both == 3 ? ~0u : both == 2 ? 0xffff0000u : both == 1 ? 0xffffu : 0;
         }
         if (!groups) {
-            const int t = min(lane & 31, left);
+            const int t = max(min(lane & 31, left), lowest);
             lane_at = (t & 16 ? at1 : at0) + (unsigned)(t & 15) * (unsigned)p.c.ss;
             lane_z = (t & 16 ? z1 : z0) + (unsigned)(t & 15) * (unsigned)p.c.zs;
         }
@@ -588,7 +760,10 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 
     // Query rows: token-major, the G heads of a token side by side.  Those past the last one are copies of it, whose results go nowhere.  They go to LDS ahead of the steps'
     // K and V: loaded into registers behind these, they were there only when all of these were (when this was changed: 4K tokens, 16 drafted 15.0 -> 14.3 us; 48 single tokens 22.7 -> 21.6).
-    auto row_token = [&](int r) { return token_of(p, (int)rb * kRows + r); };
+    auto row_token = [&](int r) {
+        if constexpr (GROUP) return (int)quotient((unsigned)((int)rb * kRows + r), (unsigned)p.G, p.by_g);
+        else return token_of(p, (int)rb * kRows + r);
+    };
     const u32x4 *const q_lds = (const u32x4 *)(lds + T::kRing);
     auto issue_q = [&] {   // a wavefront's share of them to LDS
         const unsigned to = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char *)lds + T::kRing;
@@ -599,6 +774,18 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             if (i < NB * kSteps) load_to_lds<16, false>(p.q + 2 * ((first + t) * p.q_st + ((int)h * p.G + g) * p.q_sh + T::q_at(s, group)), to + i * 1024);
         }
     };
+    [[maybe_unused]] float slope[NB];
+    if constexpr (GROUP) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            slope[nb] = 0.f;
+            if (p.slopes) {
+                const int r = min(nb * 16 + n, n_rows - 1);
+                slope[nb] = p.slopes[(int)h * p.G + (int)rb * kRows + r - row_token(r) * p.G];
+                asm volatile("" : "+v"(slope[nb]));   // here now: a wait for it in the loop would be one for the loads ahead
+            }
+        }
+    }
     u32x4 q_reg[T::kQStays ? 1 : NB][kSteps];
     f32x4 acc[NB][kColumns], sum[NB];
     float ref[NB];
@@ -794,7 +981,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     // A negative scale turns q's signs here: references and masks are those of a positive one.
-    if (const unsigned sign = arguments().q_sign; sign != 0) {
+    if (const unsigned sign = arguments<P>().q_sign; sign != 0) {
 #pragma unroll
         for (int k = 0; k < T::kQIssues; ++k) {
             const int i = wave + k * kWaves;
@@ -808,6 +995,41 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) q_reg[nb][s] = q_lds[(nb * kSteps + s) * 64 + lane];
     }
+
+    // Scores of kv_group_attn that are capped or biased. A bias is slope * (min(j, 2 pos - j) - origin): for one row that is -slope |pos - j| and a number that the softmax does not see, and as long as
+    // no token lies behind a row's position, slope * (j - origin), of which a lane needs the slope alone. Where the rows' positions are far apart each has its own for an origin.
+    [[maybe_unused]] auto shape = [&](f32x4 (&s)[NB][2], int j0) {
+        if constexpr (GROUP) {
+            const GroupParams p = arguments<P>();
+            if (p.cap > 0.f) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = p.cap * tanh_of_finite(s[nb][j / 4][j % 4] * p.cap_in);
+            } else {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][0] *= p.scale, s[nb][1] *= p.scale;
+            }
+            if (!p.slopes) return;
+            if (j0 + 31 <= pos_least && j0 + 32 <= len) {
+                const float at = (float)(j0 + group - origin);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope[nb], at + (float)(4 * j), s[nb][j / 4][j % 4]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int k = j0 + here(group) + 4 * j, kp = k < len ? k : p.positions[first + min(k - len, drafted - 1)];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const int pos = p.positions[first + row_token(min(nb * 16 + n, n_rows - 1))];
+                        s[nb][j / 4][j % 4] = fmaf(slope[nb], (float)(min((long long)kp, 2ll * pos - kp) - (by_row ? pos : origin)), s[nb][j / 4][j % 4]);
+                    }
+                }
+            }
+        }
+    };
 
 #pragma unroll 1
     for (int m = 0; m < mine; ++m) {
@@ -828,13 +1050,19 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             scores(k, s);
             if constexpr (kFirstK) __builtin_amdgcn_s_setprio(0);
         }
-        if (j0 + 32 > len || there[0] != ~0u) {
+        if constexpr (GROUP) {
+            if (p.shaped) shape(s, j0);
+        }
+        if (j0 + 32 > len || there[0] != ~0u || (GROUP && j0 < from_most)) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
-            const TreeParams p = arguments();
+            const P p = arguments<P>();
             const int row = (int)rb * kRows + here(n);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const unsigned seen = (there[0] & row_sees32(p, first, row + nb * 16, j0, len, total)) >> group;
+                unsigned seen;
+                if constexpr (GROUP) seen = there[0] & group_sees32(p, GroupRows{first, drafted, begin, len, total}, row + nb * 16, j0);
+                else seen = there[0] & row_sees32(p, first, row + nb * 16, j0, len, total);
+                seen >>= group;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = seen >> 4 * j & 1 ? s[nb][j / 4][j % 4] : -INFINITY;
             }
@@ -891,7 +1119,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
 
     // Merge: the wavefronts' references and sums become factors of their accumulators; these are added by halves: a wavefront gives the one that is not in its keeping to
     // another and gets that one's half of what is, twice.  In the end each has a quarter of the sums of all four.
-    const TreeParams a = arguments();
+    const P a = arguments<P>();
     static_assert(kWaves == 4 && NB * kColumns % 4 == 0, "halves of halves");
     constexpr int kTiles = NB * kColumns;
     f32x4 *const give = (f32x4 *)lds;                                                                // [kWaves][kTiles / 2][64]
@@ -909,8 +1137,24 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     if (lane == 0) bad_lds[wave] = wave_bad ? 1.f : 0.f;
     __syncthreads();
     if ((bad_lds[0] + bad_lds[1]) + (bad_lds[2] + bad_lds[3]) != 0.f) {
-        for (int r = wave; r < min(n_rows, kRows); r += kWaves)
-            plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, (int)rb * kRows + r, len, total, s0, s1, split, lane);
+        for (int i = wave; i < min(n_rows, kRows); i += kWaves) {
+            const int r = (int)rb * kRows + i, t = row_token(i);
+            if constexpr (GROUP) {
+                const GroupRows u{first, drafted, begin, len, total};
+                const float bias = a.slopes ? a.slopes[(int)h * a.G + r - t * a.G] : 0.f;
+                const int pos = a.slopes ? a.positions[first + t] : 0;
+                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, r, j) & 1); },
+                                           [&](float x, int j) {
+                                               if (!a.shaped) return x * a.scale_log2e;
+                                               x = a.cap > 0.f ? a.cap * tanh_of(x * a.cap_in) : x * a.scale;
+                                               if (a.slopes) x -= bias * fabsf((float)((long long)pos - (j < len ? j : a.positions[first + j - len])));
+                                               return x * a.scale_log2e;
+                                           });
+            } else {
+                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, split, lane, [&](int j) { return row_sees(a, first, r, j, len, total); },
+                                           [&](float x, int) { return x * a.scale_log2e; });
+            }
+        }
         return;
     }
     float to[NB], total_sum[NB];
@@ -957,14 +1201,17 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     static_assert(kColumns % kShare == 0, "of one row group");
     const int nb = kShare * wave / kColumns, c0 = kShare * wave % kColumns, r = nb * 16 + n;
     if (r >= n_rows) return;
-    const int t = token_of(a, (int)rb * kRows + r), hq = (int)h * a.G + (int)rb * kRows + r - t * a.G;
-    const long long part = ((long long)(first + t) * (a.H * a.G) + hq) * a.ns + split, at = a.ns == 1 ? (first + t) * a.o_st + hq * a.o_sh : part * D;
+    const int t = row_token(r), hq = (int)h * a.G + (int)rb * kRows + r - t * a.G;
+    const long long part = ((long long)(first + t) * (a.H * a.G) + hq) * a.ns + (GROUP ? slot + split : split), at = a.ns == 1 ? (first + t) * a.o_st + hq * a.o_sh : part * D;
     if (a.ns > 1 && group == 0 && c0 == 0) {
         float ml[2] = {to[0], total_sum[0]};
 #pragma unroll
         for (int k = 1; k < NB; ++k) {
             ml[0] = k == nb ? to[k] : ml[0];
             ml[1] = k == nb ? total_sum[k] : ml[1];
+        }
+        if constexpr (GROUP) {   // as if biased by its distances themselves
+            if (a.slopes && !by_row) ml[0] -= a.slopes[hq] * (float)((long long)a.positions[first + t] - origin) * a.scale_log2e;
         }
         *(f32x2 *)&a.part_ml[part * 2] = f32x2{ml[0] - kLiftLog2<BF16>, ml[1]};
     }
@@ -979,23 +1226,31 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     }
 }
 
-typedef void (*TreeKernel)(TreeParams);
-template <int FORMAT, int D, int NB>
-TreeKernel tree_kernel_of(bool bf16, bool f32)
-{
-    return !bf16 ? kv_tree_partial_kernel<D, false, FORMAT, NB, false> : f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true> : kv_tree_partial_kernel<D, true, FORMAT, NB, false>;
-}
-template <int FORMAT>
-TreeKernel tree_kernel_for(int D, bool bf16, bool f32, int nb)
-{
-    if (D == 256) return nb == 1 ? tree_kernel_of<FORMAT, 256, 1>(bf16, f32) : tree_kernel_of<FORMAT, 256, 2>(bf16, f32);
-    if (D == 128)
-        return nb == 1 ? tree_kernel_of<FORMAT, 128, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, 128, 2>(bf16, f32) : tree_kernel_of<FORMAT, 128, 4>(bf16, f32);
-    return nb == 1 ? tree_kernel_of<FORMAT, 64, 1>(bf16, f32) : nb == 2 ? tree_kernel_of<FORMAT, 64, 2>(bf16, f32) : tree_kernel_of<FORMAT, 64, 4>(bf16, f32);
-}
+template <bool GROUP>
+struct TreeKernelOf {
+    typedef void (*Kernel)(typename std::conditional<GROUP, GroupParams, TreeParams>::type);
+    template <int FORMAT, int D, int NB>
+    static Kernel of(bool bf16, bool f32)
+    {
+        return !bf16 ? kv_tree_partial_kernel<D, false, FORMAT, NB, false, GROUP>
+                     : f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true, GROUP> : kv_tree_partial_kernel<D, true, FORMAT, NB, false, GROUP>;
+    }
+    template <int FORMAT>
+    static Kernel choose(int D, bool bf16, bool f32, int nb)
+    {
+        if (D == 256) return nb == 1 ? of<FORMAT, 256, 1>(bf16, f32) : of<FORMAT, 256, 2>(bf16, f32);
+        if (D == 128) return nb == 1 ? of<FORMAT, 128, 1>(bf16, f32) : nb == 2 ? of<FORMAT, 128, 2>(bf16, f32) : of<FORMAT, 128, 4>(bf16, f32);
+        return nb == 1 ? of<FORMAT, 64, 1>(bf16, f32) : nb == 2 ? of<FORMAT, 64, 2>(bf16, f32) : of<FORMAT, 64, 4>(bf16, f32);
+    }
+};
 // In a translation unit each.
+typedef TreeKernelOf<false>::Kernel TreeKernel;
 TreeKernel tree_kernel_16(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp8(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp4(int D, bool bf16, bool f32, int nb);
+typedef TreeKernelOf<true>::Kernel GroupKernel;
+GroupKernel group_kernel_16(int D, bool bf16, bool f32, int nb);
+GroupKernel group_kernel_fp8(int D, bool bf16, bool f32, int nb);
+GroupKernel group_kernel_fp4(int D, bool bf16, bool f32, int nb);
 
 }  // namespace kvb

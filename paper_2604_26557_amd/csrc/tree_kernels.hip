@@ -6,77 +6,26 @@
 #include <climits>
 #include <cmath>
 
-#include "tree_attn.hpp"
+#include "tree_combine.hpp"
 
 namespace {
 
 using namespace kvb;
 
-// A wavefront joins the splits of one query row: out = sum_s 2^(ref_s - max) acc_s / sum_s 2^(ref_s - max) l_s.  A lane has the weight of a split (of two, beyond 64), so the
-// exponentials take one instruction for the row, and the sums of up to 8 * 64 / (D / 4) splits are loaded at once, ahead of the weights.  Bound by its launch and two dependent reads: 4.0 us for 7
-// splits of 512 rows, 5.8 for 16 of 2048 (17 MB).
-constexpr int kCombineWaves = 4;
-constexpr float kNothing = -1.f;   // weight of a split without anything
 template <int D>
 __global__ void __launch_bounds__(64 * kCombineWaves) kv_tree_combine_kernel(TreeParams p)
 {
-    constexpr int kLanes = D / 4, kTogether = 64 / kLanes, kRound = 8;   // lanes of a row; splits at a time; of them on their way
     const int b = blockIdx.y, lane = threadIdx.x & 63, Hq = p.H * p.G;
     const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * kCombineWaves + (int)(threadIdx.x >> 6));
     const int first = load_uniform(p.tok_first + b), drafted = min(load_uniform(p.tok_first + b + 1) - first, KV_TREE_MAX);
     const int total = max(0, min(load_uniform(p.seq_lens + b), p.max_total - drafted)) + drafted;
     if (r >= drafted * Hq) return;
-    const int t = first + r / Hq, hq = r % Hq;
-    const int ns = min(p.ns, (total - 1) / p.split_tokens + 1);
-    const long long row = (long long)t * Hq + hq;
-    const f32x2 *const ml = (const f32x2 *)p.part_ml + row * p.ns;
-    const int sub = lane / kLanes, d = lane % kLanes * 4;
-    const float *const part = p.part_acc + row * p.ns * D + d;
-    const f32x2 m0 = lane < ns ? ml[lane] : f32x2{kNoScore, 0.f}, m1 = 64 + lane < ns ? ml[64 + lane] : f32x2{kNoScore, 0.f};
-    f32x4 y[kRound];
-    auto load = [&](int s0) {
-#pragma unroll
-        for (int k = 0; k < kRound; ++k) {
-            const int s = s0 + k * kTogether + sub;
-            if (s0 + k * kTogether < ns) y[k] = *(const f32x4 *)&part[(long long)(s < ns ? s : 0) * D];
-        }
-    };
-    load(0);
-    float to = fmaxf(m0[0], m1[0]);
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) to = fmaxf(to, __shfl_xor(to, o));
-    const float w0 = m0[1] == 0.f ? kNothing : __builtin_amdgcn_exp2f(m0[0] - to), w1 = m1[1] == 0.f ? kNothing : __builtin_amdgcn_exp2f(m1[0] - to);
-    float l = m0[1] * w0 + m1[1] * w1;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) l += __shfl_xor(l, o);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](auto some_are_zero) {
-        for (int s0 = 0; s0 < ns; s0 += kRound * kTogether) {
-            if (s0 > 0) load(s0);
-#pragma unroll
-            for (int k = 0; k < kRound; ++k) {
-                const int s = s0 + k * kTogether + sub;
-                if (s0 + k * kTogether >= ns) break;
-                const float f = __shfl(s0 < 64 ? w0 : w1, s & 63);
-                if (s < ns && f != kNothing) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)   // a weight too small for 32 bits still counts against an infinity
-                        x[e] = fmaf(y[k][e], decltype(some_are_zero)::value && f == 0.f && !__builtin_isfinite(y[k][e]) ? 1.0e-37f : f, x[e]);
-                }
-            }
-        }
-    };
-    if (__any(w0 == 0.f || w1 == 0.f)) add(std::true_type{});
-    else add(std::false_type{});
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-#pragma unroll
-        for (int o = kLanes; o < 64; o *= 2) x[e] += __shfl_xor(x[e], o);
-    }
-    if (sub == 0) store_four(p.out, t * p.o_st + hq * p.o_sh + d, p.out_mode, x * (l == 0.f ? 0.f : 1.f / l));
+    combine_row<D>(p, first + r / Hq, r % Hq, min(p.ns, (total - 1) / p.split_tokens + 1), lane, [](int s) { return s; });
 }
 
-TreeShape shape_of(const kv_plan *p, int bits, bool paged)
+}  // namespace
+
+kvb::TreeShape kvb::tree_shape(const kv_plan *p, int bits, bool paged)
 {
     static int cus = 0;
     if (cus == 0) {
@@ -85,8 +34,6 @@ TreeShape shape_of(const kv_plan *p, int bits, bool paged)
     }
     return TreeShape{p->D, p->H, p->Hq / p->H, bits, cus, paged};
 }
-
-}  // namespace
 
 extern "C" int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t *masks, int32_t *depths)
 {
@@ -107,7 +54,7 @@ extern "C" int kv_tree_masks(const int32_t *parents, int n, int words, uint64_t 
 extern "C" size_t kv_tree_attn_workspace(const kv_plan_t *p, int n_tok, int max_len)
 {
     if (!p || n_tok < 0 || max_len < 0) return 0;
-    return (size_t)std::max<uint64_t>(16, tree_workspace_bytes(shape_of(p, 16, false), n_tok, (long long)max_len + KV_TREE_MAX));
+    return (size_t)std::max<uint64_t>(16, tree_workspace_bytes(tree_shape(p, 16, false), n_tok, (long long)max_len + KV_TREE_MAX));
 }
 
 extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *a, void *workspace,
@@ -155,7 +102,7 @@ extern "C" int kv_tree_attn(const kv_plan_t *p, const kv_view_t *view, const kv_
     t.out_mode = a->out_dtype == KV_OUT_F32 ? 0 : bf16 ? 2 : 1;
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;
-    const TreeCut cut = cut_tree(shape_of(p, format_bits(format), t.c.table != nullptr), p->B, view->seq_lens_host, a->tok_first_host, a->n_splits, ws_bytes);
+    const TreeCut cut = cut_tree(tree_shape(p, format_bits(format), t.c.table != nullptr), p->B, view->seq_lens_host, a->tok_first_host, a->n_splits, ws_bytes);
     t.ns = cut.ns;
     t.split_tokens = cut.split_tokens;
     t.row_blocks = cut.row_blocks;

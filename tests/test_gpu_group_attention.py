@@ -1,0 +1,359 @@
+"""Attention over shared prefixes and of capped, biased and bounded scores against 64-bit forms."""
+import numpy as np
+import pytest
+import torch
+
+from batchcase import Batch
+from paper_2604_26557_amd import binding as kv
+from servecase import FORMATS, random_parents
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float16, torch.bfloat16]
+ODS = [kv.KV_OUT_F32, kv.KV_OUT_SAME]
+
+
+def slopes_of(n):
+    return [float(np.float32(2.0 ** (-8 * (i + 1) / n))) for i in range(n)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("D,H,G", [(64, 2, 1), (64, 1, 7), (128, 2, 4), (128, 1, 20), (256, 2, 3), (256, 1, 8)])
+def test_shared_prefix(dtype, fmt, D, H, G):
+    for layout, P, od in (("bhsd", 100, kv.KV_OUT_F32), ("paged", 203, kv.KV_OUT_SAME)):
+        b = Batch([P + n for n in (0, 5, 70, 33)], [1, 3, 1, 2], H, G, D, dtype, fmt, layout, seed=D + G, first=[0, 4], prefix=[P])
+        for n_splits in (0, 3):
+            b.check(b.attend(od, n_splits), od == kv.KV_OUT_F32)
+
+
+@pytest.mark.parametrize("layout,bt", [("bhsd", 0), ("paged", 16), ("paged", 32), ("paged", 8), ("paged", 48)])
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+@pytest.mark.parametrize("P", [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 100, 513])
+def test_prefix_lengths(layout, bt, fmt, P):
+    """Prefixes that end anywhere in a block or a step, sequences that have nothing else, and some outside of any group."""
+    lens = [P, P + 1, P + 40, 20, P + 7, P]
+    b = Batch(lens, [1, 2, 1, 3, 1, 1], 2, 2, 64, torch.float16, fmt, layout, bt=bt or 16, seed=P, first=[0, 3, 3, 3], prefix=[P, 7, 0])
+    b.check(b.attend())
+    b.check(b.attend(n_splits=2))
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+def test_groups(fmt):
+    """Several groups of unequal sizes, a leader that has no new token, sequences before, between and after them, trees."""
+    lens = [30, 210, 200, 260, 90, 300, 333, 301, 12, 5]
+    news = [2, 0, 5, 1, 3, 1, 0, 9, 4, 1]
+    rng = np.random.default_rng(3)
+    trees = [random_parents(rng, n) for n in news]
+    for t in (trees, None):
+        b = Batch(lens, news, 3, 3, 64, torch.bfloat16, fmt, "paged", seed=11, first=[1, 4, 8], prefix=[200, 80], trees=t)
+        b.check(b.attend())
+        b.check(b.attend(n_splits=5))
+        b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+@pytest.mark.parametrize("which", range(6))
+@pytest.mark.parametrize("D,dtype,fmt", [(64, torch.float16, "fp4"), (128, torch.bfloat16, "16"), (256, torch.float16, "fp8"), (128, torch.float16, "fp8"), (64, torch.bfloat16, "16")])
+def test_wide_groups(D, dtype, fmt, which):
+    """16, 32 and 64 rows a workgroup, several row blocks of a prefix."""
+    B, news, G = [(12, 1, 1), (20, 1, 3), (40, 1, 4), (70, 1, 2), (9, 7, 4), (5, 30, 5)][which]
+    rng = np.random.default_rng(which)
+    P = 300
+    lens = [P + int(n) for n in rng.integers(0, 60, B)]
+    b = Batch(lens, [news] * B, 2, G, D, dtype, fmt, "paged" if which % 2 else "bhsd", seed=which, first=[0, B], prefix=[P], cap=(0.0, 5.0)[which % 2])
+    for od, n_splits in ((kv.KV_OUT_F32, 0), (kv.KV_OUT_SAME, 3)):
+        b.check(b.attend(od, n_splits), od == kv.KV_OUT_F32)
+
+
+def test_what_followers_hold_of_the_prefix_is_not_read():
+    """NaN in the followers' own places of the prefix, and blocks that are not there, change no bit."""
+    for layout in ("bhsd", "paged"):
+        for fmt in ("16", "fp8"):
+            P = 117
+            b = Batch([P + 3, P + 50, P], [1, 2, 1], 2, 4, 128, torch.bfloat16, fmt, layout, seed=5, first=[0, 3], prefix=[P])
+            want = b.attend()
+            b.check(want)
+            for s in (1, 2):
+                for j in range(P):
+                    i, r = b.c.place(s, j)
+                    for kind in "kv":
+                        if fmt == "16":
+                            b.c.dev[kind][i, :, r] = float("nan")
+                        else:
+                            b.c.dev[kind + "_scale"][i, :, r] = 255
+            assert torch.equal(b.attend(), want)
+            if layout == "paged":
+                b.c.table[1:, :P // 16] = -1
+                assert torch.equal(b.attend(), want)
+                b.c.table[1:, :P // 16] = 2 ** 31 - 1
+                assert torch.equal(b.attend(), want)
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("D,H,G,dtype", [(64, 1, 4, torch.float16), (128, 2, 3, torch.bfloat16), (256, 1, 2, torch.bfloat16), (128, 1, 16, torch.float16)])
+def test_caps(fmt, D, H, G, dtype):
+    for cap, size in ((30.0, 1.0), (50.0, 6.0), (0.5, 1.0), (1.0e4, 1.0), (3.0, 0.02)):
+        b = Batch([300, 41], [1, 6], H, G, D, dtype, fmt, seed=D, cap=cap, scale_k=size)
+        for od in ODS:
+            b.check(b.attend(od), od == kv.KV_OUT_F32)
+        b.check(b.attend(n_splits=1, scale=-0.3), scale=-0.3)
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp4"])
+@pytest.mark.parametrize("D,H,G,dtype", [(64, 3, 4, torch.float16), (128, 2, 5, torch.bfloat16), (256, 1, 2, torch.float16), (128, 1, 16, torch.bfloat16)])
+def test_biases(fmt, D, H, G, dtype):
+    """Distances of trees (by depth) and chains, with prefixes, caps and splits."""
+    rng = np.random.default_rng(D)
+    trees = [random_parents(rng, n) for n in (1, 12, 40)]
+    for t in (trees, None):
+        for cap in (0.0, 10.0):
+            b = Batch([300, 150, 900], [1, 12, 40], H, G, D, dtype, fmt, "paged", seed=G, slopes=slopes_of(H * G), trees=t, cap=cap, first=[0, 2], prefix=[110])
+            for n_splits in (0, 1, 4):
+                b.check(b.attend(n_splits=n_splits))
+            b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+def test_biases_of_far_positions():
+    """Positions around 10^6 and queries far behind or before their keys: what counts is the distance."""
+    b = Batch([400, 80], [3, 2], 1, 4, 64, torch.float16, seed=3, slopes=[0.5, 0.03, 1.0e-4, 0.0], positions=[1000000, 1000003, 1000001, 30, 500000])
+    b.check(b.attend())
+    b.check(b.attend(n_splits=3))
+    b = Batch([400, 80], [3, 2], 1, 4, 64, torch.float16, seed=3, slopes=[0.5, 0.03, 1.0e-4, 0.0], positions=[0, 200, 401, -50, 500])
+    b.check(b.attend())
+    b.check(b.attend(n_splits=3))
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+@pytest.mark.parametrize("window", [1, 2, 17, 32, 100, 1000])
+def test_windows(fmt, window):
+    """Windows that begin in the prefix, in the own tokens, or before both."""
+    for D, news, P in ((64, [1, 1, 1], 200), (128, [9, 1, 40], 90), (128, [1, 3, 1], 0)):
+        lens = [P + 10, P + 333, P]
+        at = [n + i for n, t in zip(lens, news) for i in range(t)]
+        b = Batch(lens, news, 2, 4, D, torch.bfloat16, fmt, "paged", seed=window, first=[0, 3], prefix=[P], sees_from=[max(0, p - window + 1) for p in at])
+        b.check(b.attend())
+        b.check(b.attend(kv.KV_OUT_SAME, 3), False)
+
+
+@pytest.mark.parametrize("od", ODS)
+def test_rows_that_see_nothing(od):
+    """Bounds past everything leave a row of zeros; so does an empty context with a token that does not see itself."""
+    b = Batch([100, 0, 64], [3, 2, 1], 2, 2, 64, torch.float16, seed=9, first=[0, 1], prefix=[64], sees_from=[0, 1000, 2 ** 31 - 1, 1, 1, 65], sees_to=[0, 0, 0, -5, 2 ** 31 - 1, -2 ** 31])
+    for n_splits in (0, 1, 2):
+        got = b.attend(od, n_splits)
+        b.check(got, od == kv.KV_OUT_F32)
+        assert (got[1] == 0).all() and (got[2] == 0).all() and (got[3] == 0).all() and (got[5] == 0).all() and (got[0] != 0).all() and (got[4] != 0).any()
+    b = Batch([100, 33], [2, 1], 1, 2, 64, torch.bfloat16, seed=9, sees_from=[-2 ** 31, -1, 0], cap=4.0)
+    b.check(b.attend(od), od == kv.KV_OUT_F32)
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("D,H,G,lens,news,dtype", [(64, 2, 1, [0, 40], [130, 257], torch.float16), (128, 1, 4, [0], [300], torch.bfloat16), (256, 1, 2, [17], [259], torch.bfloat16),
+                                                   (128, 2, 7, [100, 3, 0], [65, 1, 200], torch.float16), (64, 1, 20, [5], [80], torch.bfloat16)])
+def test_prompts(fmt, D, H, G, lens, news, dtype):
+    """Chains of more tokens than a mask holds, in one piece and behind a context."""
+    b = Batch(lens, news, H, G, D, dtype, fmt, "paged" if len(lens) % 2 else "bhsd", seed=D + G)
+    for od, n_splits in ((kv.KV_OUT_F32, 0), (kv.KV_OUT_SAME, 1), (kv.KV_OUT_F32, 3)):
+        b.check(b.attend(od, n_splits), od == kv.KV_OUT_F32)
+
+
+def test_a_prompt_in_pieces_is_the_prompt():
+    """4000 tokens at once and as chunks behind each other; and the first and last rows by the definition."""
+    H, G, D, n = 2, 4, 128, 4000
+    whole = Batch([0], [n], H, G, D, torch.bfloat16, seed=2, cap=8.0)
+    got = whole.attend()
+    for at, m in ((0, 1), (0, 700), (700, 1300), (2000, 1999), (3999, 1)):
+        whole.lens, whole.news, whole.tok_first, whole.c.lens = [at], [m], [0, m], [at]
+        whole.c.lens_dev.fill_(at)
+        whole.c.remake()
+        piece = whole.attend(q=whole.q[at:at + m].cuda())
+        # two results of the same definition: each within 2^-24 times some hundred roundings of values up to 4
+        assert (piece - got[at:at + m]).abs().max() <= 4 * 2 * 300 * 2.0 ** -24 * 4
+    x, k, v = whole.q.double().numpy(), whole.c.seq("k", 0, n), whole.c.seq("v", 0, n)
+    for t in (0, 1, 63, 64, 1000, 3999):
+        for h in (0, 5):
+            s = 8 * np.tanh(k[h // G, :t + 1] @ x[t, h] * D ** -0.5 / 8)
+            p = np.exp(s - s.max())
+            assert np.abs(got[t, h].double().cpu().numpy() - p @ v[h // G, :t + 1] / p.sum()).max() <= 4 * 300 * 2.0 ** -24 * 4
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+@pytest.mark.parametrize("both", [0, 1, 20, 1000])
+def test_documents_with_prefixes(fmt, both):
+    """Packed documents, whose first tokens see each other both ways, with biases: tokens behind a query are seen too."""
+    lens, news = [50, 0], [150, 90]
+    starts = [[10, 50 + 30, 50 + 31, 50 + 100], [0, 64]]
+    lo, up, pos = [], [], []
+    for n, t, s in zip(lens, news, starts):
+        for j in range(n, n + t):
+            start = max(x for x in s if x <= j)
+            end = min([x for x in s if x > j], default=n + t)
+            lo.append(start)
+            up.append(min(max(start, n) + both, end))
+            pos.append(j)
+    for slopes in (None, slopes_of(8)):
+        b = Batch(lens, news, 2, 4, 64, torch.float16, fmt, "paged", seed=both, slopes=slopes, sees_from=lo, sees_to=up)
+        for n_splits in (0, 1, 3):
+            b.check(b.attend(n_splits=n_splits))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["k", "v"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_values_that_are_not_finite(dtype, kind, value):
+    """Where no row looks they change nothing; a NaN that a row sees is one in its result, whatever caps it."""
+    P, fill = 70, dict(cap=10.0, slopes=slopes_of(4))
+    for D, G in ((64, 2), (128, 4)):
+        make = lambda: Batch([P + 60, P + 9], [2, 1], 4 // G if G < 4 else 1, G, D, dtype, seed=4, first=[0, 2], prefix=[P], sees_from=[40, 41, 40], **(fill if G == 4 else dict(cap=10.0)))  # noqa: E731
+        b = make()
+        want = b.attend(n_splits=2)
+        b.check(want)
+        for seq, slot in ((0, 3), (0, 39), (1, 50)):   # before every window, and a follower's place of the prefix
+            b.c.dev[kind][seq, :, slot, 5] = value
+        b.check(b.attend(n_splits=2))
+        b.check(b.attend())
+        b.c.dev[kind][0, :, P + 61, 5] = float("nan")   # the first sequence's second new token: its own row sees it, nobody else
+        got = b.attend(n_splits=2)
+        assert torch.isfinite(got[0]).all() and torch.isfinite(got[2]).all()
+        assert torch.isnan(got[1]).all() if kind == "k" else torch.isnan(got[1, :, 5]).all()
+        b = make()
+        b.c.dev["k"][0, :, 60, 5] = float("nan")   # of the prefix: all rows see it
+        assert torch.isnan(b.attend(n_splits=2)).all() and torch.isnan(b.attend(kv.KV_OUT_SAME, 1)).all()
+
+
+def test_infinite_scores_under_a_cap():
+    """bf16 products past 32 bits are infinities, which a cap makes finite again."""
+    b = Batch([40], [1], 1, 2, 64, torch.bfloat16, seed=6, cap=2.0)
+    b.c.dev["k"][0, 0, 7] = 1.0e30
+    b.c.dev["k"][0, 0, 9] = -1.0e30
+    q = torch.full((1, 2, 64), 1.0e20, dtype=torch.bfloat16, device="cuda")
+    got = b.attend(q=q).double().cpu().numpy()
+    k, v = b.c.seq("k", 0, 41), b.c.seq("v", 0, 41)
+    s = np.where(k[0].sum(1) * 1.0 > 0, 2.0, -2.0)   # all other scores are far past the cap as well, by the sign of their sums
+    s[7], s[9] = 2.0, -2.0
+    clear = np.abs(k[0].sum(1)) * 1.0e20 / 8 > 100
+    assert clear.all()
+    p = np.exp(s - s.max())
+    want = p @ v[0] / p.sum()
+    assert np.abs(got[0] - want).max() <= 64 * 2.0 ** -24 * np.abs(v).max()
+
+
+def test_steep_biases_and_large_scores():
+    """References beyond the range in which they are kept exactly: rows are gone over one by one."""
+    b = Batch([300], [2], 1, 2, 64, torch.bfloat16, seed=8, slopes=[3.0e5, 1.0], cap=0.0)
+    b.check(b.attend())
+    b = Batch([300], [2], 1, 2, 64, torch.bfloat16, seed=8, cap=3.0e6, scale_k=1.0e6)
+    got = b.attend()
+    out, _, _ = b.expected()
+    # scores of 10^6 have units of 0.06 in 32 bits: only a clear winner can be checked
+    q, k = b.q.double().numpy(), b.c.seq("k", 0, 302)
+    for t in range(2):
+        for h in range(2):
+            s = 3.0e6 * np.tanh(k[0, :301 + t] @ q[t, h] / 8 / 3.0e6)
+            top = np.sort(s)[-2:]
+            if top[1] - top[0] > 100:
+                assert np.abs(got[t, h].double().cpu().numpy() - out[t, h]).max() <= 2.0 ** -20 * np.abs(out[t, h]).max() + 1e-6
+
+
+def test_same_as_without_groups():
+    """A group of sequences whose prefixes are copies of one another: what kv_tree_attn gives for each by itself, to the roundings of both."""
+    P, D = 150, 128
+    b = Batch([P + 20, P + 64, P + 3], [2, 5, 1], 2, 4, D, torch.bfloat16, "fp8", seed=12, first=[0, 3], prefix=[P])
+    for name, t in b.c.dev.items():
+        t[1:, :, :P] = t[:1, :, :P]
+    for kind in "kv":
+        b.c.values[kind][1:, :, :P] = b.c.values[kind][:1, :, :P]
+    got = b.attend()
+    tree, _, _ = b.handles()
+    out, ws = torch.zeros_like(got), torch.empty(kv.kv_tree_attn_workspace(b.c.plan, 8, 300), dtype=torch.uint8, device="cuda")
+    kv.kv_tree_attn(b.c.plan, b.c.view, b.c.blocks, 0, tree, b.q.cuda(), out, kv.KV_OUT_F32, 0, ws)
+    _, tol, _ = b.expected()
+    assert (np.abs((got - out).double().cpu().numpy()) <= 2 * tol).all()
+    b.check(got)
+
+
+@pytest.mark.parametrize("B", [62, 64, 65, 127, 130])
+def test_more_sequences_than_lanes(B):
+    """Units are counted 64 at a time, groups first."""
+    rng = np.random.default_rng(B)
+    lens, news = (rng.integers(0, 90, B) + 40).tolist(), rng.integers(0, 4, B).tolist()
+    news[0] = news[-1] = 3
+    news[1] = 0
+    first = sorted(rng.integers(0, B, 9).tolist())
+    b = Batch(lens, news, 2, 3, 64, torch.bfloat16, "fp8", "paged", seed=B, first=first, prefix=[int(x) for x in rng.integers(0, 41, 8)])
+    for n_splits in (0, 2):
+        b.check(b.attend(n_splits=n_splits))
+
+
+def test_64_groups_and_rows_of_strided_results():
+    n = 64
+    b = Batch([20 + i % 5 for i in range(2 * n)], [1] * 2 * n, 1, 2, 64, torch.float16, seed=1, first=list(range(0, 2 * n + 1, 2)), prefix=[i % 20 for i in range(n)])
+    buf = torch.full((2 * n, 3, 67), 9.0, device="cuda")
+    out = buf[:, 1:, 2:66]
+    b.check(b.attend(out=out))
+    assert (buf[:, 0] == 9).all() and (buf[:, :, :2] == 9).all() and (buf[:, :, 66:] == 9).all()
+    # rows behind the last sequence are left as they were
+    q, out = torch.cat([b.q, b.q[:3]]).cuda(), torch.full((2 * n + 3, 2, 64), 9.0, device="cuda")
+    b.attend(q=q, out=out)
+    b.check(out[:2 * n])
+    assert (out[2 * n:] == 9).all()
+
+
+def test_smaller_workspaces():
+    b = Batch([3000, 2900, 2950], [1, 1, 2], 2, 4, 64, torch.float16, seed=13, first=[0, 3], prefix=[2000])
+    one = 4 * 8 * 66 * 4
+    for n in (2, 3, 7):
+        b.check(b.attend(ws=torch.empty(n * one, dtype=torch.uint8, device="cuda")))
+        b.check(b.attend(n_splits=128, ws=torch.empty(n * one, dtype=torch.uint8, device="cuda")))
+    with pytest.raises(kv.KVError) as e:
+        b.attend(ws=torch.empty(2 * one - 16, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == kv.KV_ENOSPC
+    b.check(b.attend(n_splits=128, ws=torch.empty(128 * one, dtype=torch.uint8, device="cuda")))
+
+
+def test_two_runs_give_the_same_bits_on_any_stream():
+    b = Batch([5000, 4100, 4700], [4, 1, 9], 2, 4, 128, torch.bfloat16, "fp8", "paged", seed=14, first=[0, 3], prefix=[4099], cap=30.0, slopes=slopes_of(8))
+    first = b.attend()
+    for _ in range(3):
+        assert torch.equal(b.attend(), first)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = b.attend()
+    s.synchronize()
+    assert torch.equal(other, first)
+
+
+def test_offsets_beyond_32_bits():
+    """A leader and a follower far apart, rows more than 4 GiB from the buffer's start."""
+    D, far, P = 64, 5 << 30, 30
+    b = Batch([P + 5, P + 9], [2, 2], 1, 4, D, torch.bfloat16, "fp8", seed=15, first=[0, 2], prefix=[P], cap=5.0)
+    want = b.attend(n_splits=2)
+    b.check(want)
+    buf = torch.zeros(far + (1 << 20), dtype=torch.uint8, device="cuda")
+    n = b.c.rows
+    for at, kind in ((0, "k"), (n * D, "v")):
+        x = buf[at:].as_strided((2, 1, n, D), (far, n * D, D, 1))
+        x[:] = b.c.dev[kind]
+        b.c.dev[kind] = x
+    b.c.remake()
+    assert torch.equal(b.attend(n_splits=2), want)
+
+
+def test_rows_looked_up_one_by_one():
+    """Tokens so far apart that a step's offsets pass 32 bits, and heads and tokens in another order."""
+    b = Batch([64 + 9, 64 + 70], [1, 2], 2, 2, 64, torch.float16, seed=16, first=[0, 2], prefix=[50], cap=5.0, sees_from=[3, 40, 60])
+    want = b.attend(n_splits=1)
+    b.check(want)
+    for kind in "kv":
+        b.c.dev[kind] = b.c.dev[kind].permute(2, 1, 0, 3).contiguous().permute(2, 1, 0, 3)   # token-major
+    b.c.remake()
+    assert torch.equal(b.attend(n_splits=1), want)
+    n, stride = b.c.rows, 1 << 24
+    buf = torch.empty(stride * n + 4096, dtype=torch.float16, device="cuda")
+    for kind, at in (("k", 0), ("v", 2048)):
+        far = buf[at:].as_strided((2, 2, n, 64), (512, 128, stride, 1))
+        far[:] = b.c.dev[kind]
+        b.c.dev[kind] = far
+    b.c.remake()
+    assert torch.equal(b.attend(n_splits=1), want)
