@@ -774,18 +774,18 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             if (i < NB * kSteps) load_to_lds<16, false>(p.q + 2 * ((first + t) * p.q_st + ((int)h * p.G + g) * p.q_sh + T::q_at(s, group)), to + i * 1024);
         }
     };
-    [[maybe_unused]] float slope[NB];
+    // A lane has the slope of a head of the KV head's; a row asks the lane of its head (of groups of more than 64, memory, at the price of a wait for all loads ahead).
+    [[maybe_unused]] float slopes = 0.f;
     if constexpr (GROUP) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            slope[nb] = 0.f;
-            if (p.slopes) {
-                const int r = min(nb * 16 + n, n_rows - 1);
-                slope[nb] = p.slopes[(int)h * p.G + (int)rb * kRows + r - row_token(r) * p.G];
-                asm volatile("" : "+v"(slope[nb]));   // here now: a wait for it in the loop would be one for the loads ahead
-            }
+        if (p.slopes && lane < p.G) {
+            slopes = p.slopes[(int)h * p.G + lane];
+            asm volatile("" : "+v"(slopes));   // here now: a wait for it in the loop would be one for the loads ahead
         }
     }
+    [[maybe_unused]] auto slope_of = [&](const GroupParams &p, int r) {
+        const int g = (int)rb * kRows + r - row_token(r) * p.G;
+        return p.G <= 64 ? __shfl(slopes, g) : p.slopes[(int)h * p.G + g];
+    };
     u32x4 q_reg[T::kQStays ? 1 : NB][kSteps];
     f32x4 acc[NB][kColumns], sum[NB];
     float ref[NB];
@@ -1014,18 +1014,26 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
             if (j0 + 31 <= pos_least && j0 + 32 <= len) {
                 const float at = (float)(j0 + group - origin);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float slope = slope_of(p, min(nb * 16 + here(n), n_rows - 1));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope[nb], at + (float)(4 * j), s[nb][j / 4][j % 4]);
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope, at + (float)(4 * j), s[nb][j / 4][j % 4]);
+                }
             } else {
+                int at[8];   // the lane's tokens' positions
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int k = j0 + here(group) + 4 * j, kp = k < len ? k : p.positions[first + min(k - len, drafted - 1)];
+                    at[j] = j0 + here(group) + 4 * j;
+                    if (at[j] >= len) at[j] = p.positions[first + min(at[j] - len, drafted - 1)];
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        const int pos = p.positions[first + row_token(min(nb * 16 + n, n_rows - 1))];
-                        s[nb][j / 4][j % 4] = fmaf(slope[nb], (float)(min((long long)kp, 2ll * pos - kp) - (by_row ? pos : origin)), s[nb][j / 4][j % 4]);
-                    }
+                for (int nb = 0; nb < NB; ++nb) {
+                    const int r = min(nb * 16 + here(n), n_rows - 1), pos = p.positions[first + row_token(r)], ahead = by_row ? 0 : pos - origin;
+                    const float slope = slope_of(p, r);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope, (float)(ahead - abs(pos - at[j])), s[nb][j / 4][j % 4]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
