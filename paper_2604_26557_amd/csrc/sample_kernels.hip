@@ -1,16 +1,17 @@
 // The next token of every row of logits: temperature, top-k, top-p and min-p from given random numbers.
 //
-// Mathematics.  w_i = exp((l_i - max) / T) is held as an integer W_i of 2^-s, s = 62 - log2(n_vocab) or 51: sums are exact, whatever their order, so splits, histograms
+// Mathematics.  w_i = exp((l_i - max) / T) is held as an integer W_i of 2^-s, s = 62 - log2(n_vocab) or 51: sums are exact, whatever their order, so slices, histograms
 // and prefix sums of any shape give one answer, and adding takes no care.  With tokens ordered by (l from the largest, index), each of the three cuts keeps a beginning of that order: what is kept
 // is every token up to one, the border, in that order, and the token is found in order of indices: sums of tiles, of which one is gone over again.
 //
 // A workgroup has a row. It is read from HBM once, for its maximum, and from L2 after that.
 //   Few of the largest (top_k up to 256): no fewer than k tokens reach the k-th largest of the threads' own maxima; a list of those that do is all there is to rank.
-//   top_p alone: the sum of all, and a histogram over distances from the maximum. A token below (1 - p) / n_vocab of the sum is kept by none: a sample says about where that is, and only what is
-//     above goes into the histogram (a quarter of the tokens in a usual case; an atomic of 64 bits for all of them takes longer than the exponentials). Then a list of what is kept for sure, and of the bin with the border.
+//   top_p alone: the sum of all, and a histogram over distances from the maximum. Tokens below (1 - p) / n_vocab of the sum are not needed to get from p to the whole: a sample says about where that is, and
+//     only what is above goes into the histogram (a third of the tokens in a usual case). Then a list of what is kept for sure, and one of the bin with the border, which is ranked.
 //   min_p alone: a list of what is above.
 //   What these have no room for, or larger top_k: histograms over the whole row, of its keys in the end, in as many rounds as they need.
-// What bounds it: the exponentials in double precision where the sum of all is needed (23 instructions each), otherwise latencies of a pass.
+// What bounds it: some 30 instructions, most of them in double precision, for every weight where the sum of all is needed, otherwise a pass' latencies.  So few rows of many tokens are shared by several
+// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 75 us with a workgroup each, SPLIT_TIME so.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,17 +27,35 @@ namespace {
 using namespace kvb;
 
 typedef unsigned long long u64;
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;   // of a row: of one workgroup, or of several
 constexpr int kBins = 2048;
 constexpr int kTiles = 1024;     // of a row, each at least 512 tokens: what a wavefront loads at once is of one
 constexpr int kExpTable = 256;
-constexpr int kList = 16384;     // tokens of a list
 constexpr int kRanked = 1024;    // tokens that are put into order one against all others
+constexpr int kMostSlices = 16;
+
+// What the slices of a row leave for the next launch.
+struct RowState {
+    float maxima[kMostSlices][kThreads];   // of each thread; +infinity for a NaN or +infinity
+    u64 tile_weight[kTiles];               // sums of what is kept for sure
+    unsigned some[kRanked];                // of what may be kept: index, logit
+    float some_logit[kRanked];
+    u64 in_bin;                            // of the target, what its bin has to give
+    float per;                             // bins per unit of a logit, of top_p rows
+    unsigned n_some, fits, unused;         // fits: the above says it all, if n_some does not pass kRanked
+};
+// And each slice of a top_p row.
+struct SliceState {
+    u64 weight[kBins], sum, unused;
+};
 
 struct SampleParams {
     kv_sample_args_t a;
-    int shift;   // log2 of the weights' unit
-    int tile;    // log2 of the tokens of a tile
+    RowState *rows;   // null: a workgroup a row does it all
+    SliceState *slice_of;
+    int slices;
+    int shift;        // log2 of the weights' unit
+    int tile;         // log2 of the tokens of a tile
 };
 
 // A logit's bits as a number that grows with it; -0 is 0.
@@ -45,6 +64,9 @@ __device__ __forceinline__ unsigned key_of(float x)
     const unsigned b = __float_as_uint(x + 0.f);
     return b >> 31 ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of(unsigned key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+// Where a token is in the order: larger ones come first. Keys are never zero.
+__device__ __forceinline__ u64 place_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
 
 template <int DTYPE> constexpr int kVector = DTYPE == KV_F32 ? 4 : 8;   // logits of a load of 16 bytes
 
@@ -56,169 +78,577 @@ __device__ __forceinline__ float logit_at(const void *row, long long i)
     else return __uint_as_float((unsigned)((const unsigned short *)row)[i] << 16);
 }
 
-struct Nothing {
-    __device__ __forceinline__ void operator()(int) const {}
-};
-// f(logit, index) for the logits of a row that fall to this thread, several loads of 16 bytes at a time; what lies before the first aligned one, and after the last, goes to a thread each.
-// loaded(first index) after each load.
-template <int DTYPE, typename F, typename L = Nothing>
-__device__ __forceinline__ void for_logits(const char *row, int V, int tid, const F &f, const L &loaded = L{})
+template <int DTYPE>
+__device__ __forceinline__ void unpack(uint4 w, float (&l)[kVector<DTYPE>])
 {
-    constexpr int E = kVector<DTYPE>, kBytes = 16 / E, kAhead = 4;
-    const int before = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / kBytes), vectors = (V - before) / E, after = before + vectors * E;
-    if (tid < before) f(logit_at<DTYPE>(row, tid), tid), loaded(tid);
-    if (tid < V - after) f(logit_at<DTYPE>(row, after + tid), after + tid), loaded(after + tid);
-    const uint4 *const at = (const uint4 *)(row + (long long)before * kBytes);
-    for (int v0 = tid; v0 < vectors; v0 += kAhead * kThreads) {
-        uint4 w[kAhead];
+    const unsigned x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (v0 + k * kThreads < vectors) w[k] = at[v0 + k * kThreads];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int v = v0 + k * kThreads;
-            if (v >= vectors) break;
-            const unsigned x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float l;
-                if constexpr (DTYPE == KV_F32) l = __uint_as_float(x[e]);
-                else if constexpr (DTYPE == KV_BF16) l = __uint_as_float(e % 2 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
-                else l = (float)__builtin_bit_cast(_Float16, (unsigned short)(e % 2 ? x[e / 2] >> 16 : x[e / 2]));
-                f(l, before + v * E + e);
-            }
-            loaded(before + v * E);
-        }
+    for (int e = 0; e < kVector<DTYPE>; ++e) {
+        if constexpr (DTYPE == KV_F32) l[e] = __uint_as_float(x[e]);
+        else if constexpr (DTYPE == KV_BF16) l[e] = __uint_as_float(e % 2 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+        else l[e] = (float)__builtin_bit_cast(_Float16, (unsigned short)(e % 2 ? x[e / 2] >> 16 : x[e / 2]));
     }
 }
 
-// Sum over the wavefront, in every lane.
-__device__ __forceinline__ u64 wave_sum(u64 x)
+// each(logits, first index, their number) for the loads of 16 bytes of a row that fall to thread `tid` of `threads`, AHEAD at a time; what lies before the first aligned one, and after the last,
+// goes to a thread each. A wavefront's loads lie side by side; with some lanes missing in the end.
+template <int DTYPE, int AHEAD, typename F>
+__device__ __forceinline__ void for_loads(const char *row, int V, int tid, int threads, const F &each)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o);
-    return x;
-}
-__device__ __forceinline__ u64 wave_sums_to(u64 x, int lane)   // of the lanes up to this one
-{
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const u64 y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+    constexpr int E = kVector<DTYPE>, kBytes = 16 / E;
+    const int before = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / kBytes), vectors = (V - before) / E, after = before + vectors * E;
+    if (tid < before + V - after) {   // at most 2 (E - 1)
+        const int i = tid < before ? tid : after + tid - before;
+        float l[E] = {};
+        l[0] = logit_at<DTYPE>(row, i);
+        each(l, i, 1);
     }
+    const uint4 *const at = (const uint4 *)(row + (long long)before * kBytes);
+    auto unpacked = [&](uint4 w, int v) {
+        float l[E];
+        unpack<DTYPE>(w, l);
+        each(l, before + v * E, E);
+    };
+    int v = tid;
+    if constexpr (AHEAD > 1) {
+        for (; v + (AHEAD - 1) * threads < vectors; v += AHEAD * threads) {
+            uint4 w[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) w[k] = at[v + k * threads];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) unpacked(w[k], v + k * threads);
+        }
+    }
+    // the next one is loaded before one is worked on
+    uint4 next = v < vectors ? at[v] : uint4{};
+#pragma unroll 1
+    for (; v < vectors; v += threads) {
+        const uint4 w = next;
+        if (v + threads < vectors) next = at[v + threads];
+        unpacked(w, v);
+    }
+}
+// f(logit, index) for each, of a workgroup's row.
+template <int DTYPE, typename F>
+__device__ __forceinline__ void for_logits(const char *row, int V, int tid, const F &f)
+{
+    for_loads<DTYPE, 1>(row, V, tid, kThreads, [&](const float (&l)[kVector<DTYPE>], int i, int n) {
+#pragma unroll
+        for (int e = 0; e < kVector<DTYPE>; ++e)
+            if (e < n) f(l[e], i + e);
+    });
+}
+
+// x moved by a data-parallel primitive (of which lanes without a source get 0)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 x)
+{
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)x, CTRL, ROWS, 0xf, false), hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(x >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)hi << 32 | lo;
+}
+// Sums over the lanes up to each: 1, 2, 4, 8 of a row of 16, then over rows. All lanes take part.
+__device__ __forceinline__ u64 wave_sums_to(u64 x)
+{
+    x += moved<0x111, 0xf>(x);
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);
+    x += moved<0x143, 0xc>(x);
     return x;
 }
+__device__ __forceinline__ u64 of_lane(u64 x, int l)
+{
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(x >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, l);
+}
+__device__ __forceinline__ u64 wave_sum(u64 x) { return of_lane(wave_sums_to(x), 63); }
+
+// 2^(i / 256), by the series of e^x.
+struct ExpTable {
+    double of[kExpTable];
+    constexpr ExpTable() : of()
+    {
+        for (int i = 0; i < kExpTable; ++i) {
+            double sum = 1., term = 1.;
+            for (int k = 1; k < 24; ++k) sum += term *= i * 0.6931471805599453 / kExpTable / k;
+            of[i] = sum;
+        }
+    }
+};
+__device__ const ExpTable kExps{};
+
+// A thread's sum of the logits from i on to their tile's: 64 loads side by side are of one.
+template <typename R>
+__device__ __forceinline__ void add_to_tile(const R &row, int i, u64 sum, u64 *weight)
+{
+    if (__ballot(1) == ~0ull) {
+        sum = wave_sum(sum);
+        if ((threadIdx.x & 63) == 0) atomicAdd(&weight[row.tile_of(i)], sum);
+    } else {
+        atomicAdd(&weight[row.tile_of(i)], sum);
+    }
+}
+
+// A row, and what is asked of it.
+template <int DTYPE>
+struct Row {
+    static constexpr int E = kVector<DTYPE>;
+    const char *at;
+    int V, shift, tile, before_loads, n_tiles;
+    float T, top_p, min_p, top;
+    unsigned k;
+    bool greedy, cut_k, cut_p;
+    float least;          // what is below does not weigh min_p
+    double per_unit, top64;
+    const double *exps;   // 2^(i / 256)
+
+    __device__ __forceinline__ Row(const SampleParams &p, int b)
+    {
+        const kv_sample_args_t &a = p.a;
+        at = (const char *)a.logits + (long long)b * a.stride * (16 / E);
+        V = a.n_vocab;
+        shift = p.shift;
+        tile = p.tile;
+        before_loads = min(V, (int)((16 - ((uintptr_t)at & 15)) & 15) / (16 / E));
+        n_tiles = max(1, ((V - before_loads - 1) >> tile) + 1);
+        T = a.temperature ? a.temperature[b] : 1.f;
+        greedy = !(T > 0.f);
+        const int asked = greedy ? 1 : a.top_k ? a.top_k[b] : 0;
+        k = asked <= 0 || asked > V ? (unsigned)V : (unsigned)asked;
+        cut_k = k < (unsigned)V;
+        top_p = greedy || !a.top_p ? 1.f : a.top_p[b];
+        cut_p = top_p < 1.f;
+        min_p = greedy || !a.min_p ? 0.f : fminf(a.min_p[b], 1.f);
+    }
+    __device__ __forceinline__ void set_top(float t, const double *table)
+    {
+        top = t;
+        top64 = t;
+        per_unit = greedy ? 0. : 1.4426950408889634 * kExpTable / (double)T;
+        exps = table;
+        // less some units of its own rounding
+        least = min_p > 0.f ? (float)(top64 + log((double)min_p) * (double)T) - 1.0e-5f * (fabsf(top) + 1.f) - 1.0e-5f * T : -INFINITY;
+        if (!(least == least)) least = -INFINITY;
+    }
+    // exp((l - max) / T) * 2^shift = 2^(n / 256 + g / 256 + shift) with |g| <= 1/2: a table, and e^(g ln 2 / 256) by its series (the next term is below 2^-54). What is below 2^-60 counts as that.
+    __device__ __forceinline__ double scaled_weight(float x, int by) const
+    {
+        static_assert(kExpTable == 256, "8 bits");
+        constexpr double c = 0.6931471805599453 / kExpTable;
+        const double y = fmax(((double)x - top64) * per_unit, -60. * kExpTable);   // the bound for an infinity times zero as well
+        const double n = rint(y), g = y - n;
+        const int i = (int)n;
+        const double e = fma(g, fma(g, fma(g, fma(g, c * c * c * c / 24, c * c * c / 6), c * c / 2), c), 1.);
+        return ldexp(exps[i & (kExpTable - 1)] * e, (i >> 8) + by);
+    }
+    __device__ __forceinline__ bool weighs(float x) const { return !(min_p > 0.f) || scaled_weight(x, 0) >= (double)min_p; }
+    // to the nearest integer by adding 2^52, whose lowest bit is worth one
+    __device__ __forceinline__ u64 units_of(float x) const { return (u64)__double_as_longlong(scaled_weight(x, shift) + 4503599627370496.) & 0xfffffffffffffull; }
+    // Tiles begin where loads of 16 bytes do; what is before that is of the first.
+    __device__ __forceinline__ int tile_of(int i) const { return max(0, i - before_loads) >> tile; }
+    __device__ __forceinline__ int tile_begin(int t) const { return t == 0 ? 0 : before_loads + (t << tile); }
+    __device__ __forceinline__ int tile_end(int t) const { return min(V, before_loads + ((t + 1) << tile)); }
+
+    __device__ __forceinline__ float largest(int tid, int threads) const
+    {
+        float t = -INFINITY;
+        for_loads<DTYPE, 8>(at, V, tid, threads, [&](const float (&l)[E], int, int n) {
+            if (n == 1) {
+                t = l[0] <= FLT_MAX ? fmaxf(t, l[0]) : INFINITY;
+                return;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) t = l[e] <= FLT_MAX ? fmaxf(t, l[e]) : INFINITY;
+        });
+        return t;
+    }
+    // Every thread's part of a sample, a load of each of up to 1024, and how many logits that is in all: about the sum of the weights.
+    __device__ __forceinline__ int sample_size() const { return min((V - before_loads) / E, kThreads) * E; }
+    __device__ __forceinline__ float sampled(int i) const
+    {
+        const unsigned vectors = (unsigned)(V - before_loads) / E;
+        float x = 0.f;
+        if ((unsigned)i < vectors) {
+            float l[E];
+            unpack<DTYPE>(((const uint4 *)(at + (long long)before_loads * (16 / E)))[vectors > kThreads ? (unsigned)i * vectors / kThreads : i], l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x += __expf((l[e] - top) / T);
+        }
+        return x;
+    }
+    // Bins per unit of a logit: they reach down to a quarter of the weight that is looked for; the largest alone weighs 1. 0: no such thing.
+    __device__ __forceinline__ float bins_per_unit(float sample) const
+    {
+        const int n = sample_size();
+        const float sum = fmaxf(1.f, n > 0 ? sample * (float)V / (float)n : 1.f);
+        const float reach = fminf(T * __logf(4.f * (float)V / ((1.f - fmaxf(top_p, 0.f)) * sum)), T * 42.f), per = (float)kBins / reach;
+        return reach > 0.f && reach <= FLT_MAX && per <= FLT_MAX ? per : 0.f;
+    }
+    // Sum of this thread's weights, and the histogram.
+    __device__ __forceinline__ u64 sum_and_bins(int tid, int threads, float per, u64 *weight) const
+    {
+        u64 sum = 0;
+        for_loads<DTYPE, 1>(at, V, tid, threads, [&](const float (&l)[E], int, int n) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (e >= n) break;
+                const u64 w = units_of(l[e]);
+                sum += w;
+                const float bin = (top - l[e]) * per;
+                if (bin < (float)kBins) atomicAdd(&weight[(int)bin], w);
+            }
+        });
+        return sum;
+    }
+    __device__ __forceinline__ void sum_tiles(int tid, int threads, u64 *weight) const
+    {
+        for_loads<DTYPE, 1>(at, V, tid, threads, [&](const float (&l)[E], int i, int n) {
+            u64 sum = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum += e < n ? units_of(l[e]) : 0;
+            add_to_tile(*this, i, sum, weight);
+        });
+    }
+    __device__ __forceinline__ bool nothing_cut() const { return !greedy && !cut_k && !cut_p && !(min_p > 0.f); }
+    __device__ __forceinline__ bool by_bins() const { return !cut_k && cut_p; }
+    __device__ __forceinline__ bool few() const { return cut_k && k <= 256; }
+    __device__ __forceinline__ u64 target_of(u64 sum) const   // of top_p
+    {
+        const double want = ceil((double)(top_p > 0.f ? top_p : 0.f) * (double)sum);
+        return max((u64)1, min((u64)want, sum));
+    }
+};
 
 struct Shared {
     double exps[kExpTable];
     u64 weight[kBins];
     unsigned count[kBins];
     u64 tile_weight[kTiles];
-    unsigned list[kList];           // indices
     u64 ranked[kRanked];            // (key, ~index): what is larger comes first
     u64 ranked_weight[kRanked];
-    unsigned n_list, n_ranked, n_kept;
+    unsigned some[kRanked];
+    float some_logit[kRanked];
+    unsigned n_some;
     u64 wave_u64[kWaves];
     unsigned wave_u32[kWaves];
-    float wave_max[kWaves];
+    float wave_f32[kWaves];
     // what one thread tells the others
     u64 told_weight, told_all;
-    unsigned told_bin, told_count;
+    unsigned told_bin;
 };
 
-// Where a token is in the order: larger ones come first. Keys are never zero.
-__device__ __forceinline__ u64 place_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
+// A workgroup's steps that all of its threads take together.
+struct Group {
+    Shared &s;
+    int tid, lane, wave;
+    __device__ __forceinline__ explicit Group(Shared &shared) : s(shared), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {}
+
+    __device__ __forceinline__ void begin()
+    {
+        if (tid < kExpTable) s.exps[tid] = kExps.of[tid];
+        if (tid == 0) s.n_some = 0;
+    }
+    // Sums over the wavefronts up to each, in the lanes of their numbers.
+    __device__ __forceinline__ u64 waves_to(u64 of_wave, int from_lane)
+    {
+        static_assert(kWaves == 16, "a row of lanes");
+        __syncthreads();
+        if (lane == from_lane) s.wave_u64[wave] = of_wave;
+        __syncthreads();
+        u64 x = s.wave_u64[lane & 15];
+        x += moved<0x111, 0xf>(x);
+        x += moved<0x112, 0xf>(x);
+        x += moved<0x114, 0xf>(x);
+        x += moved<0x118, 0xf>(x);
+        return x;
+    }
+    // Sum, in every thread.
+    __device__ __forceinline__ u64 sum_of(u64 x) { return of_lane(waves_to(wave_sums_to(x), 63), 15); }
+    // Sum over the threads before this one, and of all.
+    __device__ __forceinline__ u64 sum_before(u64 x, u64 *all = nullptr)
+    {
+        const u64 to = wave_sums_to(x), waves = waves_to(to, 63);
+        if (all) *all = of_lane(waves, 15);
+        return to - x + (wave > 0 ? of_lane(waves, max(wave - 1, 0)) : 0);
+    }
+    __device__ __forceinline__ float largest_of(float x)
+    {
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) x = fmaxf(x, __shfl_xor(x, o));
+        __syncthreads();
+        if (lane == 0) s.wave_f32[wave] = x;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x = fmaxf(x, s.wave_f32[w]);
+        return x;
+    }
+    __device__ __forceinline__ float sum_of_f32(float x)
+    {
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) x += __shfl_xor(x, o);
+        __syncthreads();
+        if (lane == 0) s.wave_f32[wave] = x;
+        __syncthreads();
+        x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x += s.wave_f32[w];
+        return x;
+    }
+    // Lists: `which` has a bit for each of this thread's logits that goes there; one counter's step for a wavefront's loads.
+    template <int E>
+    __device__ __forceinline__ void append(const float (&l)[E], int i, unsigned which, unsigned *n, unsigned *to, float *logits, unsigned room)
+    {
+        const u64 active = __ballot(1);
+        if (__ballot(which != 0) == 0) return;
+        unsigned at;
+        const unsigned count = (unsigned)__popc(which);
+        if (active == ~0ull) {
+            const unsigned upto = (unsigned)wave_sums_to(count);
+            unsigned first = 0;
+            if (lane == 63) first = atomicAdd(n, upto);
+            at = (unsigned)__builtin_amdgcn_readlane((int)first, 63) + upto - count;
+        } else {
+            at = count ? atomicAdd(n, count) : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (which >> e & 1) {
+                if (at < room) to[at] = (unsigned)(i + e), logits[at] = l[e];
+                ++at;
+            }
+    }
+    // Adds up in s.tile_weight what of the row's share (tid of threads) is kept: logits from `sure` on, but none that is after `border` in the order or weighs too little. Those from `from` on and below
+    // `sure` go to the list. Weights are taken where a wavefront has any: a dense list of what is kept, in LDS, took longer to write than the weights of idle lanes.
+    template <int DTYPE>
+    __device__ __forceinline__ void keep(const Row<DTYPE> &row, int tid, int threads, float sure, float from, u64 border)
+    {
+        constexpr int E = kVector<DTYPE>;
+        for_loads<DTYPE, 1>(row.at, row.V, tid, threads, [&](const float (&l)[E], int i, int n) {
+            unsigned some = 0;
+            u64 sum = 0;
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool is = e < n && l[e] >= from && l[e] >= row.least, certain = is && l[e] >= sure && place_of(key_of(l[e]), i + e) >= border;
+                some |= is && l[e] < sure ? 1u << e : 0;
+                if (__ballot(certain) == 0) continue;
+                any = true;
+                sum += certain && row.weighs(l[e]) ? row.units_of(l[e]) : 0;
+            }
+            if (any) add_to_tile(row, i, sum, s.tile_weight);
+            append(l, i, some, &s.n_some, s.some, s.some_logit, kRanked);
+        });
+        __syncthreads();
+    }
+    // The list of those from `from` on alone.
+    template <int DTYPE>
+    __device__ __forceinline__ void list_from(const Row<DTYPE> &row, int tid, int threads, float from)
+    {
+        constexpr int E = kVector<DTYPE>;
+        for_loads<DTYPE, 4>(row.at, row.V, tid, threads, [&](const float (&l)[E], int i, int n) {
+            unsigned all = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) all |= e < n && l[e] >= from ? 1u << e : 0;
+            append(l, i, all, &s.n_some, s.some, s.some_logit, kRanked);
+        });
+        __syncthreads();
+    }
+    // Which bin of s.weight a sum of `target` is reached in, and what of it is the bin's to give; kBins: none.
+    __device__ __forceinline__ unsigned bin_of_target(u64 target, u64 *in_bin)
+    {
+        const u64 w0 = s.weight[2 * tid], w1 = s.weight[2 * tid + 1], before = sum_before(w0 + w1);
+        if (tid == 0) s.told_bin = kBins;
+        __syncthreads();
+        if (before < target && target <= before + w0 + w1) {
+            const bool second = target > before + w0;
+            s.told_bin = 2 * tid + second;
+            s.told_weight = target - before - (second ? w0 : 0);
+        }
+        __syncthreads();
+        *in_bin = s.told_weight;
+        return s.told_bin;
+    }
+    // The least logit of a bin before `end`: a logit's bin never grows with it, so a search for the first finds it, 64 at a time.
+    template <int DTYPE>
+    __device__ __forceinline__ float least_of(const Row<DTYPE> &row, float per, float end) const
+    {
+        unsigned lo = key_of(-FLT_MAX), hi = key_of(row.top);   // hi is one of them, what is below lo is none
+        while (lo < hi) {
+            const unsigned step = (hi - lo) / 64 + 1, at = (unsigned)min((u64)lo + (u64)lane * step, (u64)hi);
+            const u64 is = __ballot((row.top - logit_of(at)) * per < end);
+            if (is == 0) {
+                lo += 63 * step + 1;
+                continue;
+            }
+            const int first = __ffsll((long long)is) - 1;
+            hi = (unsigned)__builtin_amdgcn_readlane((int)at, first);
+            if (first > 0) lo = (unsigned)__builtin_amdgcn_readlane((int)at, first - 1) + 1;
+            else lo = hi;
+        }
+        return logit_of(hi);
+    }
+    // What the k-th largest is not below: at least k threads' maxima reach it. NaN: there are fewer.
+    template <int DTYPE>
+    __device__ __forceinline__ float reached_by(const Row<DTYPE> &row, float mine)
+    {
+        s.count[tid] = 0;
+        const float lowest = -largest_of(-(mine == -INFINITY ? row.top : mine));
+        const float span = row.top - lowest, per = span > 0.f && span <= FLT_MAX ? 1023.f / span : 0.f;
+        if (mine != -INFINITY) atomicAdd(&s.count[(int)fminf((row.top - mine) * per, 1023.f)], 1u);
+        __syncthreads();
+        const u64 own = s.count[tid], before = sum_before(own);
+        if (tid == 0) s.told_bin = kBins;
+        __syncthreads();
+        if (before < row.k && row.k <= before + own) s.told_bin = (unsigned)tid;
+        __syncthreads();
+        const unsigned last = s.told_bin;
+        if (last >= (unsigned)kBins || !(span <= FLT_MAX)) return NAN;
+        return least_of(row, per, (float)(last + 1));
+    }
+};
+
+// The threads' maxima of a slice, and what the next launches add to.
+template <int DTYPE>
+__global__ void __launch_bounds__(kThreads) kv_sample_max_kernel(SampleParams p)
+{
+    const Row<DTYPE> row(p, blockIdx.y);
+    RowState &state = p.rows[blockIdx.y];
+    const int tid = threadIdx.x;
+    state.maxima[blockIdx.x][tid] = row.largest(blockIdx.x * kThreads + tid, p.slices * kThreads);
+    if (blockIdx.x == 0) {
+        state.tile_weight[tid] = 0;
+        if (tid == 0) state.n_some = state.fits = 0;
+    }
+}
+// The weights of a slice.
+template <int DTYPE>
+__global__ void __launch_bounds__(kThreads) kv_sample_sum_kernel(SampleParams p)
+{
+    __shared__ Shared s;
+    Row<DTYPE> row(p, blockIdx.y);
+    if (!row.nothing_cut() && !row.by_bins()) return;
+    RowState &state = p.rows[blockIdx.y];
+    Group g(s);
+    const int tid = threadIdx.x, threads = p.slices * kThreads;
+    g.begin();
+    float mine = -INFINITY;
+    for (int j = 0; j < p.slices; ++j) mine = fmaxf(mine, state.maxima[j][tid]);
+    const float top = g.largest_of(mine);
+    if (!(fabsf(top) <= FLT_MAX)) return;
+    row.set_top(top, s.exps);
+    s.weight[tid] = s.weight[kThreads + tid] = 0;
+    if (row.nothing_cut()) {
+        if (blockIdx.x == 0 && tid == 0) state.fits = 1;
+        row.sum_tiles(blockIdx.x * kThreads + tid, threads, state.tile_weight);
+        return;
+    }
+    const float per = row.bins_per_unit(g.sum_of_f32(row.sampled(tid)));
+    if (blockIdx.x == 0 && tid == 0) state.per = per;
+    if (per == 0.f) return;
+    SliceState &slice = p.slice_of[blockIdx.y * p.slices + blockIdx.x];
+    const u64 sum = g.sum_of(row.sum_and_bins(blockIdx.x * kThreads + tid, threads, per, s.weight));
+    if (tid == 0) slice.sum = sum;
+    slice.weight[tid] = s.weight[tid];
+    slice.weight[kThreads + tid] = s.weight[kThreads + tid];
+}
+// What of a slice is kept for sure, and what may be.
+template <int DTYPE>
+__global__ void __launch_bounds__(kThreads) kv_sample_keep_kernel(SampleParams p)
+{
+    __shared__ Shared s;
+    Row<DTYPE> row(p, blockIdx.y);
+    if (row.greedy || row.nothing_cut() || (row.cut_k && !row.few())) return;
+    RowState &state = p.rows[blockIdx.y];
+    Group g(s);
+    const int tid = threadIdx.x, threads = p.slices * kThreads;
+    g.begin();
+    float mine = -INFINITY;
+    for (int j = 0; j < p.slices; ++j) mine = fmaxf(mine, state.maxima[j][tid]);
+    const float top = g.largest_of(mine);
+    if (!(fabsf(top) <= FLT_MAX)) return;
+    row.set_top(top, s.exps);
+    s.tile_weight[tid] = 0;
+    float sure = INFINITY, from;
+    if (row.few()) {
+        from = g.reached_by(row, mine);
+        if (!(from == from)) return;
+    } else if (row.cut_p) {
+        const float per = state.per;
+        if (per == 0.f) return;
+        const SliceState *const slices = p.slice_of + blockIdx.y * p.slices;
+        u64 sum = 0, w[2] = {0, 0};
+        for (int j = 0; j < p.slices; ++j) {
+            w[0] += slices[j].weight[tid];
+            w[1] += slices[j].weight[kThreads + tid];
+            sum += slices[j].sum;
+        }
+        s.weight[tid] = w[0];
+        s.weight[kThreads + tid] = w[1];
+        __syncthreads();
+        u64 in_bin;
+        const unsigned bin = g.bin_of_target(row.target_of(sum), &in_bin);
+        if (bin >= (unsigned)kBins) return;
+        if (bin > 0) sure = g.least_of(row, per, (float)bin);
+        from = g.least_of(row, per, (float)bin + 1.f);
+        if (blockIdx.x == 0 && tid == 0) state.in_bin = in_bin;
+    } else {
+        sure = from = row.least;
+    }
+    if (blockIdx.x == 0 && tid == 0) state.fits = 1;
+    __syncthreads();
+    if (row.few()) g.list_from(row, blockIdx.x * kThreads + tid, threads, from);
+    else g.keep(row, blockIdx.x * kThreads + tid, threads, sure, from, 0);
+    const unsigned n = s.n_some;
+    if (tid == 0) s.told_bin = n ? atomicAdd(&state.n_some, n) : 0;
+    __syncthreads();
+    if (const unsigned to = s.told_bin + tid; (unsigned)tid < n && to < (unsigned)kRanked) {
+        state.some[to] = s.some[tid];
+        state.some_logit[to] = s.some_logit[tid];
+    }
+    if (const u64 w = s.tile_weight[tid]; w != 0) atomicAdd(&state.tile_weight[tid], w);
+}
 
 template <int DTYPE>
 __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
 {
     __shared__ Shared s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = p.a.n_vocab;
+    Group g(s);
+    const int tid = g.tid, lane = g.lane, wave = g.wave;
     const int b = blockIdx.x;
-    const char *const row = (const char *)p.a.logits + (long long)b * p.a.stride * (DTYPE == KV_F32 ? 4 : 2);
+    Row<DTYPE> row(p, b);
+    const RowState *const state = p.rows ? p.rows + b : nullptr;
+    const int V = row.V;
+    const float T = row.T;
+    const unsigned k = row.k;
     auto answer = [&](int token, float prob) {
         p.a.tokens[b] = token;
         if (p.a.probs) p.a.probs[b] = prob;
     };
-    // Sum over the workgroup, in every thread.
-    auto sum_of = [&](u64 x) {
-        x = wave_sum(x);
-        __syncthreads();
-        if (lane == 0) s.wave_u64[wave] = x;
-        __syncthreads();
-        u64 all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += s.wave_u64[w];
-        return all;
-    };
-    // Sum over the threads before this one.
-    auto sum_before = [&](u64 x) {
-        const u64 to = wave_sums_to(x, lane);
-        __syncthreads();
-        if (lane == 63) s.wave_u64[wave] = to;
-        __syncthreads();
-        u64 before = to - x;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) before += w < wave ? s.wave_u64[w] : 0;
-        return before;
-    };
-
-    const float T = p.a.temperature ? p.a.temperature[b] : 1.f;
-    const bool greedy = !(T > 0.f);
-    const int k_asked = greedy ? 1 : p.a.top_k ? p.a.top_k[b] : 0;
-    const unsigned k = k_asked <= 0 || k_asked > V ? (unsigned)V : (unsigned)k_asked;
-    const bool cut_k = k < (unsigned)V;
-    const float top_p = greedy || !p.a.top_p ? 1.f : p.a.top_p[b];
-    const float min_p = greedy || !p.a.min_p ? 0.f : fminf(p.a.min_p[b], 1.f);
-    const bool cut_p = top_p < 1.f;
     float u = p.a.u[b];
     u = u > 0.f ? u : 0.f;
 
-    // The largest logit, its first index, and this thread's own; a NaN or +infinity makes it +infinity.
-    if (tid < kExpTable) s.exps[tid] = exp2((double)tid / kExpTable);
-    if (tid == 0) s.n_list = s.n_ranked = s.n_kept = 0;
-    float top = -INFINITY, mine;
-    for_logits<DTYPE>(row, V, tid, [&](float x, int) { top = x <= FLT_MAX ? fmaxf(top, x) : INFINITY; });
-    mine = top;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
-    if (lane == 0) s.wave_max[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s.wave_max[w]);
+    // The largest logit, and this thread's own; a NaN or +infinity makes it +infinity.
+    g.begin();
+    float mine = -INFINITY;
+    if (state) {
+        for (int j = 0; j < p.slices; ++j) mine = fmaxf(mine, state->maxima[j][tid]);
+    } else {
+        mine = row.largest(tid, kThreads);
+    }
+    const float top = g.largest_of(mine);
     if (!(fabsf(top) <= FLT_MAX)) {
         if (tid == 0) answer(-1, 0.f);
         return;
     }
-
-    // exp((l - max) / T) = 2^(n / 256 + g / 256) with |g| <= 1/2: a table, and e^(g ln 2 / 256) by its series (the next term is below 2^-54). What is below 2^-60 has no weight.
-    const double per_unit = greedy ? 0. : 1.4426950408889634 * kExpTable / (double)T, top64 = top;
-    auto scaled_weight = [&](float x, int shift) -> double {
-        constexpr double c = 0.6931471805599453 / kExpTable;
-        const double y = fmax(((double)x - top64) * per_unit, -60. * kExpTable);
-        const double n = rint(y), g = y - n;
-        const int at = (int)n;
-        const double e = fma(g, fma(g, fma(g, fma(g, c * c * c * c / 24, c * c * c / 6), c * c / 2), c), 1.);
-        return ldexp(s.exps[at & (kExpTable - 1)] * e, (at >> 8) + shift);
-        static_assert(kExpTable == 256, "8 bits");
-    };
-    auto weight_of = [&](float x) { return x == -INFINITY ? 0. : scaled_weight(x, 0); };
-    // to the nearest integer by adding 2^52, whose lowest bit is worth one
-    auto units_of = [&](float x) { return x == -INFINITY ? 0 : (u64)__double_as_longlong(scaled_weight(x, p.shift) + 4503599627370496.) & 0xfffffffffffffull; };
+    row.set_top(top, s.exps);
+    s.tile_weight[tid] = 0;
 
     // The border: kept is what is not after it in the order (and weighs enough).
     u64 border = 0;
-    // Tiles begin where loads of 16 bytes do; what is before that is of the first.
-    const int before_loads = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / (DTYPE == KV_F32 ? 4 : 2)), n_tiles = max(1, ((V - before_loads - 1) >> p.tile) + 1);
-    auto tile_of = [&](int i) { return max(0, i - before_loads) >> p.tile; };
-    auto tile_begin = [&](int t) { return t == 0 ? 0 : before_loads + (t << p.tile); };
-    auto tile_end = [&](int t) { return min(V, before_loads + ((t + 1) << p.tile)); };
     auto pick = [&] {   // tile_weight holds the sums of what is kept
         __syncthreads();
-        const u64 own = tid < n_tiles ? s.tile_weight[tid] : 0, before = sum_before(own);
-        u64 all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += s.wave_u64[w];
+        u64 all;
+        const u64 own = tid < row.n_tiles ? s.tile_weight[tid] : 0, before = g.sum_before(own, &all);
         const double at = (double)u * (double)all;
         const u64 target = min((u64)at, all - 1);   // the largest has a weight: all > 0
         if (before <= target && target < before + own) {
@@ -226,46 +656,38 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             s.told_weight = before;
         }
         __syncthreads();
-        if (wave != 0) return;
-        const int t = (int)s.told_bin, end = tile_end(t);
+        // a thread a token
+        const int t = (int)s.told_bin, end = row.tile_end(t);
         u64 sum = s.told_weight;
-        for (int i0 = tile_begin(t); i0 < end; i0 += 64) {
-            const int i = i0 + lane;
-            const float x = i < end ? logit_at<DTYPE>(row, i) : -INFINITY;
-            const bool in = i < end && place_of(key_of(x), i) >= border && weight_of(x) >= (double)min_p;
-            const u64 to = sum + wave_sums_to(in ? units_of(x) : 0, lane);
-            const u64 hit = __ballot(to > target);
-            if (hit != 0) {
-                if (lane == __ffsll((long long)hit) - 1) answer(i, (float)(scaled_weight(x, p.shift) / (double)all));
-                return;
-            }
-            sum = __shfl(to, 63);
+        for (int i0 = row.tile_begin(t); i0 < end; i0 += kThreads) {
+            const int i = i0 + tid;
+            const float x = i < end ? logit_at<DTYPE>(row.at, i) : -INFINITY;
+            const u64 w = i < end && place_of(key_of(x), i) >= border && row.weighs(x) ? row.units_of(x) : 0;
+            u64 here;
+            const u64 from = sum + g.sum_before(w, &here);
+            if (from <= target && target < from + w) answer(i, (float)(row.scaled_weight(x, p.shift) / (double)all));
+            sum += here;
+            if (sum > target) return;
         }
     };
-    auto clear_tiles = [&] { s.tile_weight[tid] = 0; };
     static_assert(kTiles == kThreads, "a tile each");
-    // Adds a token for sure kept to the list, for all lanes at once; false: no room.
-    auto append = [&](bool is, unsigned value, unsigned *n, unsigned *to, unsigned room) {
-        const u64 some = __ballot(is);
-        if (some == 0) return;
-        unsigned at = 0;
-        if (lane == __ffsll((long long)some) - 1) at = atomicAdd(n, (unsigned)__popcll(some));
-        at = (unsigned)__shfl((int)at, __ffsll((long long)some) - 1) + (unsigned)__popcll(some & ((1ull << lane) - 1));
-        if (is && at < room) to[at] = value;
-    };
-    // s.ranked[0 .. n) and weights: the sum of weights (or the number) before each in the order
+    // Of s.ranked[0 .. n): the sum of weights, or the number, before each in the order.
     auto before_in_order = [&](int n, auto by_weight) {
         u64 before = 0;
         if (tid < n) {
             const u64 own = s.ranked[tid];
-            for (int j = 0; j < n; ++j) before += s.ranked[j] > own ? (decltype(by_weight)::value ? s.ranked_weight[j] : 1) : 0;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) {
+                const u64 place = s.ranked[j], w = decltype(by_weight)::value ? s.ranked_weight[j] : 1;   // both loaded, whatever the one says
+                before += place > own ? w : 0;
+            }
         }
         return before;
     };
 
-    if (greedy) {   // the first of the largest
+    if (row.greedy) {   // the first of the largest
         int at = INT_MAX;
-        if (mine == top) for_logits<DTYPE>(row, V, tid, [&](float x, int i) { at = x == top ? min(at, i) : at; });
+        if (mine == top) for_logits<DTYPE>(row.at, V, tid, [&](float x, int i) { at = x == top ? min(at, i) : at; });
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) at = min(at, __shfl_xor(at, o));
         if (lane == 0) s.wave_u64[wave] = (u64)at;
@@ -276,205 +698,81 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
         }
         return;
     }
-    // a logit that weighs min_p, less some units of its own rounding: what is below is not kept
-    float least = min_p > 0.f ? (float)((double)top + log((double)min_p) * (double)T) - 1.0e-5f * (fabsf(top) + 1.f) - 1.0e-5f * T : -INFINITY;
-    if (!(least == least)) least = -INFINITY;
 
-    if (!cut_k && !cut_p && !(min_p > 0.f)) {   // nothing is cut off
-        clear_tiles();
+    // What is kept for sure, in s.tile_weight, and what may be: s.some
+    bool fits = false;
+    u64 in_bin = 0;
+    if (state) {
+        fits = state->fits != 0 && state->n_some <= (unsigned)kRanked;
+        if (fits) {
+            s.tile_weight[tid] = state->tile_weight[tid];
+            if (tid < (int)state->n_some) s.some[tid] = state->some[tid], s.some_logit[tid] = state->some_logit[tid];
+            if (tid == 0) s.n_some = state->n_some;
+            in_bin = state->in_bin;
+        }
+    } else if (row.nothing_cut()) {
         __syncthreads();
-        u64 sum = 0;
-        for_logits<DTYPE>(
-            row, V, tid, [&](float x, int) { sum += units_of(x); },
-            [&](int i) {
-                if (__ballot(1) == ~0ull) {   // 64 loads side by side are of one tile
-                    sum = wave_sum(sum);
-                    if (lane == 0) atomicAdd(&s.tile_weight[tile_of(i)], sum);
-                } else {
-                    atomicAdd(&s.tile_weight[tile_of(i)], sum);
+        row.sum_tiles(tid, kThreads, s.tile_weight);
+        fits = true;
+    } else if (row.few() || row.cut_p == false || row.by_bins()) {
+        float sure = INFINITY, from = NAN;
+        if (row.few()) {
+            from = g.reached_by(row, mine);
+        } else if (row.by_bins()) {
+            s.weight[tid] = s.weight[kThreads + tid] = 0;
+            const float per = row.bins_per_unit(g.sum_of_f32(row.sampled(tid)));
+            if (per != 0.f) {
+                const u64 sum = g.sum_of(row.sum_and_bins(tid, kThreads, per, s.weight));
+                const unsigned bin = g.bin_of_target(row.target_of(sum), &in_bin);
+                if (bin < (unsigned)kBins) {
+                    if (bin > 0) sure = g.least_of(row, per, (float)bin);
+                    from = g.least_of(row, per, (float)bin + 1.f);
                 }
-                sum = 0;
-            });
+            }
+        } else if (!row.cut_k) {
+            sure = from = row.least;
+        }
+        if (from == from) {
+            __syncthreads();
+            if (row.few()) g.list_from(row, tid, kThreads, from);
+            else g.keep(row, tid, kThreads, sure, from, 0);
+            fits = s.n_some <= (unsigned)kRanked;
+        }
+    }
+    if (fits) {
+        __syncthreads();
+        const int n = (int)s.n_some;
+        const float x = tid < n ? s.some_logit[tid] : 0.f;
+        if (tid < n) {
+            s.ranked[tid] = place_of(key_of(x), (int)s.some[tid]);
+            s.ranked_weight[tid] = row.units_of(x);
+        }
+        if (tid == 0) s.told_all = n > 0 ? ~0ull : 0;
+        __syncthreads();
+        bool in = tid < n;
+        if (row.few()) {
+            in = in && before_in_order(n, std::false_type{}) < k;
+            if (row.cut_p) {
+                // weights of what the first cut leaves out do not count
+                __syncthreads();
+                if (tid < n && !in) s.ranked_weight[tid] = 0;
+                __syncthreads();
+                const u64 target = row.target_of(g.sum_of(in ? s.ranked_weight[tid] : 0));
+                in = in && before_in_order(n, std::true_type{}) < target;
+            }
+        } else {
+            in = in && before_in_order(n, std::true_type{}) < in_bin;
+        }
+        if (in) {
+            atomicMin(&s.told_all, s.ranked[tid]);
+            if (row.weighs(x)) atomicAdd(&s.tile_weight[row.tile_of((int)s.some[tid])], s.ranked_weight[tid]);
+        }
+        __syncthreads();
+        border = s.told_all;
         pick();
         return;
     }
-
-    if (cut_k && k <= 256) {
-        // at least k threads' maxima reach the lower end of the bin with the k-th of them
-        s.count[tid] = 0;
-        float lowest = mine == -INFINITY ? top : mine;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) lowest = fminf(lowest, __shfl_xor(lowest, o));
-        __syncthreads();
-        if (lane == 0) s.wave_max[wave] = lowest;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) lowest = fminf(lowest, s.wave_max[w]);
-        const float span = top - lowest, per = span > 0.f && span <= FLT_MAX ? 1023.f / span : 0.f;
-        const int bin = mine == -INFINITY ? -1 : (int)fminf((top - mine) * per, 1023.f);
-        if (bin >= 0) atomicAdd(&s.count[bin], 1u);
-        __syncthreads();
-        const u64 own = s.count[tid], before = sum_before(own);
-        if (tid == 0) s.told_bin = kBins;
-        __syncthreads();
-        if (before < k && k <= before + own) s.told_bin = (unsigned)tid;
-        __syncthreads();
-        const unsigned last = s.told_bin;
-        // by the same arithmetic as the bins: what is in one of the first `last` + 1
-        auto reaches = [&](float x) { return x != -INFINITY && (top - x) * per < (float)(last + 1); };
-        if (last < (unsigned)kBins && span <= FLT_MAX) {
-            for_logits<DTYPE>(row, V, tid, [&](float x, int i) {
-                if (__any(reaches(x))) append(reaches(x), (unsigned)i, &s.n_list, s.list, kList);
-            });
-            __syncthreads();
-            const int n = (int)s.n_list;
-            if (n <= kRanked) {
-                float x = 0.f;
-                if (tid < n) {
-                    x = logit_at<DTYPE>(row, (long long)s.list[tid]);
-                    s.ranked[tid] = place_of(key_of(x), (int)s.list[tid]);
-                    s.ranked_weight[tid] = units_of(x);
-                }
-                __syncthreads();
-                const u64 rank = before_in_order(n, std::false_type{});
-                bool in = tid < n && rank < k;
-                if (cut_p) {
-                    // weights of what the first cut leaves out do not count
-                    __syncthreads();
-                    if (tid < n && !in) s.ranked_weight[tid] = 0;
-                    __syncthreads();
-                    const u64 sum = sum_of(in ? s.ranked_weight[tid] : 0);
-                    const double want = ceil((double)(top_p > 0.f ? top_p : 0.f) * (double)sum);
-                    const u64 target = max((u64)1, min((u64)want, sum));
-                    in = in && before_in_order(n, std::true_type{}) < target;
-                }
-                in = in && weight_of(x) >= (double)min_p;
-                clear_tiles();
-                if (tid == 0) s.told_all = ~0ull;
-                __syncthreads();
-                if (in) {
-                    atomicAdd(&s.tile_weight[tile_of((int)s.list[tid])], s.ranked_weight[tid]);
-                    atomicMin(&s.told_all, s.ranked[tid]);
-                }
-                __syncthreads();
-                border = s.told_all;
-                pick();
-                return;
-            }
-            __syncthreads();
-            if (tid == 0) s.n_list = 0;
-        }
-        __syncthreads();
-    }
-
-    if (!cut_k && cut_p) {
-        // Weights of every 1024th of the row give about the sum; the largest alone is 1.
-        float sample = 0.f;
-        const int take = min(V, 8 * kThreads);
-        for (int j = 0; j < 8; ++j) {
-            const int i = j * kThreads + tid;
-            if (i < take) sample += __expf((logit_at<DTYPE>(row, (long long)i * V / take) - top) / T);
-        }
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) sample += __shfl_xor(sample, o);
-        __syncthreads();
-        if (lane == 0) s.wave_max[wave] = sample;
-        s.count[tid] = s.count[kThreads + tid] = 0;
-        s.weight[tid] = s.weight[kThreads + tid] = 0;
-        __syncthreads();
-        sample = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) sample += s.wave_max[w];
-        sample = fmaxf(1.f, sample * (float)V / (float)take);
-        // down to a quarter of what is looked for, in bins
-        const float reach = fminf(T * __logf(4.f * (float)V / ((1.f - fmaxf(top_p, 0.f)) * sample)), T * 42.f), per = (float)kBins / reach;
-        u64 sum = 0;
-        if (reach > 0.f && reach <= FLT_MAX && per <= FLT_MAX) {
-            for_logits<DTYPE>(row, V, tid, [&](float x, int) {
-                const u64 w = units_of(x);
-                sum += w;
-                const float bin = (top - x) * per;
-                if (bin < (float)kBins) {
-                    atomicAdd(&s.count[(int)bin], 1u);
-                    atomicAdd(&s.weight[(int)bin], w);
-                }
-            });
-            sum = sum_of(sum);
-            const double want = ceil((double)(top_p > 0.f ? top_p : 0.f) * (double)sum);
-            const u64 target = max((u64)1, min((u64)want, sum));
-            const u64 w0 = s.weight[2 * tid], w1 = s.weight[2 * tid + 1], before = sum_before(w0 + w1);
-            if (tid == 0) s.told_bin = kBins;
-            const u64 counts = (u64)s.count[2 * tid] + s.count[2 * tid + 1], counts_before = sum_before(counts);
-            if (before < target && target <= before + w0 + w1) {
-                const bool second = target > before + w0;
-                s.told_bin = 2 * tid + second;
-                s.told_weight = target - before - (second ? w0 : 0);   // of the bin itself
-                s.told_count = (unsigned)min(counts_before + (second ? s.count[2 * tid] : 0), (u64)UINT_MAX);
-            }
-            __syncthreads();
-            const unsigned bin = s.told_bin;
-            const u64 in_bin = s.told_weight;
-            if (bin < (unsigned)kBins && s.count[bin] <= (unsigned)kRanked && s.told_count <= (unsigned)kList) {
-                const float from = (float)bin;
-                for_logits<DTYPE>(row, V, tid, [&](float x, int i) {
-                    const float at = (top - x) * per;
-                    const bool sure = at < from && x >= least, maybe = at >= from && at < from + 1.f;
-                    if (!__any(sure || maybe)) return;
-                    append(sure, (unsigned)i, &s.n_list, s.list, kList);
-                    append(maybe, (unsigned)i, &s.n_ranked, (unsigned *)s.ranked_weight + kRanked, kRanked);
-                });
-                __syncthreads();
-                const int n = (int)s.n_ranked, n_sure = (int)s.n_list;
-                unsigned i = 0;
-                float x = 0.f;
-                u64 w = 0;
-                if (tid < n) {
-                    i = ((unsigned *)s.ranked_weight)[kRanked + tid];
-                    x = logit_at<DTYPE>(row, (long long)i);
-                    w = units_of(x);
-                    s.ranked[tid] = place_of(key_of(x), (int)i);
-                }
-                clear_tiles();
-                if (tid == 0) s.told_all = ~0ull;
-                __syncthreads();
-                if (tid < n) s.ranked_weight[tid] = w;
-                __syncthreads();
-                if (tid < n && before_in_order(n, std::true_type{}) < in_bin) {
-                    atomicMin(&s.told_all, s.ranked[tid]);
-                    if (weight_of(x) >= (double)min_p) atomicAdd(&s.tile_weight[tile_of((int)i)], w);
-                }
-                for (int j = tid; j < n_sure; j += kThreads) {
-                    const unsigned at = s.list[j];
-                    const float y = logit_at<DTYPE>(row, (long long)at);
-                    if (weight_of(y) >= (double)min_p) atomicAdd(&s.tile_weight[tile_of((int)at)], units_of(y));
-                }
-                __syncthreads();
-                border = s.told_all;
-                pick();
-                return;
-            }
-        }
-        __syncthreads();
-    }
-
-    if (!cut_k && !cut_p) {   // min_p alone
-        for_logits<DTYPE>(row, V, tid, [&](float x, int i) {
-            if (__any(x >= least)) append(x >= least, (unsigned)i, &s.n_list, s.list, kList);
-        });
-        clear_tiles();
-        __syncthreads();
-        const int n = (int)s.n_list;
-        if (n <= kList) {
-            for (int j = tid; j < n; j += kThreads) {
-                const unsigned at = s.list[j];
-                const float y = logit_at<DTYPE>(row, (long long)at);
-                if (weight_of(y) >= (double)min_p) atomicAdd(&s.tile_weight[tile_of((int)at)], units_of(y));
-            }
-            pick();
-            return;
-        }
-        __syncthreads();
-    }
+    __syncthreads();
 
     // Anything: the key at which a count, or a sum of weights, is reached, going down: histograms over bins of falling keys, whose bin with the border becomes the next range. All keys above
     // `border_key` are kept, and of those that equal it the first `ties`.
@@ -497,17 +795,17 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             __syncthreads();
             for (int i = tid; i < kBins; i += kThreads) s.weight[i] = 0, s.count[i] = 0;
             __syncthreads();
-            for_logits<DTYPE>(row, V, tid, [&](float x, int) {
+            for_logits<DTYPE>(row.at, V, tid, [&](float x, int) {
                 const unsigned key = key_of(x);
                 if (key < low || key > high) return;
                 const unsigned at = bin_of(x, key);
                 atomicAdd(&s.count[at], 1u);
-                atomicAdd(&s.weight[at], units_of(x));
+                atomicAdd(&s.weight[at], row.units_of(x));
             });
             __syncthreads();
             // sums before each bin: a thread has two
             const u64 c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1], w0 = s.weight[2 * tid], w1 = s.weight[2 * tid + 1];
-            const u64 counts = above + sum_before(c0 + c1), weights = above_weight + sum_before(w0 + w1);
+            const u64 counts = above + g.sum_before(c0 + c1), weights = above_weight + g.sum_before(w0 + w1);
             const u64 before = W ? weights : counts, first = W ? w0 : c0, both = W ? w0 + w1 : c0 + c1;
             if (tid == 0) s.told_bin = kBins;
             __syncthreads();
@@ -527,7 +825,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             if (by_distance) {
                 // the keys that are in the bin
                 unsigned least_key = ~0u, most_key = 0;
-                for_logits<DTYPE>(row, V, tid, [&](float x, int) {
+                for_logits<DTYPE>(row.at, V, tid, [&](float x, int) {
                     const unsigned key = key_of(x);
                     if (key >= low && key <= high && bin_of(x, key) == bin) least_key = min(least_key, key), most_key = max(most_key, key);
                 });
@@ -556,77 +854,78 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             }
         }
     };
-    if (cut_k) find_border(std::false_type{}, (u64)k, 0u);
-    if (cut_p) {
-        if (!cut_k) {   // the sum of all
+    if (row.cut_k) find_border(std::false_type{}, (u64)k, 0u);
+    if (row.cut_p) {
+        if (!row.cut_k) {   // the sum of all
             u64 sum = 0;
-            for_logits<DTYPE>(row, V, tid, [&](float x, int) { sum += units_of(x); });
-            kept = sum_of(sum);
+            for_logits<DTYPE>(row.at, V, tid, [&](float x, int) { sum += row.units_of(x); });
+            kept = g.sum_of(sum);
         }
         // no more than the top-k's keys; what of its border's key is past k counts in no sum before the target, which is at most theirs
-        const double want = ceil((double)(top_p > 0.f ? top_p : 0.f) * (double)kept);
-        const u64 target = max((u64)1, min((u64)want, kept));
+        const u64 target = row.target_of(kept);
         const unsigned k_border = border_key, k_ties = ties;
         find_border(std::true_type{}, target, border_key);
-        if (border_key == k_border && cut_k) ties = min(ties, k_ties);
+        if (border_key == k_border && row.cut_k) ties = min(ties, k_ties);
     }
 
-    // Tiles: sums of what is above the border's key, and how many have it; the last of these that is kept is the border.
+    // Tiles: how many have the border's key; the last of these that is kept is the border.
+    if (border_key != 0) {
+        __syncthreads();
+        s.count[tid] = 0;
+        if (tid == 0) s.told_all = 0;
+        __syncthreads();
+        for_logits<DTYPE>(row.at, V, tid, [&](float x, int i) {
+            if (key_of(x) == border_key) atomicAdd(&s.count[row.tile_of(i)], 1u);
+        });
+        __syncthreads();
+        const u64 equal = s.count[tid], before = g.sum_before(equal);
+        if (before < ties && before + equal >= ties) s.told_all = (u64)(ties - before) << 32 | (unsigned)tid;   // the last one is in this tile
+        __syncthreads();
+        border = place_of(border_key, INT_MAX);
+        if (s.told_all != 0) {
+            // every wavefront for itself
+            unsigned left = (unsigned)(s.told_all >> 32);
+            const int t = (int)(unsigned)s.told_all, end = row.tile_end(t);
+            for (int i0 = row.tile_begin(t); i0 < end; i0 += 64) {
+                const int i = i0 + lane;
+                u64 is = __ballot(i < end && key_of(logit_at<DTYPE>(row.at, min(i, end - 1))) == border_key);
+                const unsigned n = (unsigned)__popcll(is);
+                if (n >= left) {
+                    for (; left > 1; --left) is &= is - 1;
+                    border = place_of(border_key, i0 + __ffsll((long long)is) - 1);
+                    break;
+                }
+                left -= n;
+            }
+        }
+    }
     __syncthreads();
-    s.count[tid] = 0;
     s.tile_weight[tid] = 0;
     __syncthreads();
-    for (int t = wave; t < n_tiles; t += kWaves) {
-        u64 sum = 0;
-        unsigned equal = 0;
-        const int end = tile_end(t);
-        for (int i = tile_begin(t) + lane; i < end; i += 64) {
-            const float x = logit_at<DTYPE>(row, i);
-            const unsigned key = key_of(x);
-            if (key > border_key && x >= least && weight_of(x) >= (double)min_p) sum += units_of(x);
-            equal += key == border_key;
-        }
-        sum = wave_sum(sum);
-        equal = (unsigned)wave_sum(equal);
-        if (lane == 0) s.tile_weight[t] = sum, s.count[t] = equal;
-    }
-    __syncthreads();
-    const float border_logit = __uint_as_float(border_key >> 31 ? border_key & 0x7fffffffu : ~border_key);
-    const u64 each = border_key != 0 && weight_of(border_logit) >= (double)min_p ? units_of(border_logit) : 0;
-    const u64 equal = s.count[tid], equal_before = sum_before(equal), taken = equal_before >= ties ? 0 : min(equal, ties - equal_before);
-    s.tile_weight[tid] += taken * each;
-    if (tid == 0) s.told_all = 0;
-    __syncthreads();
-    if (border_key != 0 && equal_before < ties && equal_before + equal >= ties) s.told_all = (u64)(ties - equal_before) << 32 | (unsigned)tid;   // the last one is in this tile
-    __syncthreads();
-    if (s.told_all != 0) {
-        // every wavefront for itself
-        unsigned left = (unsigned)(s.told_all >> 32);
-        const int t = (int)(unsigned)s.told_all, end = tile_end(t);
-        for (int i0 = tile_begin(t); i0 < end; i0 += 64) {
-            const int i = i0 + lane;
-            u64 is = __ballot(i < end && key_of(logit_at<DTYPE>(row, min(i, end - 1))) == border_key);
-            const unsigned n = (unsigned)__popcll(is);
-            if (n >= left) {
-                for (; left > 1; --left) is &= is - 1;
-                border = place_of(border_key, i0 + __ffsll((long long)is) - 1);
-                break;
-            }
-            left -= n;
-        }
-    } else if (border_key != 0) {
-        border = place_of(border_key, INT_MAX);
-    }
-    __syncthreads();
+    const float from = border_key != 0 ? logit_of(border_key) : -FLT_MAX;
+    g.keep(row, tid, kThreads, from, from, border);
     pick();
 }
 
 }  // namespace
 
+static int slices_of(int n_rows, int n_vocab)
+{
+    // 128 rows fill half of the card by themselves; short rows are over before another launch has begun
+    if (n_rows < 1 || n_rows >= 128 || n_vocab <= 65536) return 1;
+    int slices = kMostSlices;   // a power of two: equal shares of a row's threads
+    while (slices * n_rows > 256) slices /= 2;
+    return slices;
+}
+
 extern "C" size_t kv_sample_workspace(int n_rows, int n_vocab)
 {
     if (n_rows < 0 || n_vocab < 0) return 0;
-    return 16;
+    // what fewer rows need as well: they may be shared by more slices
+    size_t most = 16;
+    for (int n = 1; n <= std::min(n_rows, 127); ++n)
+        if (const int slices = slices_of(n, n_vocab); slices > 1) most = std::max(most, n * (sizeof(RowState) + slices * sizeof(SliceState)));
+    return most;
 }
 
 extern "C" int kv_sample(const kv_sample_args_t *a, void *workspace, size_t ws_bytes, void *hip_stream)
@@ -645,8 +944,18 @@ extern "C" int kv_sample(const kv_sample_args_t *a, void *workspace, size_t ws_b
     p.shift = std::min(51, 62 - bits);
     p.tile = 9;
     while (((a->n_vocab - 1) >> p.tile) >= kTiles) ++p.tile;
-    (void)launch_kernel(a->dtype == KV_F32 ? kv_sample_kernel<KV_F32> : a->dtype == KV_F16 ? kv_sample_kernel<KV_F16> : kv_sample_kernel<KV_BF16>, dim3((unsigned)a->n_rows),
-                        dim3(kThreads), (hipStream_t)hip_stream, p);
+    p.slices = slices_of(a->n_rows, a->n_vocab);
+    p.rows = p.slices > 1 ? (RowState *)workspace : nullptr;
+    p.slice_of = (SliceState *)((RowState *)workspace + a->n_rows);
+    auto of = [&](auto f32, auto f16, auto bf16) { return a->dtype == KV_F32 ? f32 : a->dtype == KV_F16 ? f16 : bf16; };
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (p.rows) {
+        const dim3 grid((unsigned)p.slices, (unsigned)a->n_rows), block(kThreads);
+        (void)launch_kernel(of(kv_sample_max_kernel<KV_F32>, kv_sample_max_kernel<KV_F16>, kv_sample_max_kernel<KV_BF16>), grid, block, st, p);
+        (void)launch_kernel(of(kv_sample_sum_kernel<KV_F32>, kv_sample_sum_kernel<KV_F16>, kv_sample_sum_kernel<KV_BF16>), grid, block, st, p);
+        if (a->top_p || a->top_k || a->min_p) (void)launch_kernel(of(kv_sample_keep_kernel<KV_F32>, kv_sample_keep_kernel<KV_F16>, kv_sample_keep_kernel<KV_BF16>), grid, block, st, p);
+    }
+    (void)launch_kernel(of(kv_sample_kernel<KV_F32>, kv_sample_kernel<KV_F16>, kv_sample_kernel<KV_BF16>), dim3((unsigned)a->n_rows), dim3(kThreads), st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     return KV_OK;
