@@ -17,9 +17,9 @@ struct GroupUnit {
     bool prefix;
 };
 struct GroupCut {
-    int nb;                        // 16-row groups of a workgroup
+    int nb, nb_prefix;                // 16-row groups of a workgroup, and of a prefix' workgroup: as many, or the most where the others have one
     int prefix_tokens, split_tokens;  // of a split, multiples of 32
-    int prefix_ns, ns;             // partial results of a row: of its prefix, and in all
+    int prefix_ns, ns;                // partial results of a row: of its prefix, and in all
 };
 
 inline int splits_of(int span, int split_tokens) { return span <= 0 ? 0 : (span - 1) / split_tokens + 1; }
@@ -52,12 +52,13 @@ inline uint64_t group_workspace_bytes(const TreeShape &s, long long n_tok, long 
 inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, bool chain, int n_splits, uint64_t ws_bytes, long long n_tok)
 {
     int longest = 0, longest_prefix = 0;
-    long long rows = 0;
+    long long rows = 0, prefix_rows = 0;
     double context = 0;
     for (int i = 0; i < n; ++i) {
         if (units[i].tokens <= 0 || units[i].span <= 0) continue;
         (units[i].prefix ? longest_prefix : longest) = std::max(units[i].prefix ? longest_prefix : longest, units[i].span);
         rows = std::max(rows, (long long)units[i].tokens * s.G);
+        if (units[i].prefix) prefix_rows = std::max(prefix_rows, (long long)units[i].tokens * s.G);
         context += units[i].span;
     }
     const uint64_t fit = ws_bytes / tree_split_bytes(s, n_tok);
@@ -75,24 +76,28 @@ inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, boo
     for (int ns = only > 0 ? only : 1; ns <= kMaxTreeSplits; ns = next_splits(ns)) {
         if (results_of(ns) > most) break;
         const int st = tokens_of(ns), of_prefix = splits_of(longest_prefix, st), of_own = splits_of(longest, st);
-        for (int k = 0; k < (s.D == 256 ? 2 : 3); ++k) {
-            const int nb = 1 << k;
-            if (k > 0 && rows <= 8 * nb) break;   // half of the rows would be none
-            const double step = 0.95 + 0.18 * nb * s.D / 128 * (s.D == 256 ? 1.4 : 1) + (s.paged ? 0.05 : 0), start = 2.6 + 0.6 * nb;
-            double groups = 0, work = 0, parts = 0;
+        const int most_nb = s.D == 256 ? 2 : 4;
+        for (int k = 0; k < 4; ++k) {   // 1, 2, 4 of both; the most of prefixes alone
+            const int nb = k == 3 ? 1 : 1 << k, nb_prefix = k == 3 ? most_nb : nb;
+            if (nb > most_nb || (k == 3 && longest_prefix == 0)) continue;
+            if (k > 0 && (k == 3 ? prefix_rows : rows) <= 8 * nb_prefix) continue;   // half of the rows would be none
+            auto step = [&](int n) { return 0.95 + 0.18 * n * s.D / 128 * (s.D == 256 ? 1.4 : 1) + (s.paged ? 0.05 : 0); };
+            double groups = 0, work = 0, parts = 0, longest_one = 0;
             for (int i = 0; i < n; ++i) {
                 if (units[i].tokens <= 0 || units[i].span <= 0) continue;
-                const double blocks = std::ceil((double)units[i].tokens * s.G / (16 * nb)), splits = splits_of(units[i].span, st);
+                const int mine = units[i].prefix ? nb_prefix : nb;
+                const double start = 2.6 + 0.6 * mine, blocks = std::ceil((double)units[i].tokens * s.G / (16 * mine)), splits = splits_of(units[i].span, st);
                 const double seen = !units[i].prefix && chain ? units[i].span - 0.5 * units[i].tokens : units[i].span;
                 groups += blocks * splits * s.H;
-                work += blocks * s.H * (splits * start + seen / 128 * step);
+                work += blocks * s.H * (splits * start + seen / 128 * step(mine));
                 parts += units[i].tokens * splits;
+                longest_one = std::max(longest_one, start + std::min(st, units[i].span) / 128.0 * step(mine));
             }
-            const double one = start + std::min(st, span) / 128.0 * step;
-            const double us = std::max({hbm + 1.06 * start, groups > s.cus ? 1.45 * one : one, work / (s.cus * 1.4)}) + (of_prefix + of_own > 1 ? 3.9 + parts * part + 0.03 * (of_prefix + of_own) : 0);
+            const double us = std::max({hbm + 3.4, groups > s.cus ? 1.45 * longest_one : longest_one, work / (s.cus * 1.4)}) +
+                              (of_prefix + of_own > 1 ? 3.9 + parts * part + 0.03 * (of_prefix + of_own) : 0);
             if (us < least) {
                 least = us;
-                best = GroupCut{nb, st, st, of_prefix, of_prefix + of_own};
+                best = GroupCut{nb, nb_prefix, st, st, of_prefix, of_prefix + of_own};
             }
         }
         if (only > 0) break;

@@ -140,14 +140,14 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
     t.bt_shift = -1;
     if (t.c.table && (t.c.bt & (t.c.bt - 1)) == 0) t.bt_shift = __builtin_ctz((unsigned)t.c.bt);
     uint64_t workgroups = 0;
-    for (int i = 0; i < n_units; ++i) workgroups += unit_workgroups(shape, units[i], cut.nb, units[i].prefix ? cut.prefix_tokens : cut.split_tokens);
+    for (int i = 0; i < n_units; ++i) workgroups += unit_workgroups(shape, units[i], units[i].prefix ? cut.nb_prefix : cut.nb, units[i].prefix ? cut.prefix_tokens : cut.split_tokens);
     if (workgroups * kTreeThreads >= 1ull << 32) return KV_ERANGE;   // threads of a launch
     auto over = [](int d) { return (unsigned)(((1ull << 32) + d - 1) / d); };
     t.by_g = over(t.G); t.by_h = over(p->H); t.by_split = over(cut.split_tokens); t.by_prefix = over(cut.prefix_tokens);
     t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < (1ull << 32) / (uint64_t)t.c.bt
                           : t.c.ss < 1ull << 25 && t.c.zs < 1ull << 25;
     t.dense = t.c.ss == (uint64_t)p->D * format_bits(format) / 8;
-    GroupKernel k = (format == KV_FORMAT_FP8 ? group_kernel_fp8 : format == KV_FORMAT_FP4 ? group_kernel_fp4 : group_kernel_16)(p->D, bf16, t.out_mode == 0, cut.nb);
+    GroupKernel k = (format == KV_FORMAT_FP8 ? group_kernel_fp8 : format == KV_FORMAT_FP4 ? group_kernel_fp4 : group_kernel_16)(p->D, bf16, t.out_mode == 0, cut.nb, cut.nb_prefix != cut.nb);
     hipStream_t st = (hipStream_t)hip_stream;
     const dim3 cgrid((unsigned)((most_new * p->Hq + kCombineWaves - 1) / kCombineWaves), (unsigned)p->B);
     if (cut.ns > 1 && (uint64_t)cgrid.x * 64 * kCombineWaves >= 1ull << 32) return KV_ERANGE;

@@ -445,147 +445,107 @@ __device__ __forceinline__ void plain_row(const TreeParams &p, const int *table,
     if (lane < D / 4) store_sums<D>(p, first + t, hq, split, 4 * at, x, top == -INFINITY ? kNoScore : top, l);
 }
 
-template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
-__global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1))
-    kv_tree_partial_kernel(typename std::conditional<GROUP, GroupParams, TreeParams>::type p)
-{
-    using P = typename std::conditional<GROUP, GroupParams, TreeParams>::type;
-    using T = TreeTile<D, FORMAT, NB>;
-    constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = kParts<BF16, F32>, kWaves = T::kWaves, kStages = T::kStages;
-    constexpr bool kNT = NB <= 2;   // with more rows other workgroups may read the same K and V out of L2
-
-    // The arguments' cache lines at once, not each where the first of its values is needed.
-    asm volatile("" ::"s"(p.c.k), "s"(p.c.kz), "s"(p.q), "s"(p.part_acc), "s"(p.scale_log2e), "s"(p.by_split));
-
-    // Which sequence, KV head, split and row block.  Workgroups go round the eight XCDs; the row blocks of a split are a multiple of eight apart: they run at about the same
-    // time on one XCD and share its L2.
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// What a workgroup does: rows of a KV head over a split of the tokens in a sequence's place of the cache.
+struct Unit {
     unsigned b, h, split, rb = 0;
     int first, drafted, len;
-    [[maybe_unused]] int begin = 0, end_of_rows = 0;   // of the unit's tokens; past the last that a row of this workgroup sees
-    [[maybe_unused]] unsigned slot = 0;                // of the first split's partial result
-    if constexpr (GROUP) {
-        // Units, a lane each: groups, then sequences by 64. What a group's lane knows of it is asked for by the sequences' lanes.
-        unsigned at = blockIdx.x;
-        int group_first = 0, group_end = 0, shared = 0;
-        if (lane < p.n_groups) {
-            group_first = p.group_first[lane];
-            group_end = p.group_first[lane + 1];
-            shared = p.prefix[lane];
+    // kv_group_attn's: where the unit's tokens begin, past the last that its rows see, the first split's partial result, the unit's splits
+    int begin = 0, end_of_rows = 0;
+    unsigned slot = 0, splits = 1;
+    bool is_prefix = false;
+};
+
+// Of ROWS_PREFIX query rows of a group over its prefix, or ROWS of a sequence. false: no work.
+template <int ROWS_PREFIX, int ROWS>
+__device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &u)
+{
+    // Units, a lane each: groups, then sequences by 64. What a group's lane knows of it is asked for by the sequences' lanes.
+    unsigned at = blockIdx.x;
+    int group_first = 0, group_end = 0, shared = 0;
+    if (lane < p.n_groups) {
+        group_first = p.group_first[lane];
+        group_end = p.group_first[lane + 1];
+        shared = p.prefix[lane];
+    }
+    for (int b0 = p.n_groups > 0 ? -1 : 0; b0 < p.B; b0 = b0 < 0 ? 0 : b0 + 64) {
+        const bool is_group = b0 < 0;
+        const int rows = is_group ? ROWS_PREFIX : ROWS;
+        int f = 0, n = 0, l = 0, from = 0, kb = 0;   // first token, their number, context, where the unit's tokens begin, sequence in whose place they are
+        if (is_group) {
+            if (lane < p.n_groups && shared > 0) {
+                f = p.tok_first[group_first];
+                n = p.tok_first[group_end] - f;
+                l = shared;
+                kb = group_first;
+            }
+        } else {
+            kb = b0 + lane;
+            for (int g = 0; g < p.n_groups; ++g) {
+                const int x = __builtin_amdgcn_readlane(group_first, g), y = __builtin_amdgcn_readlane(group_end, g), z = __builtin_amdgcn_readlane(shared, g);
+                from = kb >= x && kb < y ? z : from;
+            }
+            if (kb < p.B) {
+                f = p.tok_first[kb];
+                n = p.tok_first[kb + 1] - f;
+                l = max(from, min(p.seq_lens[kb], p.max_total - n));
+            }
         }
-        bool found = false;
-        for (int b0 = p.n_groups > 0 ? -1 : 0; b0 < p.B; b0 = b0 < 0 ? 0 : b0 + 64) {
-            const bool is_group = b0 < 0;
-            int f = 0, n = 0, l = 0, from = 0, kb = 0;   // first token, their number, context, where the unit's tokens begin, sequence in whose place they are
-            if (is_group) {
-                if (lane < p.n_groups && shared > 0) {
-                    f = p.tok_first[group_first];
-                    n = p.tok_first[group_end] - f;
-                    l = shared;
-                    kb = group_first;
-                }
-            } else {
-                kb = b0 + lane;
-                for (int g = 0; g < p.n_groups; ++g) {
-                    const int x = __builtin_amdgcn_readlane(group_first, g), y = __builtin_amdgcn_readlane(group_end, g), z = __builtin_amdgcn_readlane(shared, g);
-                    from = kb >= x && kb < y ? z : from;
-                }
-                if (kb < p.B) {
-                    f = p.tok_first[kb];
-                    n = p.tok_first[kb + 1] - f;
-                    l = max(from, min(p.seq_lens[kb], p.max_total - n));
-                }
-            }
-            const int st = is_group ? p.prefix_tokens : p.split_tokens;
-            unsigned units = 0;
-            if (n > 0) {
-                const int span = is_group ? l : l + n - (from & ~31);
-                units = (quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1) * (unsigned)p.H;
-                if (n * (long long)p.G > kRows) units = (units + 7) & ~7u;
-            }
-            const unsigned all = units * (unsigned)(((long long)n * p.G + kRows - 1) / kRows);
-            unsigned end = all;
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
-            end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
-            const int which = __popcll(__ballot(end <= at));
-            if (which >= 64) {
-                at -= (unsigned)__builtin_amdgcn_readlane((int)end, 63);
-                continue;
-            }
-            first = __builtin_amdgcn_readlane(f, which);
-            drafted = __builtin_amdgcn_readlane(n, which);
-            len = __builtin_amdgcn_readlane(l, which);
-            begin = __builtin_amdgcn_readlane(from, which);
-            b = (unsigned)__builtin_amdgcn_readlane(kb, which);
-            units = (unsigned)__builtin_amdgcn_readlane((int)units, which);
-            unsigned unit = at - (unsigned)__builtin_amdgcn_readlane((int)(end - all), which);
-            if (unit >= units) {
-                rb = unit / units;
-                unit -= rb * units;
-            }
-            split = quotient(unit, (unsigned)p.H, p.by_h);
-            h = unit - split * (unsigned)p.H;
-            slot = is_group ? 0 : (unsigned)p.prefix_ns;
-            end_of_rows = is_group ? len : len + drafted;
-            found = true;
-            break;
+        const int st = is_group ? p.prefix_tokens : p.split_tokens;
+        unsigned units = 0, of_unit = 0;
+        if (n > 0) {
+            const int span = is_group ? l : l + n - (from & ~31);
+            of_unit = quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1;
+            units = of_unit * (unsigned)p.H;
+            if (n * (long long)p.G > rows) units = (units + 7) & ~7u;
         }
-        if (!found) return;
-    } else if (p.ragged) {
-        // Only what there is, sequence after sequence (a lane each): workgroups that have nothing to do would take places from others, which then share a compute unit
-        // while the next one is idle.
-        int f = 0, n = 0, l = 0;
-        unsigned units = 0;   // splits of heads, in eights where there may be row blocks
-        if (lane < p.B) {
-            f = p.tok_first[lane];
-            n = min(p.tok_first[lane + 1] - f, KV_TREE_MAX);
-            l = max(0, min(p.seq_lens[lane], p.max_total - n));
-            units = n <= 0 ? 0 : (quotient((unsigned)(l + n - 1), (unsigned)p.split_tokens, p.by_split) + 1) * (unsigned)p.H;
-            if (p.row_blocks > 1) units = (units + 7) & ~7u;
-        }
-        const unsigned all = units * ((unsigned)(n * p.G + kRows - 1) / kRows);
-        unsigned end = all;   // of the sequence's workgroups
-        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);   // sums over the lanes below: 1, 2, 4, 8 of a row of 16, then over rows
+        const unsigned all = units * (unsigned)(((long long)n * p.G + rows - 1) / rows);
+        unsigned end = all;
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
-        b = (unsigned)__popcll(__ballot(end <= blockIdx.x));
-        if (b >= (unsigned)p.B) return;
-        first = __builtin_amdgcn_readlane(f, (int)b);
-        drafted = __builtin_amdgcn_readlane(n, (int)b);
-        len = __builtin_amdgcn_readlane(l, (int)b);
-        units = (unsigned)__builtin_amdgcn_readlane((int)units, (int)b);
-        unsigned unit = blockIdx.x - (unsigned)__builtin_amdgcn_readlane((int)(end - all), (int)b);
+        const int which = __popcll(__ballot(end <= at));
+        if (which >= 64) {
+            at -= (unsigned)__builtin_amdgcn_readlane((int)end, 63);
+            continue;
+        }
+        u.first = __builtin_amdgcn_readlane(f, which);
+        u.drafted = __builtin_amdgcn_readlane(n, which);
+        u.len = __builtin_amdgcn_readlane(l, which);
+        u.begin = __builtin_amdgcn_readlane(from, which);
+        u.b = (unsigned)__builtin_amdgcn_readlane(kb, which);
+        units = (unsigned)__builtin_amdgcn_readlane((int)units, which);
+        u.splits = (unsigned)__builtin_amdgcn_readlane((int)of_unit, which);
+        unsigned unit = at - (unsigned)__builtin_amdgcn_readlane((int)(end - all), which);
         if (unit >= units) {
-            rb = unit / units;
-            unit -= rb * units;
+            u.rb = unit / units;
+            unit -= u.rb * units;
         }
-        split = quotient(unit, (unsigned)p.H, p.by_h);
-        h = unit - split * (unsigned)p.H;
-    } else {
-        unsigned unit = blockIdx.x;
-        if (p.row_blocks > 1) {
-            const unsigned turn = blockIdx.x / 8, eights = quotient(turn, (unsigned)p.row_blocks, p.by_row_blocks);
-            rb = turn - eights * (unsigned)p.row_blocks;
-            unit = eights * 8 + blockIdx.x % 8;
-        }
-        const unsigned bh = quotient(unit, (unsigned)p.ns, p.by_ns);
-        split = unit - bh * (unsigned)p.ns;
-        b = quotient(bh, (unsigned)p.H, p.by_h);
-        h = bh - b * (unsigned)p.H;
-        if (b >= (unsigned)p.B) return;
-        const int next = load_uniform(p.tok_first + b + 1), l = load_uniform(p.seq_lens + b);
-        first = load_uniform(p.tok_first + b);
-        __builtin_amdgcn_sched_barrier(0);   // one wait for all three
-        drafted = min(next - first, KV_TREE_MAX);
-        len = max(0, min(l, p.max_total - drafted));
+        u.split = quotient(unit, (unsigned)p.H, p.by_h);
+        u.h = unit - u.split * (unsigned)p.H;
+        u.slot = is_group ? 0 : (unsigned)p.prefix_ns;
+        u.end_of_rows = is_group ? u.len : u.len + u.drafted;
+        u.is_prefix = is_group;
+        return true;
     }
+    return false;
+}
+
+// lds: TreeTile::kLds bytes of a workgroup's.
+template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
+__device__ __forceinline__ void tree_work(const typename std::conditional<GROUP, GroupParams, TreeParams>::type &p, const Unit &u, char *const lds, int lane, int wave)
+{
+    using P = typename std::conditional<GROUP, GroupParams, TreeParams>::type;
+    using T = TreeTile<D, FORMAT, NB>;
+    constexpr int kRows = T::kRows, kColumns = T::kColumns, kSteps = T::kSteps, kP = kParts<BF16, F32>, kWaves = T::kWaves, kStages = T::kStages;
+    constexpr bool kNT = NB <= 2;   // with more rows other workgroups may read the same K and V out of L2
+    const unsigned b = u.b, h = u.h, split = u.split, rb = u.rb;
+    const int first = u.first, drafted = u.drafted, len = u.len;
+    [[maybe_unused]] const int begin = u.begin;
+    [[maybe_unused]] int end_of_rows = u.end_of_rows;
+    [[maybe_unused]] const unsigned slot = u.slot, splits = u.splits;
     const int n_rows = drafted * p.G - (int)rb * kRows;   // of this block: the first kRows of them
     if (n_rows <= 0) return;
     const int total = GROUP ? end_of_rows : len + drafted;
@@ -593,10 +553,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     [[maybe_unused]] int from_most = begin, pos_least = INT_MAX, origin = len;   // all rows see what is between from_most and the context's end; none of their positions is below pos_least
     [[maybe_unused]] bool by_row = false;   // positions too far from one origin for 32 bits
     if constexpr (GROUP) {
-        const int st = total == len ? p.prefix_tokens : p.split_tokens, start = begin & ~31;
-        if (!split_has_tokens(split, st, total - start)) return;
-        s0 = start + (int)split * st;
-        s1 = min(s0 + st, total);
+        if (split >= splits) return;
         int from_least = begin;
         if (total > len && !p.mask) end_of_rows = len + 1 + (int)quotient((unsigned)((int)rb * kRows + min(n_rows, kRows) - 1), (unsigned)p.G, p.by_g);
         if (p.from || p.to || p.slopes) {
@@ -620,10 +577,11 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
                 if (by_row) pos_least = INT_MIN;
             }
         }
-        // tokens that none of the rows sees are left out
-        s1 = min(s1, end_of_rows);
-        s0 = max(s0, min(from_least & ~31, s1 & ~31));
-        s1 = max(s0, s1);
+        // What the rows see of the unit's tokens, shared out to its splits: a window, or the end of a chain, shortens them all.
+        const int end = min(total, end_of_rows), start = min(from_least & ~31, end & ~31), seen = max(end - start, 0);
+        const int share = splits == 1 ? seen : (int)((((unsigned)seen + splits - 1) / splits + 31) & ~31u);
+        s0 = min(start + (int)split * share, (end + 31) & ~31);
+        s1 = max(s0, min(s0 + share, end));
     } else {
         if (!split_has_tokens(split, p.split_tokens, total)) return;
         s0 = (int)split * p.split_tokens;
@@ -635,8 +593,7 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     const unsigned long long zbase = p.c.table ? h * p.c.zh : b * p.c.zb + h * p.c.zh;
     const int *const table = p.c.table ? p.c.table + (long long)b * p.c.max_blocks : nullptr;
 
-    // The ring of each wavefront's stages, then q; after the last step the merge's rows and states.
-    __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+    // lds: the ring of each wavefront's stages, then q; after the last step the merge's rows and states.
     const unsigned ring_at = (unsigned)wave * (kStages * T::kStage);
     const unsigned lds_at = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char *)lds + ring_at;
     const char *const ring = lds + ring_at;
@@ -1234,6 +1191,92 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
     }
 }
 
+template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
+__global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1))
+    kv_tree_partial_kernel(typename std::conditional<GROUP, GroupParams, TreeParams>::type p)
+{
+    using T = TreeTile<D, FORMAT, NB>;
+    constexpr int kRows = T::kRows;
+
+    // The arguments' cache lines at once, not each where the first of its values is needed.
+    asm volatile("" ::"s"(p.c.k), "s"(p.c.kz), "s"(p.q), "s"(p.part_acc), "s"(p.scale_log2e), "s"(p.by_split));
+
+    // Which sequence, KV head, split and row block.  Workgroups go round the eight XCDs; the row blocks of a split are a multiple of eight apart: they run at about the same
+    // time on one XCD and share its L2.
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Unit u;
+    if constexpr (GROUP) {
+        if (!find_unit<T::kRows, T::kRows>(p, lane, u)) return;
+    } else if (p.ragged) {
+        // Only what there is, sequence after sequence (a lane each): workgroups that have nothing to do would take places from others, which then share a compute unit
+        // while the next one is idle.
+        int f = 0, n = 0, l = 0;
+        unsigned units = 0;   // splits of heads, in eights where there may be row blocks
+        if (lane < p.B) {
+            f = p.tok_first[lane];
+            n = min(p.tok_first[lane + 1] - f, KV_TREE_MAX);
+            l = max(0, min(p.seq_lens[lane], p.max_total - n));
+            units = n <= 0 ? 0 : (quotient((unsigned)(l + n - 1), (unsigned)p.split_tokens, p.by_split) + 1) * (unsigned)p.H;
+            if (p.row_blocks > 1) units = (units + 7) & ~7u;
+        }
+        const unsigned all = units * ((unsigned)(n * p.G + kRows - 1) / kRows);
+        unsigned end = all;   // of the sequence's workgroups
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);   // sums over the lanes below: 1, 2, 4, 8 of a row of 16, then over rows
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x114, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x118, 0xf, 0xf, true);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x142, 0xa, 0xf, false);
+        end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x143, 0xc, 0xf, false);
+        u.b = (unsigned)__popcll(__ballot(end <= blockIdx.x));
+        if (u.b >= (unsigned)p.B) return;
+        u.first = __builtin_amdgcn_readlane(f, (int)u.b);
+        u.drafted = __builtin_amdgcn_readlane(n, (int)u.b);
+        u.len = __builtin_amdgcn_readlane(l, (int)u.b);
+        units = (unsigned)__builtin_amdgcn_readlane((int)units, (int)u.b);
+        unsigned unit = blockIdx.x - (unsigned)__builtin_amdgcn_readlane((int)(end - all), (int)u.b);
+        if (unit >= units) {
+            u.rb = unit / units;
+            unit -= u.rb * units;
+        }
+        u.split = quotient(unit, (unsigned)p.H, p.by_h);
+        u.h = unit - u.split * (unsigned)p.H;
+    } else {
+        unsigned unit = blockIdx.x;
+        if (p.row_blocks > 1) {
+            const unsigned turn = blockIdx.x / 8, eights = quotient(turn, (unsigned)p.row_blocks, p.by_row_blocks);
+            u.rb = turn - eights * (unsigned)p.row_blocks;
+            unit = eights * 8 + blockIdx.x % 8;
+        }
+        const unsigned bh = quotient(unit, (unsigned)p.ns, p.by_ns);
+        u.split = unit - bh * (unsigned)p.ns;
+        u.b = quotient(bh, (unsigned)p.H, p.by_h);
+        u.h = bh - u.b * (unsigned)p.H;
+        if (u.b >= (unsigned)p.B) return;
+        const int next = load_uniform(p.tok_first + u.b + 1), l = load_uniform(p.seq_lens + u.b);
+        u.first = load_uniform(p.tok_first + u.b);
+        __builtin_amdgcn_sched_barrier(0);   // one wait for all three
+        u.drafted = min(next - u.first, KV_TREE_MAX);
+        u.len = max(0, min(l, p.max_total - u.drafted));
+    }
+    __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+    tree_work<D, BF16, FORMAT, NB, F32, GROUP>(p, u, lds, lane, wave);
+}
+
+// Prefixes, whose rows are many, with NBP row groups of a workgroup, and sequences with one in the same launch.
+template <int D, bool BF16, int FORMAT, int NBP, bool F32>
+__global__ void __launch_bounds__(kTreeThreads, (TreeTile<D, FORMAT, NBP>::kLds <= TreeTile<D, FORMAT, NBP>::kHalfLds && TreeTile<D, FORMAT, 1>::kLds <= TreeTile<D, FORMAT, 1>::kHalfLds ? 2 : 1))
+    kv_group_mixed_kernel(GroupParams p)
+{
+    constexpr int kLds = TreeTile<D, FORMAT, NBP>::kLds > TreeTile<D, FORMAT, 1>::kLds ? TreeTile<D, FORMAT, NBP>::kLds : TreeTile<D, FORMAT, 1>::kLds;
+    asm volatile("" ::"s"(p.c.k), "s"(p.c.kz), "s"(p.q), "s"(p.part_acc), "s"(p.scale_log2e), "s"(p.by_split));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Unit u;
+    if (!find_unit<16 * NBP, 16>(p, lane, u)) return;
+    __shared__ __attribute__((aligned(1024))) char lds[kLds];
+    if (u.is_prefix) tree_work<D, BF16, FORMAT, NBP, F32, true>(p, u, lds, lane, wave);
+    else tree_work<D, BF16, FORMAT, 1, F32, true>(p, u, lds, lane, wave);
+}
+
 template <bool GROUP>
 struct TreeKernelOf {
     typedef void (*Kernel)(typename std::conditional<GROUP, GroupParams, TreeParams>::type);
@@ -1250,6 +1293,18 @@ struct TreeKernelOf {
         if (D == 128) return nb == 1 ? of<FORMAT, 128, 1>(bf16, f32) : nb == 2 ? of<FORMAT, 128, 2>(bf16, f32) : of<FORMAT, 128, 4>(bf16, f32);
         return nb == 1 ? of<FORMAT, 64, 1>(bf16, f32) : nb == 2 ? of<FORMAT, 64, 2>(bf16, f32) : of<FORMAT, 64, 4>(bf16, f32);
     }
+    // the most rows for prefixes, the fewest for sequences
+    template <int FORMAT, int D>
+    static Kernel mixed_of(bool bf16, bool f32)
+    {
+        constexpr int kNB = D == 256 ? 2 : 4;
+        return !bf16 ? kv_group_mixed_kernel<D, false, FORMAT, kNB, false> : f32 ? kv_group_mixed_kernel<D, true, FORMAT, kNB, true> : kv_group_mixed_kernel<D, true, FORMAT, kNB, false>;
+    }
+    template <int FORMAT>
+    static Kernel choose_mixed(int D, bool bf16, bool f32)
+    {
+        return D == 256 ? mixed_of<FORMAT, 256>(bf16, f32) : D == 128 ? mixed_of<FORMAT, 128>(bf16, f32) : mixed_of<FORMAT, 64>(bf16, f32);
+    }
 };
 // In a translation unit each.
 typedef TreeKernelOf<false>::Kernel TreeKernel;
@@ -1257,8 +1312,8 @@ TreeKernel tree_kernel_16(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp8(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp4(int D, bool bf16, bool f32, int nb);
 typedef TreeKernelOf<true>::Kernel GroupKernel;
-GroupKernel group_kernel_16(int D, bool bf16, bool f32, int nb);
-GroupKernel group_kernel_fp8(int D, bool bf16, bool f32, int nb);
-GroupKernel group_kernel_fp4(int D, bool bf16, bool f32, int nb);
+GroupKernel group_kernel_16(int D, bool bf16, bool f32, int nb, bool mixed);
+GroupKernel group_kernel_fp8(int D, bool bf16, bool f32, int nb, bool mixed);
+GroupKernel group_kernel_fp4(int D, bool bf16, bool f32, int nb, bool mixed);
 
 }  // namespace kvb

@@ -42,7 +42,7 @@ int main()
         uint64_t groups = 0, covered = 0;
         for (const auto &u : units) {
             const int st = u.prefix ? c.prefix_tokens : c.split_tokens, most = u.prefix ? c.prefix_ns : c.ns - c.prefix_ns;
-            groups += kvb::unit_workgroups(s, u, c.nb, st);
+            groups += kvb::unit_workgroups(s, u, u.prefix ? c.nb_prefix : c.nb, st);
             covered += kvb::splits_of(u.span, st) <= most;
         }
         std::printf("%d %d %d %d %d %d %llu %llu %d\n", c.nb, c.prefix_tokens, c.split_tokens, c.prefix_ns, c.ns, (int)std::min<uint64_t>(ws / one, 1u << 30), (unsigned long long)groups,
