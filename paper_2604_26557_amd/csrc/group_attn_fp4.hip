@@ -2,5 +2,5 @@
 
 kvb::GroupKernel kvb::group_kernel_fp4(int D, bool bf16, bool f32, int nb, bool mixed)
 {
-    return mixed ? TreeKernelOf<true>::choose_mixed<KV_FORMAT_FP4>(D, bf16, f32) : TreeKernelOf<true>::choose<KV_FORMAT_FP4>(D, bf16, f32, nb);
+    return mixed ? TreeKernelOf<true, false>::choose_mixed<KV_FORMAT_FP4>(D, bf16, f32) : TreeKernelOf<true, false>::choose<KV_FORMAT_FP4>(D, bf16, f32, nb);
 }

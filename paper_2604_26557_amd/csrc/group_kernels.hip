@@ -106,8 +106,10 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
         t.from = scores->sees_from;
         t.to = scores->sees_to;
     }
-    t.shaped = t.cap > 0.f || t.slopes;
-    t.scale_log2e = (float)(1.4426950408889634 * (t.shaped ? 1. : scale));
+    const bool shaped = t.cap > 0.f || t.slopes;
+    // the error of a cap by sigmoids grows with it: beyond 64 it would show in 16-bit results
+    if (t.out_mode != 0 && t.cap > 0.f && t.cap <= 64.f) t.sigmoid_in = -2.88539008f * t.cap_in;
+    t.scale_log2e = (float)(1.4426950408889634 * (!shaped ? scale : t.sigmoid_in != 0.f && !t.slopes ? 2. * t.cap : 1.));
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;
     const TreeShape shape = tree_shape(p, format_bits(format), t.c.table != nullptr);
@@ -147,7 +149,8 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
     t.grouped = t.c.table ? t.c.bt % 16 == 0 && t.c.sb < 1ull << 32 && t.c.zb < 1ull << 32 && t.c.zs < (1ull << 32) / (uint64_t)t.c.bt
                           : t.c.ss < 1ull << 25 && t.c.zs < 1ull << 25;
     t.dense = t.c.ss == (uint64_t)p->D * format_bits(format) / 8;
-    GroupKernel k = (format == KV_FORMAT_FP8 ? group_kernel_fp8 : format == KV_FORMAT_FP4 ? group_kernel_fp4 : group_kernel_16)(p->D, bf16, t.out_mode == 0, cut.nb, cut.nb_prefix != cut.nb);
+    GroupKernel k = (format == KV_FORMAT_FP8 ? shaped ? shaped_kernel_fp8 : group_kernel_fp8
+                     : format == KV_FORMAT_FP4 ? shaped ? shaped_kernel_fp4 : group_kernel_fp4 : shaped ? shaped_kernel_16 : group_kernel_16)(p->D, bf16, t.out_mode == 0, cut.nb, cut.nb_prefix != cut.nb);
     hipStream_t st = (hipStream_t)hip_stream;
     const dim3 cgrid((unsigned)((most_new * p->Hq + kCombineWaves - 1) / kCombineWaves), (unsigned)p->B);
     if (cut.ns > 1 && (uint64_t)cgrid.x * 64 * kCombineWaves >= 1ull << 32) return KV_ERANGE;

@@ -63,8 +63,9 @@ struct GroupParams : TreeParams {
     int n_groups, prefix_ns;           // partial results of a row that are of its prefix
     int prefix_tokens;                 // of a split of a prefix, a multiple of 32
     unsigned by_prefix;
-    int shaped;                        // scores are capped or biased: the softmax takes them as they are then, scale_log2e = log2(e)
+    // In kernels whose scores are capped or biased the softmax takes them as they are then: scale_log2e is log2(e), but for sigmoids alone.
     float scale, cap, cap_in;          // cap 0: none; cap_in = scale / cap
+    float sigmoid_in;                  // not 0: the cap by sigmoids, this = -2 log2(e) scale / cap
     const float *slopes;
     const int *positions, *from, *to;
 };
@@ -498,7 +499,7 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
             units = of_unit * (unsigned)p.H;
             if (n * (long long)p.G > rows) units = (units + 7) & ~7u;
         }
-        const unsigned all = units * (unsigned)(((long long)n * p.G + rows - 1) / rows);
+        const unsigned blocks = (unsigned)(((long long)n * p.G + rows - 1) / rows), all = units * blocks;
         unsigned end = all;
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x111, 0xf, 0xf, true);
         end += (unsigned)__builtin_amdgcn_update_dpp(0, (int)end, 0x112, 0xf, 0xf, true);
@@ -523,6 +524,7 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
             u.rb = unit / units;
             unit -= u.rb * units;
         }
+        u.rb = (unsigned)__builtin_amdgcn_readlane((int)blocks, which) - 1 - u.rb;   // a chain's last rows see the most: they begin first
         u.split = quotient(unit, (unsigned)p.H, p.by_h);
         u.h = unit - u.split * (unsigned)p.H;
         u.slot = is_group ? 0 : (unsigned)p.prefix_ns;
@@ -534,7 +536,7 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
 }
 
 // lds: TreeTile::kLds bytes of a workgroup's.
-template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
+template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP, bool SHAPED>
 __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP, GroupParams, TreeParams>::type &p, const Unit &u, char *const lds, int lane, int wave)
 {
     using P = typename std::conditional<GROUP, GroupParams, TreeParams>::type;
@@ -556,9 +558,9 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
         if (split >= splits) return;
         int from_least = begin;
         if (total > len && !p.mask) end_of_rows = len + 1 + (int)quotient((unsigned)((int)rb * kRows + min(n_rows, kRows) - 1), (unsigned)p.G, p.by_g);
-        if (p.from || p.to || p.slopes) {
+        if (p.from || p.to || (SHAPED && p.slopes)) {
             const int r = (int)rb * kRows + min(lane, min(n_rows, kRows) - 1), t = first + (int)quotient((unsigned)r, (unsigned)p.G, p.by_g);
-            int lo = max(begin, p.from ? p.from[t] : 0), most = lo, up = p.to ? p.to[t] : 0, least = p.slopes ? p.positions[t] : 0, far = least;
+            int lo = max(begin, p.from ? p.from[t] : 0), most = lo, up = p.to ? p.to[t] : 0, least = SHAPED && p.slopes ? p.positions[t] : 0, far = least;
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
                 lo = min(lo, __shfl_xor(lo, o));
@@ -570,7 +572,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             from_least = __builtin_amdgcn_readfirstlane(lo);
             from_most = __builtin_amdgcn_readfirstlane(most);
             if (total > len) end_of_rows = max(end_of_rows, min(__builtin_amdgcn_readfirstlane(up), total));
-            if (p.slopes) {
+            if (SHAPED && p.slopes) {
                 pos_least = __builtin_amdgcn_readfirstlane(least);
                 if (total > len) origin = __builtin_amdgcn_readfirstlane(far);
                 by_row = total > len ? (long long)origin - pos_least > 1024 : pos_least < len;
@@ -733,7 +735,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     };
     // A lane has the slope of a head of the KV head's; a row asks the lane of its head (of groups of more than 64, memory, at the price of a wait for all loads ahead).
     [[maybe_unused]] float slopes = 0.f;
-    if constexpr (GROUP) {
+    if constexpr (SHAPED) {
         if (p.slopes && lane < p.G) {
             slopes = p.slopes[(int)h * p.G + lane];
             asm volatile("" : "+v"(slopes));   // here now: a wait for it in the loop would be one for the loads ahead
@@ -956,9 +958,19 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     // Scores of kv_group_attn that are capped or biased. A bias is slope * (min(j, 2 pos - j) - origin): for one row that is -slope |pos - j| and a number that the softmax does not see, and as long as
     // no token lies behind a row's position, slope * (j - origin), of which a lane needs the slope alone. Where the rows' positions are far apart each has its own for an origin.
     [[maybe_unused]] auto shape = [&](f32x4 (&s)[NB][2], int j0) {
-        if constexpr (GROUP) {
+        if constexpr (SHAPED) {
             const GroupParams p = arguments<P>();
-            if (p.cap > 0.f) {
+            if (!F32 && p.sigmoid_in != 0.f) {
+                // tanh(y) = 2 / (1 + e^(-2y)) - 1, of which the softmax does not see the last. Off by cap 2^-21 at most, where it is chosen a sixteenth of what a 16-bit result is rounded by;
+                // 40 cycles of a wavefront's for a score, the other form takes 72.
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[nb][j / 4][j % 4] * p.sigmoid_in));
+                if (!p.slopes) return;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][0] *= 2.f * p.cap, s[nb][1] *= 2.f * p.cap;
+            } else if (p.cap > 0.f) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -1015,9 +1027,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             scores(k, s);
             if constexpr (kFirstK) __builtin_amdgcn_s_setprio(0);
         }
-        if constexpr (GROUP) {
-            if (p.shaped) shape(s, j0);
-        }
+        if constexpr (SHAPED) shape(s, j0);
         if (j0 + 32 > len || there[0] != ~0u || (GROUP && j0 < from_most)) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
             const P p = arguments<P>();
@@ -1106,14 +1116,15 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             const int r = (int)rb * kRows + i, t = row_token(i);
             if constexpr (GROUP) {
                 const GroupRows u{first, drafted, begin, len, total};
-                const float bias = a.slopes ? a.slopes[(int)h * a.G + r - t * a.G] : 0.f;
-                const int pos = a.slopes ? a.positions[first + t] : 0;
+                const float bias = SHAPED && a.slopes ? a.slopes[(int)h * a.G + r - t * a.G] : 0.f;
+                const int pos = SHAPED && a.slopes ? a.positions[first + t] : 0;
                 plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, r, j) & 1); },
                                            [&](float x, int j) {
-                                               if (!a.shaped) return x * a.scale_log2e;
+                                               if constexpr (!SHAPED) return x * a.scale_log2e;
                                                x = a.cap > 0.f ? a.cap * tanh_of(x * a.cap_in) : x * a.scale;
+                                               if (!F32 && a.sigmoid_in != 0.f) x += a.cap;   // as the others have it
                                                if (a.slopes) x -= bias * fabsf((float)((long long)pos - (j < len ? j : a.positions[first + j - len])));
-                                               return x * a.scale_log2e;
+                                               return x * 1.44269504f;
                                            });
             } else {
                 plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, split, lane, [&](int j) { return row_sees(a, first, r, j, len, total); },
@@ -1175,7 +1186,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             ml[0] = k == nb ? to[k] : ml[0];
             ml[1] = k == nb ? total_sum[k] : ml[1];
         }
-        if constexpr (GROUP) {   // as if biased by its distances themselves
+        if constexpr (SHAPED) {   // as if biased by its distances themselves
             if (a.slopes && !by_row) ml[0] -= a.slopes[hq] * (float)((long long)a.positions[first + t] - origin) * a.scale_log2e;
         }
         *(f32x2 *)&a.part_ml[part * 2] = f32x2{ml[0] - kLiftLog2<BF16>, ml[1]};
@@ -1191,7 +1202,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     }
 }
 
-template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP>
+template <int D, bool BF16, int FORMAT, int NB, bool F32, bool GROUP, bool SHAPED>
 __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeTile<D, FORMAT, NB>::kLds <= TreeTile<D, FORMAT, NB>::kHalfLds ? 2 : 1))
     kv_tree_partial_kernel(typename std::conditional<GROUP, GroupParams, TreeParams>::type p)
 {
@@ -1259,11 +1270,11 @@ __global__ void __launch_bounds__((64 * TreeTile<D, FORMAT, NB>::kWaves), (TreeT
         u.len = max(0, min(l, p.max_total - u.drafted));
     }
     __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
-    tree_work<D, BF16, FORMAT, NB, F32, GROUP>(p, u, lds, lane, wave);
+    tree_work<D, BF16, FORMAT, NB, F32, GROUP, SHAPED>(p, u, lds, lane, wave);
 }
 
 // Prefixes, whose rows are many, with NBP row groups of a workgroup, and sequences with one in the same launch.
-template <int D, bool BF16, int FORMAT, int NBP, bool F32>
+template <int D, bool BF16, int FORMAT, int NBP, bool F32, bool SHAPED>
 __global__ void __launch_bounds__(kTreeThreads, (TreeTile<D, FORMAT, NBP>::kLds <= TreeTile<D, FORMAT, NBP>::kHalfLds && TreeTile<D, FORMAT, 1>::kLds <= TreeTile<D, FORMAT, 1>::kHalfLds ? 2 : 1))
     kv_group_mixed_kernel(GroupParams p)
 {
@@ -1273,18 +1284,18 @@ __global__ void __launch_bounds__(kTreeThreads, (TreeTile<D, FORMAT, NBP>::kLds 
     Unit u;
     if (!find_unit<16 * NBP, 16>(p, lane, u)) return;
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
-    if (u.is_prefix) tree_work<D, BF16, FORMAT, NBP, F32, true>(p, u, lds, lane, wave);
-    else tree_work<D, BF16, FORMAT, 1, F32, true>(p, u, lds, lane, wave);
+    if (u.is_prefix) tree_work<D, BF16, FORMAT, NBP, F32, true, SHAPED>(p, u, lds, lane, wave);
+    else tree_work<D, BF16, FORMAT, 1, F32, true, SHAPED>(p, u, lds, lane, wave);
 }
 
-template <bool GROUP>
+template <bool GROUP, bool SHAPED>
 struct TreeKernelOf {
     typedef void (*Kernel)(typename std::conditional<GROUP, GroupParams, TreeParams>::type);
     template <int FORMAT, int D, int NB>
     static Kernel of(bool bf16, bool f32)
     {
-        return !bf16 ? kv_tree_partial_kernel<D, false, FORMAT, NB, false, GROUP>
-                     : f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true, GROUP> : kv_tree_partial_kernel<D, true, FORMAT, NB, false, GROUP>;
+        return !bf16 ? kv_tree_partial_kernel<D, false, FORMAT, NB, false, GROUP, SHAPED>
+                     : f32 ? kv_tree_partial_kernel<D, true, FORMAT, NB, true, GROUP, SHAPED> : kv_tree_partial_kernel<D, true, FORMAT, NB, false, GROUP, SHAPED>;
     }
     template <int FORMAT>
     static Kernel choose(int D, bool bf16, bool f32, int nb)
@@ -1298,7 +1309,7 @@ struct TreeKernelOf {
     static Kernel mixed_of(bool bf16, bool f32)
     {
         constexpr int kNB = D == 256 ? 2 : 4;
-        return !bf16 ? kv_group_mixed_kernel<D, false, FORMAT, kNB, false> : f32 ? kv_group_mixed_kernel<D, true, FORMAT, kNB, true> : kv_group_mixed_kernel<D, true, FORMAT, kNB, false>;
+        return !bf16 ? kv_group_mixed_kernel<D, false, FORMAT, kNB, false, SHAPED> : f32 ? kv_group_mixed_kernel<D, true, FORMAT, kNB, true, SHAPED> : kv_group_mixed_kernel<D, true, FORMAT, kNB, false, SHAPED>;
     }
     template <int FORMAT>
     static Kernel choose_mixed(int D, bool bf16, bool f32)
@@ -1307,13 +1318,16 @@ struct TreeKernelOf {
     }
 };
 // In a translation unit each.
-typedef TreeKernelOf<false>::Kernel TreeKernel;
+typedef TreeKernelOf<false, false>::Kernel TreeKernel;
 TreeKernel tree_kernel_16(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp8(int D, bool bf16, bool f32, int nb);
 TreeKernel tree_kernel_fp4(int D, bool bf16, bool f32, int nb);
-typedef TreeKernelOf<true>::Kernel GroupKernel;
+typedef TreeKernelOf<true, false>::Kernel GroupKernel;
 GroupKernel group_kernel_16(int D, bool bf16, bool f32, int nb, bool mixed);
 GroupKernel group_kernel_fp8(int D, bool bf16, bool f32, int nb, bool mixed);
 GroupKernel group_kernel_fp4(int D, bool bf16, bool f32, int nb, bool mixed);
+GroupKernel shaped_kernel_16(int D, bool bf16, bool f32, int nb, bool mixed);
+GroupKernel shaped_kernel_fp8(int D, bool bf16, bool f32, int nb, bool mixed);
+GroupKernel shaped_kernel_fp4(int D, bool bf16, bool f32, int nb, bool mixed);
 
 }  // namespace kvb

@@ -116,9 +116,10 @@ class Batch:
                 m[i, :max(0, self.sees_from[at + i])] = False
         return m
 
-    def expected(self, scale=None):
+    def expected(self, scale=None, f32=True):
         """(out, bound, sum p |v|): the definition in float64 of what the cache holds, and how far 32-bit arithmetic may be from it, token by token.  A score is a sum of D products (D + 8 roundings
-        of it), its cap is off by 6 units of 2^-24, a bias by 8 of the distance's (4 operations, and 64 tokens more from which a group of rows counts), the exponent's argument by 4 of the
+        of it), its cap is off by 6 units of 2^-24, with 16-bit
+        results and caps up to 64 by 8 units times the cap (2 cap / (1 + e): a quarter of 2 units of the exponential, one of the sum, 2 of the reciprocal), a bias by 8 of the distance's (4 operations, and 64 tokens more from which a group of rows counts), the exponent's argument by 4 of the
         largest and its own; what that changes of a weight changes numerator and sum.  Sums of rows over 64 wavefronts and splits add 64 units."""
         scale = scale or self.D ** -0.5
         q, u = self.q.double().numpy(), 2.0 ** -24
@@ -138,7 +139,7 @@ class Batch:
                     e = (np.abs(kk) @ np.abs(x0)) * abs(scale) * (self.D + 8)
                     if self.cap:
                         x = self.cap * np.tanh(x / self.cap)
-                        e = e + 6 * np.abs(x)
+                        e = e + (8 * self.cap if not f32 and self.cap <= 64 else 6 * np.abs(x))
                     if self.slopes is not None:
                         dist = np.abs(self.positions[at + i] - key_pos[idx])
                         x = x - self.slopes[h] * dist
@@ -152,7 +153,7 @@ class Batch:
         return out, tol + 1e-30, weight
 
     def check(self, got, f32=True, scale=None):
-        out, tol, weight = self.expected(scale)
+        out, tol, weight = self.expected(scale, f32)
         g = got.double().cpu().numpy()
         if not f32:   # what the parts of a probability lose, in numerator and sum, and one rounding
             tol = tol + 2 * (2.0 ** -22 if self.dtype == torch.float16 else 2.0 ** -16) * weight
