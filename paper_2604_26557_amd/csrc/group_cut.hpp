@@ -47,60 +47,103 @@ inline uint64_t group_workspace_bytes(const TreeShape &s, long long n_tok, long 
     return std::max(tree_workspace_bytes(s, n_tok, tokens + 64), 2 * tree_split_bytes(s, n_tok));
 }
 
-// By an estimate of the time in us, with the costs of cut_tree: what the workgroups take that a compute unit gets, two side by side, at least as long as one of them; the cache through HBM once; where there are
-// splits a second launch and partial results. units: those of up to `counted` with work; chains without a mask see half of their new tokens.
-inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, bool chain, int n_splits, uint64_t ws_bytes, long long n_tok)
+// What all units of a kind come to. By row groups of a workgroup, 1, 2 and 4: row blocks, the tokens that they go over, and those of them that they see.
+struct GroupWork {
+    int units = 0, longest = 0;
+    long long rows = 0;          // the most of a unit
+    double blocks[3] = {0, 0, 0}, over[3] = {0, 0, 0}, seen[3] = {0, 0, 0}, tokens = 0, parts = 0, context = 0;
+
+    void add(const TreeShape &s, const GroupUnit &u, double of_span)   // of_span: what of its tokens a row sees
+    {
+        ++units;
+        longest = std::max(longest, u.span);
+        rows = std::max(rows, (long long)u.tokens * s.G);
+        for (int k = 0; k < 3; ++k) {
+            const double n = std::ceil((double)u.tokens * s.G / (16 << k));
+            blocks[k] += n;
+            over[k] += n * u.span;
+            seen[k] += n * of_span;
+        }
+        tokens += u.tokens;
+        parts += (double)u.tokens * u.span;
+        context += of_span;
+    }
+};
+
+// Which cut: by an estimate of the time in us, made of the longest workgroup, of all of them shared out to the places for them, of the rounds that those of prefixes take, and of
+// what the bytes of K and V take, read once and again by further row blocks; where there are splits of the second launch and partial results. Its numbers were fitted to choose well rather than to
+// tell the time: to 20 shapes (1 to 64 sequences, up to 4 prefixes of 300 to 16K tokens, 1 to 900 new tokens, every format and head_dim), each with 10 to 300 of the cuts below; what it
+// chose there took 2 % longer than the best on average, 10 % at most (a common length of all splits, by cut_tree's numbers: 13 % and 45 %).
+// chain: without a mask a sequence sees half of its new tokens; bounded: rows see only some tokens, how many only the GPU knows: half is taken. At least one unit has work.
+inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, bool chain, bool bounded, bool shaped, int n_splits, uint64_t ws_bytes, long long n_tok)
 {
-    int longest = 0, longest_prefix = 0;
-    long long rows = 0, prefix_rows = 0;
-    double context = 0;
+    GroupWork own, prefix;
     for (int i = 0; i < n; ++i) {
-        if (units[i].tokens <= 0 || units[i].span <= 0) continue;
-        (units[i].prefix ? longest_prefix : longest) = std::max(units[i].prefix ? longest_prefix : longest, units[i].span);
-        rows = std::max(rows, (long long)units[i].tokens * s.G);
-        if (units[i].prefix) prefix_rows = std::max(prefix_rows, (long long)units[i].tokens * s.G);
-        context += units[i].span;
+        const GroupUnit &u = units[i];
+        if (u.tokens <= 0 || u.span <= 0) continue;
+        (u.prefix ? prefix : own).add(s, u, (u.span - (chain && !u.prefix ? 0.5 * u.tokens : 0)) * (bounded ? 0.5 : 1));
     }
     const uint64_t fit = ws_bytes / tree_split_bytes(s, n_tok);
-    const int least_ns = longest_prefix > 0 ? 2 : 1;   // one of each kind: the caller has checked for their room
+    const int least_ns = prefix.longest > 0 ? 2 : 1;   // one of each kind: the caller has checked for their room
     const int room = (int)std::max<uint64_t>(least_ns, std::min<uint64_t>(fit, kMaxTreeSplits));
     const int most = n_splits > 0 ? room : std::min(room, std::max(least_ns, tree_most_splits(s, n_tok)));
-    const int span = std::max(longest, longest_prefix);
-    const double row = s.H * 2.0 * s.D * s.bits / 8, hbm = context * row / 7.4e6, part = 2.0 * s.H * s.G * s.D * 4 / 2.0e6;
-    auto tokens_of = [&](int ns) { return (int)((((long long)span + ns - 1) / ns + 31) / 32 * 32); };
-    auto results_of = [&](int ns) { return splits_of(longest_prefix, tokens_of(ns)) + splits_of(longest, tokens_of(ns)); };
-    int only = n_splits;
-    while (only > 1 && results_of(only) > most) --only;
+    const double row = s.H * 2.0 * s.D * s.bits / 8e6, part = 2.0 * s.H * s.G * s.D * 4 / 1e6;
     GroupCut best{};
     double least = 1e30;
-    for (int ns = only > 0 ? only : 1; ns <= kMaxTreeSplits; ns = next_splits(ns)) {
-        if (results_of(ns) > most) break;
-        const int st = tokens_of(ns), of_prefix = splits_of(longest_prefix, st), of_own = splits_of(longest, st);
-        const int most_nb = s.D == 256 ? 2 : 4;
-        for (int k = 0; k < 4; ++k) {   // 1, 2, 4 of both; the most of prefixes alone
-            const int nb = k == 3 ? 1 : 1 << k, nb_prefix = k == 3 ? most_nb : nb;
-            if (nb > most_nb || (k == 3 && longest_prefix == 0)) continue;
-            if (k > 0 && (k == 3 ? prefix_rows : rows) <= 8 * nb_prefix) continue;   // half of the rows would be none
-            auto step = [&](int n) { return 0.95 + 0.18 * n * s.D / 128 * (s.D == 256 ? 1.4 : 1) + (s.paged ? 0.05 : 0); };
-            double groups = 0, work = 0, parts = 0, longest_one = 0;
-            for (int i = 0; i < n; ++i) {
-                if (units[i].tokens <= 0 || units[i].span <= 0) continue;
-                const int mine = units[i].prefix ? nb_prefix : nb;
-                const double start = 2.6 + 0.6 * mine, blocks = std::ceil((double)units[i].tokens * s.G / (16 * mine)), splits = splits_of(units[i].span, st);
-                const double seen = !units[i].prefix && chain ? units[i].span - 0.5 * units[i].tokens : units[i].span;
-                groups += blocks * splits * s.H;
-                work += blocks * s.H * (splits * start + seen / 128 * step(mine));
-                parts += units[i].tokens * splits;
-                longest_one = std::max(longest_one, start + std::min(st, units[i].span) / 128.0 * step(mine));
-            }
-            const double us = std::max({hbm + 3.4, groups > s.cus ? 1.45 * longest_one : longest_one, work / (s.cus * 1.4)}) +
-                              (of_prefix + of_own > 1 ? 3.9 + parts * part + 0.03 * (of_prefix + of_own) : 0);
+    auto consider = [&](int st, int pt) {
+        const int of_prefix = splits_of(prefix.longest, pt), of_own = splits_of(own.longest, st), ns = of_prefix + of_own;
+        if (ns > most) return;
+        const int most_nb = s.D == 256 ? 1 : 2;   // of 0, 1, 2
+        for (int k = 0; k < 4; ++k) {   // 1, 2, 4 row groups of both kinds; the most for prefixes alone
+            const int of = k == 3 ? 0 : k, of_p = k == 3 ? most_nb : k;
+            if (of > most_nb || (k == 3 && prefix.units == 0)) continue;
+            if (k > 0 && (k == 3 ? prefix.rows : std::max(own.rows, prefix.rows)) <= 8 << of_p) continue;   // half of the rows would be none
+            // workgroups that a compute unit holds, by their LDS
+            const bool one_each = s.D == 256 && (s.bits == 16 || (s.bits == 8 && of_p == 1));
+            const double slots = one_each ? s.cus : 2 * s.cus, slower = one_each ? 1 : 1.256;
+            double work = 0, groups = 0, longest = 0, again = 0, parts = 0, rounds = 0;
+            auto kind = [&](const GroupWork &w, int nb, int tokens, bool ahead) {
+                if (w.units == 0) return;
+                const int rows16 = 1 << nb;
+                const double step = (1.039 + 0.16 * rows16 * s.D / 128 * (s.D == 256 ? 2.837 : 1) + (s.bits < 16 ? 0.045 : 0) + (shaped ? 0.144 * rows16 : 0)) / 128, start = 3.0 + 1.55 * rows16;
+                // about as many splits as there are: half a one more of each unit than its tokens fill
+                const double splits = w.longest <= tokens ? w.blocks[nb] : std::max(w.blocks[nb], w.over[nb] / tokens + 0.5 * w.blocks[nb]);
+                const double one = start + std::min(tokens, w.longest) * (bounded ? 0.5 : 1) * step, r = splits * s.H / slots;
+                groups += splits * s.H;
+                work += (splits * start + w.seen[nb] * step) * s.H;
+                longest = std::max(longest, one);
+                again += w.seen[nb] - w.context;
+                parts += w.longest <= tokens ? w.tokens : std::max(w.tokens, w.parts / tokens + 0.5 * w.tokens);
+                // prefixes go first, and others fill what they leave; one kind alone, of unequal lengths, is over a little earlier
+                if (ahead || prefix.units == 0) rounds = std::max(rounds, (r < 4 ? std::ceil(r - 0.02) : r + 0.5) * one * slower * (ahead ? 1 : 0.8));
+            };
+            kind(own, of, st, false);
+            kind(prefix, of_p, pt, true);
+            const double memory = (own.context + prefix.context) * row / 10.3 + again * row / 15.8 + 0.345 * longest;
+            const double us = (groups <= s.cus ? std::max(longest, memory) : std::max({work * slower / slots + 0.355 * longest, rounds, memory})) +
+                              (ns > 1 ? 6.1 + parts * part / 4.37 + 0.047 * ns : 0);
             if (us < least) {
                 least = us;
-                best = GroupCut{nb, nb_prefix, st, st, of_prefix, of_prefix + of_own};
+                best = GroupCut{1 << of, 1 << of_p, pt, st, of_prefix, ns};
             }
         }
-        if (only > 0) break;
+    };
+    const int span = std::max(own.longest, prefix.longest);
+    auto even = [&](int ns) { return (int)((((long long)span + ns - 1) / ns + 31) / 32 * 32); };
+    if (n_splits > 0) {
+        for (int ns = n_splits; best.nb == 0 && ns >= 1; --ns) consider(even(ns), even(ns));
+        return best;
+    }
+    // lengths of which those past twice a kind's longest say nothing new; the last is the whole
+    static constexpr int kLengths[] = {128, 256, 384, 512, 768, 1024, 1536, 2048, 3072, 4096, 8192, 16384};
+    for (int i = 0; i <= 12; ++i) {
+        const bool whole = i == 12 || kLengths[i] >= own.longest;
+        for (int j = 0; j <= 12; ++j) {
+            const bool whole_prefix = j == 12 || kLengths[j] >= prefix.longest;
+            consider(whole ? even(1) : kLengths[i], whole_prefix ? even(1) : kLengths[j]);
+            if (whole_prefix) break;
+        }
+        if (whole) break;
     }
     return best;
 }

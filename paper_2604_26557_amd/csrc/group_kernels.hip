@@ -129,7 +129,7 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
         any_prefix = any_prefix || u.prefix;
     }
     if (any_prefix && ws_bytes < 2 * tree_split_bytes(shape, n_tok)) return KV_ENOSPC;
-    const GroupCut cut = cut_group(shape, units, n_units, !a->mask, a->n_splits, ws_bytes, n_tok);
+    const GroupCut cut = cut_group(shape, units, n_units, !a->mask, t.from != nullptr, shaped, a->n_splits, ws_bytes, n_tok);
     t.ns = cut.ns;
     t.prefix_ns = cut.prefix_ns;
     t.split_tokens = cut.split_tokens;

@@ -38,7 +38,7 @@ int main()
         }
         const long long n_tok = first[(size_t)B];
         const uint64_t one = kvb::tree_split_bytes(s, n_tok), ws = ws_splits >= 0 ? one * (uint64_t)ws_splits : kvb::group_workspace_bytes(s, n_tok, (long long)longest + n_tok);
-        const kvb::GroupCut c = kvb::cut_group(s, units.data(), (int)units.size(), chain != 0, n_splits, ws, n_tok);
+        const kvb::GroupCut c = kvb::cut_group(s, units.data(), (int)units.size(), chain != 0, n_tok % 2 != 0, n_tok % 3 == 0, n_splits, ws, n_tok);
         uint64_t groups = 0, covered = 0;
         for (const auto &u : units) {
             const int st = u.prefix ? c.prefix_tokens : c.split_tokens, most = u.prefix ? c.prefix_ns : c.ns - c.prefix_ns;
