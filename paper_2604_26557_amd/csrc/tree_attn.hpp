@@ -554,10 +554,14 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     int s0, s1;
     [[maybe_unused]] int from_most = begin, pos_least = INT_MAX, origin = len;   // all rows see what is between from_most and the context's end; none of their positions is below pos_least
     [[maybe_unused]] bool by_row = false;   // positions too far from one origin for 32 bits
+    [[maybe_unused]] int all_see = len, in_line = len;   // up to where, from from_most on, all rows see everything, and up to where a token's position is its number
     if constexpr (GROUP) {
         if (split >= splits) return;
         int from_least = begin;
-        if (total > len && !p.mask) end_of_rows = len + 1 + (int)quotient((unsigned)((int)rb * kRows + min(n_rows, kRows) - 1), (unsigned)p.G, p.by_g);
+        if (total > len && !p.mask) {
+            end_of_rows = len + 1 + (int)quotient((unsigned)((int)rb * kRows + min(n_rows, kRows) - 1), (unsigned)p.G, p.by_g);
+            all_see = len + 1 + (int)quotient((unsigned)((int)rb * kRows), (unsigned)p.G, p.by_g);
+        }
         if (p.from || p.to || (SHAPED && p.slopes)) {
             const int r = (int)rb * kRows + min(lane, min(n_rows, kRows) - 1), t = first + (int)quotient((unsigned)r, (unsigned)p.G, p.by_g);
             int lo = max(begin, p.from ? p.from[t] : 0), most = lo, up = p.to ? p.to[t] : 0, least = SHAPED && p.slopes ? p.positions[t] : 0, far = least;
@@ -584,6 +588,11 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
         const int share = splits == 1 ? seen : (int)((((unsigned)seen + splits - 1) / splits + 31) & ~31u);
         s0 = min(start + (int)split * share, (end + 31) & ~31);
         s1 = max(s0, min(s0 + share, end));
+        if (SHAPED && p.slopes && s1 > len) {   // are the new tokens' positions their numbers, as a chain's?
+            bool are = true;
+            for (int j = max(s0, len) + lane; j < s1; j += 64) are = are && p.positions[first + j - len] == j;
+            if (__all(are)) in_line = s1;
+        }
     } else {
         if (!split_has_tokens(split, p.split_tokens, total)) return;
         s0 = (int)split * p.split_tokens;
@@ -980,7 +989,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
                 for (int nb = 0; nb < NB; ++nb) s[nb][0] *= p.scale, s[nb][1] *= p.scale;
             }
             if (!p.slopes) return;
-            if (j0 + 31 <= pos_least && j0 + 32 <= len) {
+            if (j0 + 31 <= pos_least && min(j0 + 32, s1) <= in_line) {
                 const float at = (float)(j0 + group - origin);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
@@ -1028,7 +1037,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             if constexpr (kFirstK) __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (SHAPED) shape(s, j0);
-        if (j0 + 32 > len || there[0] != ~0u || (GROUP && j0 < from_most)) {
+        if (j0 + 32 > (GROUP ? all_see : len) || there[0] != ~0u || (GROUP && j0 < from_most)) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
             const P p = arguments<P>();
             const int row = (int)rb * kRows + here(n);
