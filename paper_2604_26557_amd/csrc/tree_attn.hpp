@@ -331,14 +331,14 @@ __device__ __forceinline__ float tanh_of(float y) { return tanh_within(fabsf(y) 
 // The same for what is finite; anything else becomes a NaN (one instruction instead of three).
 __device__ __forceinline__ float tanh_of_finite(float y) { return fmaf(y, 0.f, tanh_within(__builtin_amdgcn_fmed3f(y, -8.5f, 8.5f))); }
 
-// Query rows of a unit of kv_group_attn: which of 32 tokens from j on row r sees, as bits. Tokens before `begin` are another unit's; from len on they are new ones.
+// Which of 32 tokens from j on the rows of token t of a unit of kv_group_attn see, as bits: from `from` on, where the unit's tokens begin at least; from len to total they are new ones, of
+// which those before `to` are seen in any case.
 struct GroupRows {
-    int first, tokens, begin, len, total;   // the rows' tokens; where the unit's tokens begin, the new ones begin, and they end
+    int first, len, total;   // the first token of the rows; where the new ones begin, and end
 };
-__device__ __forceinline__ unsigned group_sees32(const GroupParams &p, const GroupRows &u, int r, int j)
+__device__ __forceinline__ unsigned group_sees32(const GroupParams &p, const GroupRows &u, int t, int from, int to, int j)
 {
     auto below = [](int x) { return x >= 32 ? ~0u : (1u << max(x, 0)) - 1u; };
-    const int t = min((int)quotient((unsigned)r, (unsigned)p.G, p.by_g), u.tokens - 1), at = u.first + t;
     unsigned seen = below(u.len - j);
     const unsigned drafted = below(u.total - j) & ~seen;
     if (drafted != 0) {
@@ -347,17 +347,17 @@ __device__ __forceinline__ unsigned group_sees32(const GroupParams &p, const Gro
         if (!p.mask) {
             bits = below(t + 1 - i);
         } else {
-            const unsigned long long *const row = p.mask + (long long)at * p.words;
+            const unsigned long long *const row = p.mask + (long long)(u.first + t) * p.words;
             const int w = max(i, 0) >> 6, shift = max(i, 0) & 63;
             unsigned long long x = w < p.words ? row[w] >> shift : 0;
             if (shift > 32 && w + 1 < p.words) x |= row[w + 1] << (64 - shift);
             if (i < 0) x <<= -i;
             bits = (unsigned)x;
         }
-        if (p.to) bits |= below(max(p.to[at], 0) - j);
+        bits |= below(max(to, 0) - j);
         seen |= drafted & bits;
     }
-    return seen & ~below(max(u.begin, p.from ? p.from[at] : 0) - j);
+    return seen & ~below(from - j);
 }
 
 // The same of 32 tokens from j on, as bits.
@@ -554,6 +554,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     int s0, s1;
     [[maybe_unused]] int from_most = begin, pos_least = INT_MAX, origin = len;   // all rows see what is between from_most and the context's end; none of their positions is below pos_least
     [[maybe_unused]] bool by_row = false;   // positions too far from one origin for 32 bits
+    [[maybe_unused]] int row_from = begin, row_to = 0, row_pos = 0;         // of the row with the lane's number
     [[maybe_unused]] int all_see = len, in_line = len;   // up to where, from from_most on, all rows see everything, and up to where a token's position is its number
     if constexpr (GROUP) {
         if (split >= splits) return;
@@ -564,7 +565,10 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
         }
         if (p.from || p.to || (SHAPED && p.slopes)) {
             const int r = (int)rb * kRows + min(lane, min(n_rows, kRows) - 1), t = first + (int)quotient((unsigned)r, (unsigned)p.G, p.by_g);
-            int lo = max(begin, p.from ? p.from[t] : 0), most = lo, up = p.to ? p.to[t] : 0, least = SHAPED && p.slopes ? p.positions[t] : 0, far = least;
+            row_from = max(begin, p.from ? p.from[t] : 0);
+            row_to = p.to ? p.to[t] : 0;
+            row_pos = SHAPED && p.slopes ? p.positions[t] : 0;
+            int lo = row_from, most = lo, up = row_to, least = row_pos, far = least;
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
                 lo = min(lo, __shfl_xor(lo, o));
@@ -1002,12 +1006,12 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     at[j] = j0 + here(group) + 4 * j;
-                    if (at[j] >= len) at[j] = p.positions[first + min(at[j] - len, drafted - 1)];
+                    if (at[j] >= len && s1 > in_line) at[j] = p.positions[first + min(at[j] - len, drafted - 1)];
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const int r = min(nb * 16 + here(n), n_rows - 1), pos = p.positions[first + row_token(r)], ahead = by_row ? 0 : pos - origin;
+                    const int r = min(nb * 16 + here(n), n_rows - 1), pos = __shfl(row_pos, nb * 16 + here(n)), ahead = by_row ? 0 : pos - origin;
                     const float slope = slope_of(p, r);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope, (float)(ahead - abs(pos - at[j])), s[nb][j / 4][j % 4]);
@@ -1040,11 +1044,12 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
         if (j0 + 32 > (GROUP ? all_see : len) || there[0] != ~0u || (GROUP && j0 < from_most)) {
             // Branch-free, for the compiler's sake too: with a condition for every token, inlined, it lost the masks of some instances.
             const P p = arguments<P>();
-            const int row = (int)rb * kRows + here(n);
+            [[maybe_unused]] const int row = (int)rb * kRows + here(n);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 unsigned seen;
-                if constexpr (GROUP) seen = there[0] & group_sees32(p, GroupRows{first, drafted, begin, len, total}, row + nb * 16, j0);
+                if constexpr (GROUP)
+                    seen = there[0] & group_sees32(p, GroupRows{first, len, total}, row_token(min(here(n) + nb * 16, n_rows - 1)), __shfl(row_from, nb * 16 + here(n)), __shfl(row_to, nb * 16 + here(n)), j0);
                 else seen = there[0] & row_sees32(p, first, row + nb * 16, j0, len, total);
                 seen >>= group;
 #pragma unroll
@@ -1124,10 +1129,11 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
         for (int i = wave; i < min(n_rows, kRows); i += kWaves) {
             const int r = (int)rb * kRows + i, t = row_token(i);
             if constexpr (GROUP) {
-                const GroupRows u{first, drafted, begin, len, total};
+                const GroupRows u{first, len, total};
+                const int from = max(begin, a.from ? a.from[first + t] : 0), to = a.to ? a.to[first + t] : 0;
                 const float bias = SHAPED && a.slopes ? a.slopes[(int)h * a.G + r - t * a.G] : 0.f;
                 const int pos = SHAPED && a.slopes ? a.positions[first + t] : 0;
-                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, r, j) & 1); },
+                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, t, from, to, j) & 1); },
                                            [&](float x, int j) {
                                                if constexpr (!SHAPED) return x * a.scale_log2e;
                                                x = a.cap > 0.f ? a.cap * tanh_of(x * a.cap_in) : x * a.scale;
