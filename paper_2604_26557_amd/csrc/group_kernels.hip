@@ -109,7 +109,11 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
     const bool shaped = t.cap > 0.f || t.slopes;
     // the error of a cap by sigmoids grows with it: beyond 64 it would show in 16-bit results
     if (t.out_mode != 0 && t.cap > 0.f && t.cap <= 64.f) t.sigmoid_in = -2.88539008f * t.cap_in;
-    t.scale_log2e = (float)(1.4426950408889634 * (!shaped ? scale : t.sigmoid_in != 0.f && !t.slopes ? 2. * t.cap : 1.));
+    // slopes without a cap are divided by the scale, unless that would leave the range of 32 bits: a multiplication of each score less
+    const bool divided = !(t.cap > 0.f) && scale > 1e-6 && scale < 1e6;
+    t.bias = divided ? (float)(1 / scale) : 1.f;
+    t.prescale = divided || t.cap > 0.f ? 1.f : t.scale;
+    t.scale_log2e = (float)(1.4426950408889634 * (!shaped || divided ? scale : t.sigmoid_in != 0.f && !t.slopes ? 2. * t.cap : 1.));
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;
     const TreeShape shape = tree_shape(p, format_bits(format), t.c.table != nullptr);
