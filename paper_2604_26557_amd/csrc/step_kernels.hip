@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "plan.hpp"
@@ -11,10 +12,9 @@ namespace {
 
 using namespace kvb;
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMostSequences = 8192;
-constexpr int kSegment = 512;       // entries of a row that a wavefront goes over, where rows are copied
-constexpr int kTokens = 4096;       // rows of the maps that a workgroup writes
+constexpr int kSegment = 256;       // entries of a row that a wavefront goes over, where rows are copied
+constexpr int kTokens = 2048;       // rows of the maps that a workgroup writes
 
 struct TablesParams {
     kv_tables_args_t a;
@@ -60,22 +60,44 @@ __device__ __forceinline__ int segment_of(const unsigned *first, int n, unsigned
     return lo;
 }
 
+// Sums over the lanes up to each: 1, 2, 4, 8 of a row of 16, then over rows. All lanes take part.
+__device__ __forceinline__ unsigned long long wave_sums_to(unsigned long long x)
+{
+    auto moved = [](unsigned long long x, auto ctrl, auto rows) {
+        const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(x >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        return (unsigned long long)hi << 32 | lo;
+    };
+    using std::integral_constant;
+    const integral_constant<int, 0xf> all;
+    x += moved(x, integral_constant<int, 0x111>{}, all);
+    x += moved(x, integral_constant<int, 0x112>{}, all);
+    x += moved(x, integral_constant<int, 0x114>{}, all);
+    x += moved(x, integral_constant<int, 0x118>{}, all);
+    x += moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+    x += moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return x;
+}
+
 // Every workgroup sums up all lengths by itself (a few loads a thread), so that one launch does: the first ones go over rows of the table, a wavefront a row or a part of it, the others
 // write the maps. In place it is one workgroup for the table, which looks everything up before it changes it. Bound by the launch and a chain of dependent loads: lengths, sums, the entry
-// of the stack, the table.
-template <int MOST>
+// of the stack, the table. TIMES
+template <int MOST, int kThreads>
 __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p)
 {
+    constexpr int kWaves = kThreads / 64;
+    constexpr bool kKept = MOST <= 1024;   // what a length says of its sequence, in LDS
     const kv_tables_args_t &a = p.a;
-    const int B = a.batch, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int B = a.batch, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     __shared__ unsigned first[MOST + 1], fresh[MOST + 1], gone[MOST + 1];
+    __shared__ int4 kept[kKept ? MOST : 1];   // need (-1: ended), held, shared entries, leader
     __shared__ unsigned long long sums[3][kWaves];
     __shared__ int unfit[kWaves];
-
     const bool maps = (int)blockIdx.x >= p.table_groups;
+    const int free_now = maps ? 0 : a.n_free[0];
 
-    // Sums before each sequence: a thread has `per` neighbouring ones.
-    const int per = (B + kThreads - 1) / kThreads, b0 = tid * per, b1 = min(b0 + per, B);
+    // Sums before each sequence: a thread has up to `per` neighbouring ones.
+    const int per = (B + kThreads - 1) / kThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
     unsigned long long mine[3] = {0, 0, 0};
     int over = 0;
     for (int b = b0; b < b1; ++b) {
@@ -84,22 +106,17 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         mine[1] += fresh_of(r);
         mine[2] += gone_of(r);
         over += r.need > a.max_blocks;
+        if constexpr (kKept) kept[b] = int4{r.ended ? -1 : (int)min(r.need, (long long)INT_MAX), r.held, r.common, r.leader};
     }
     unsigned long long before[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        unsigned long long x = mine[k];
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const unsigned long long y = __shfl_up(x, o);
-            if (lane >= o) x += y;
-        }
+        const unsigned long long x = wave_sums_to(mine[k]);
         before[k] = x - mine[k];
         if (lane == 63) sums[k][wave] = x;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) over += __shfl_xor(over, o);
-    if (lane == 0) unfit[wave] = over;
+    over = __popcll(__ballot(over > 0)) > 0 ? (int)wave_sums_to((unsigned long long)over) : 0;
+    if (lane == 63) unfit[wave] = over;
     __syncthreads();
     unsigned long long all[3] = {0, 0, 0};
     over = 0;
@@ -113,14 +130,31 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         }
     }
     auto count = [](unsigned long long x) { return (unsigned)min(x, (unsigned long long)INT_MAX); };
+    // as the lengths, or LDS, have it
+    auto request = [&](int b) {
+        if constexpr (kKept) {
+            const int4 k = kept[b];
+            Request r{};
+            r.need = max(k.x, 0);
+            r.held = k.y;
+            r.common = k.z;
+            r.leader = k.w;
+            r.ended = k.x < 0;
+            return r;
+        } else {
+            return request_of(a, b);
+        }
+    };
     for (int b = b0; b < b1; ++b) {
-        const Request r = request_of(a, b, maps);
         first[b] = count(before[0]);
         fresh[b] = count(before[1]);
         gone[b] = count(before[2]);
-        before[0] += r.news;
-        before[1] += fresh_of(r);
-        before[2] += gone_of(r);
+        if (b + 1 < b1) {
+            const Request r = request_of(a, b, maps);
+            before[0] += r.news;
+            before[1] += fresh_of(r);
+            before[2] += gone_of(r);
+        }
     }
     if (tid == 0) first[B] = count(all[0]), fresh[B] = count(all[1]), gone[B] = count(all[2]);
     __syncthreads();
@@ -136,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         return;
     }
 
-    const unsigned n_free = (unsigned)min(max(a.n_free[0], 0), a.n_pool);
+    const unsigned n_free = (unsigned)min(max(free_now, 0), a.n_pool);
     const unsigned long long top = n_free + all[2];   // of the stack, with what ends
     const bool fine = all[1] <= top && over == 0;
     // The block that is taken after k others. What ends in this call is looked up in its row.
@@ -145,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         if (i < n_free) return a.free_ids[i];
         const unsigned g = (unsigned)(i - n_free);
         const int b = segment_of(gone, B, g);
-        const int common = request_of(a, b).common;
+        const int common = request(b).common;
         return a.block_table[(long long)b * a.max_blocks + common + (int)(g - gone[b])];
     };
     // The entry i of row b as this call finds or fills it. Sequences without an offset of their own share it with the next: segment_of takes the last, which has some.
@@ -156,7 +190,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
     auto entry = [&](const Request &r, int b, int i) {
         if (r.ended) return -1;
         if (!(fine && i >= r.held && i < min((long long)r.common, r.need))) return filled(r, b, i);
-        const Request l = request_of(a, r.leader);
+        const Request l = request(r.leader);
         return l.ended || (i >= l.held && i < l.common) ? -1 : filled(l, r.leader, i);
     };
 
@@ -164,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         const int items = B * p.segments;
         for (int item = blockIdx.x * kWaves + wave; item < items; item += p.table_groups * kWaves) {
             const int b = item / p.segments, i0 = (item - b * p.segments) * kSegment, i1 = min(i0 + kSegment, a.max_blocks);
-            const Request r = request_of(a, b);
+            const Request r = request(b);
             for (int i = i0 + lane; i < i1; i += 64) {
                 const long long at = (long long)b * a.max_blocks + i;
                 if (r.ended && i >= r.common && i < r.held) {
@@ -178,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
     } else {
         // Fill and push, then clear: what ended is read until then. Its entries and what is filled are different places.
         for (int b = wave; b < B; b += kWaves) {
-            const Request r = request_of(a, b);
+            const Request r = request(b);
             const int i0 = r.ended ? r.common : r.held, i1 = r.ended ? r.held : fine ? (int)r.need : 0;
             for (int i = i0 + lane; i < i1; i += 64) {
                 const long long at = (long long)b * a.max_blocks + i;
@@ -192,13 +226,13 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
         }
         __syncthreads();
         for (int b = wave; b < B; b += kWaves) {
-            const Request r = request_of(a, b);
+            const Request r = request(b);
             for (int i = lane; r.ended && i < a.max_blocks; i += 64) a.block_table_out[(long long)b * a.max_blocks + i] = -1;
         }
         __syncthreads();
         // each thread its own sequences: nobody else looks at what they held any more
         for (int b = b0; b < b1; ++b) {
-            const Request r = request_of(a, b);
+            const Request r = request(b);
             a.held_out[b] = r.ended ? 0 : fine ? (int)max((long long)r.held, r.need) : r.held;
         }
     }
@@ -228,10 +262,13 @@ extern "C" int kv_step_tables(const kv_tables_args_t *a, void *hip_stream)
     p.a = *a;
     p.in_place = in_place;
     p.segments = in_place ? 1 : std::max(1, (a->max_blocks + kSegment - 1) / kSegment);
-    p.table_groups = in_place ? 1 : std::min(256, (a->batch * p.segments + kWaves - 1) / kWaves);
+    // in place one workgroup has all rows: as many wavefronts as it may have
+    const bool few = a->batch <= 1024 && !in_place;
+    const int threads = !few ? 1024 : a->batch <= 256 ? 256 : 512, waves = threads / 64;   // a sequence each, for most
+    p.table_groups = in_place ? 1 : std::min(few ? 1024 : 256, (a->batch * p.segments + waves - 1) / waves);
     const unsigned maps = (unsigned)((a->n_tok + (int64_t)kTokens - 1) / kTokens);
-    (void)launch_kernel(a->batch <= 1024 ? kv_step_tables_kernel<1024> : kv_step_tables_kernel<kMostSequences>, dim3((unsigned)p.table_groups + maps), dim3(kThreads),
-                        (hipStream_t)hip_stream, p);
+    (void)launch_kernel(threads == 256 ? kv_step_tables_kernel<1024, 256> : threads == 512 ? kv_step_tables_kernel<1024, 512> : a->batch <= 1024 ? kv_step_tables_kernel<1024, 1024> : kv_step_tables_kernel<kMostSequences, 1024>,
+                        dim3((unsigned)p.table_groups + maps), dim3((unsigned)threads), (hipStream_t)hip_stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_hip_error((int)e); return KV_EHIP; }
     return KV_OK;
