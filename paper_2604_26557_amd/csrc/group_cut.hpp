@@ -24,14 +24,12 @@ struct GroupCut {
 
 inline int splits_of(int span, int split_tokens) { return span <= 0 ? 0 : (span - 1) / split_tokens + 1; }
 
-// Workgroups of a unit: its splits of all heads, in eights where it has several row blocks, times these.
+// Workgroups of a unit: its splits of all heads, times its row blocks.
 inline uint64_t unit_workgroups(const TreeShape &s, const GroupUnit &u, int nb, int split_tokens)
 {
     if (u.tokens <= 0 || u.span <= 0) return 0;
     const uint64_t rows = (uint64_t)u.tokens * s.G, blocks = (rows + 16 * nb - 1) / (16 * nb);
-    uint64_t units = (uint64_t)splits_of(u.span, split_tokens) * s.H;
-    if (blocks > 1) units = (units + 7) / 8 * 8;
-    return units * blocks;
+    return (uint64_t)splits_of(u.span, split_tokens) * s.H * blocks;
 }
 
 // Unit i of groups, then sequences: span of a sequence's own tokens begins at a multiple of 32.
@@ -135,7 +133,7 @@ inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, boo
         return best;
     }
     // lengths of which those past twice a kind's longest say nothing new; the last is the whole
-    static constexpr int kLengths[] = {128, 256, 384, 512, 768, 1024, 1536, 2048, 3072, 4096, 8192, 16384};
+    static constexpr int kLengths[] = {128, 256, 384, 512, 768, 1024, 1536, 2048, 2816, 4096, 8192, 16384};
     for (int i = 0; i <= 12; ++i) {
         const bool whole = i == 12 || kLengths[i] >= own.longest;
         for (int j = 0; j <= 12; ++j) {
