@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(64 * kCombineWaves) kv_group_combine_kernel(Gr
     const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * kCombineWaves + (int)(threadIdx.x >> 6));
     const int first = load_uniform(p.tok_first + b), drafted = load_uniform(p.tok_first + b + 1) - first;
     int shared = 0;
-    if (p.n_groups > 0) {
+    if (p.n_groups > 0 && !p.joined) {
         const bool of = lane < p.n_groups && b >= p.group_first[lane] && b < p.group_first[lane + 1];
         const unsigned long long which = __ballot(of);
         if (which != 0) shared = load_uniform(p.prefix + __ffsll((long long)which) - 1);
@@ -117,10 +117,12 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
 
     const int format = blocks ? blocks->format : KV_FORMAT_16;
     const TreeShape shape = tree_shape(p, format_bits(format), t.c.table != nullptr);
-    GroupUnit few[256];
-    const std::unique_ptr<GroupUnit[]> many(n_groups + p->B > 256 ? new (std::nothrow) GroupUnit[(size_t)n_groups + p->B] : nullptr);
-    if (n_groups + p->B > 256 && !many) return KV_ENOSPC;
-    GroupUnit *const units = many ? many.get() : few;
+    // prefixes and sequences, and sequences alone
+    GroupUnit few[384];
+    const size_t n_most = (size_t)n_groups + 2 * (size_t)p->B;
+    const std::unique_ptr<GroupUnit[]> many(n_most > 384 ? new (std::nothrow) GroupUnit[n_most] : nullptr);
+    if (n_most > 384 && !many) return KV_ENOSPC;
+    GroupUnit *units = many ? many.get() : few;
     int n_units = 0;
     bool any_prefix = false;
     for (int i = 0, g = 0; i < n_groups + p->B; ++i) {
@@ -133,7 +135,22 @@ extern "C" int kv_group_attn(const kv_plan_t *p, const kv_view_t *view, const kv
         any_prefix = any_prefix || u.prefix;
     }
     if (any_prefix && ws_bytes < 2 * tree_split_bytes(shape, n_tok)) return KV_ENOSPC;
-    const GroupCut cut = cut_group(shape, units, n_units, !a->mask, t.from != nullptr, shaped, a->n_splits, ws_bytes, n_tok);
+    GroupCut cut = cut_group(shape, units, n_units, !a->mask, t.from != nullptr, shaped, a->n_splits, ws_bytes, n_tok);
+    if (any_prefix && a->n_splits == 0) {
+        GroupUnit *const own = units + n_groups + p->B;
+        int n_own = 0;
+        for (int b = 0; b < p->B; ++b) {
+            const GroupUnit u = group_unit(b, 0, nullptr, nullptr, view->seq_lens_host, a->tok_first_host, 0);
+            if (u.tokens > 0 && u.span > 0) own[n_own++] = u;
+        }
+        const GroupCut joined = cut_group(shape, own, n_own, !a->mask, t.from != nullptr, shaped, 0, ws_bytes, n_tok);
+        if (better_joined(joined, cut, !a->mask, n_tok, p->B)) {
+            cut = joined;
+            units = own;
+            n_units = n_own;
+            t.joined = 1;
+        }
+    }
     t.ns = cut.ns;
     t.prefix_ns = cut.prefix_ns;
     t.split_tokens = cut.split_tokens;

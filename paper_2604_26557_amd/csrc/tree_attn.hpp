@@ -61,6 +61,7 @@ struct TreeParams {
 struct GroupParams : TreeParams {
     const int *group_first, *prefix;   // [n_groups + 1], [n_groups]
     int n_groups, prefix_ns;           // partial results of a row that are of its prefix
+    int joined;                        // no units of prefixes: sequences go over theirs themselves, in the place of the group's first
     int prefix_tokens;                 // of a split of a prefix, a multiple of 32
     unsigned by_prefix;
     // In kernels whose scores are capped or biased: what q K^T is multiplied by first (1: nothing), and slopes; the softmax multiplies by scale_log2e what comes of it.
@@ -397,15 +398,16 @@ __device__ __forceinline__ void store_sums(const TreeParams &p, int token, int h
 // One query row over a split on the vector ALU, a token at a time: its largest score, then its sums.  Whatever the cache holds, nothing but what the row sees
 // enters them.  A lane has four columns (of which several lanes may have the same).
 // sees(j): does it see token j; shaped(x, j): its score times log2(e), from its product with K.
-template <int D, bool BF16, int FORMAT, typename Sees, typename Shaped>
-__device__ __forceinline__ void plain_row(const TreeParams &p, const int *table, unsigned long long base, unsigned long long zbase, unsigned h, int first, int r, int t,
+// place(c, j): where the cache has it.
+template <int D, bool BF16, int FORMAT, typename Place, typename Sees, typename Shaped>
+__device__ __forceinline__ void plain_row(const TreeParams &p, const Place &place, unsigned h, int first, int r, int t,
                                        int s0, int s1, unsigned split, int lane, const Sees &sees, const Shaped &shaped)
 {
     const int hq = (int)h * p.G + r - t * p.G, at = lane % (D / 4);
     const u32x2 qw = *(const u32x2 *)(p.q + 2 * ((first + t) * p.q_st + hq * p.q_sh + 4 * at));
     const f32x2 q0 = unpack2<BF16>(qw[0] ^ p.q_sign), q1 = unpack2<BF16>(qw[1] ^ p.q_sign);
     auto row = [&](const char *rows, const char *scales, int j, bool *there) {
-        const RowAt x = row_at(p.c, table, base, zbase, j);
+        const RowAt x = place(p.c, j);
         *there = x.there;
         u32x2 w;
         if constexpr (FORMAT == KV_FORMAT_16) {
@@ -455,6 +457,9 @@ struct Unit {
     int begin = 0, end_of_rows = 0;
     unsigned slot = 0, splits = 1;
     bool is_prefix = false;
+    // where prefixes are joined: the tokens before `shared` are those of sequence `lead`
+    int shared = 0;
+    unsigned lead = 0;
 };
 
 // Of ROWS_PREFIX query rows of a group over its prefix, or ROWS of a sequence. false: no work.
@@ -471,10 +476,10 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
         group_end = p.group_first[lane + 1];
         shared = p.prefix[lane];
     }
-    for (int b0 = p.n_groups > 0 ? -1 : 0; b0 < p.B; b0 = b0 < 0 ? 0 : b0 + 64) {
+    for (int b0 = p.n_groups > 0 && !p.joined ? -1 : 0; b0 < p.B; b0 = b0 < 0 ? 0 : b0 + 64) {
         const bool is_group = b0 < 0;
         const int rows = is_group ? ROWS_PREFIX : ROWS;
-        int f = 0, n = 0, l = 0, from = 0, kb = 0;   // first token, their number, context, where the unit's tokens begin, sequence in whose place they are
+        int f = 0, n = 0, l = 0, from = 0, kb = 0, lead = 0;   // first token, their number, context, where the unit's tokens begin, sequence in whose place they are
         if (is_group) {
             if (lane < p.n_groups && shared > 0) {
                 f = p.tok_first[group_first];
@@ -487,6 +492,7 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
             for (int g = 0; g < p.n_groups; ++g) {
                 const int x = __builtin_amdgcn_readlane(group_first, g), y = __builtin_amdgcn_readlane(group_end, g), z = __builtin_amdgcn_readlane(shared, g);
                 from = kb >= x && kb < y ? z : from;
+                lead = kb >= x && kb < y ? x : lead;
             }
             if (kb < p.B) {
                 f = p.tok_first[kb];
@@ -497,7 +503,7 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
         const int st = is_group ? p.prefix_tokens : p.split_tokens;
         unsigned units = 0, of_unit = 0;
         if (n > 0) {
-            const int span = is_group ? l : l + n - (from & ~31);
+            const int span = is_group ? l : l + n - (p.joined ? 0 : from & ~31);
             of_unit = quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1;
             units = of_unit * (unsigned)p.H;
         }
@@ -518,6 +524,11 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
         u.drafted = __builtin_amdgcn_readlane(n, which);
         u.len = __builtin_amdgcn_readlane(l, which);
         u.begin = __builtin_amdgcn_readlane(from, which);
+        if (p.joined) {
+            u.shared = u.begin;
+            u.begin = 0;
+            u.lead = (unsigned)__builtin_amdgcn_readlane(lead, which);
+        }
         u.b = (unsigned)__builtin_amdgcn_readlane(kb, which);
         units = (unsigned)__builtin_amdgcn_readlane((int)units, which);
         u.splits = (unsigned)__builtin_amdgcn_readlane((int)of_unit, which);
@@ -613,6 +624,13 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     const unsigned long long base = p.c.table ? h * p.c.sh : b * p.c.sb + h * p.c.sh;
     const unsigned long long zbase = p.c.table ? h * p.c.zh : b * p.c.zb + h * p.c.zh;
     const int *const table = p.c.table ? p.c.table + (long long)b * p.c.max_blocks : nullptr;
+    // A row of K and V: of the sequence's place, or before `shared` of the leader's.
+    const int shared = GROUP ? u.shared : 0;
+    auto place = [=](const CacheAddr &c, int j) {
+        const bool of_lead = GROUP && j < shared;
+        const long long off = of_lead ? (long long)u.lead - b : 0;
+        return row_at(c, table + (c.table ? off * c.max_blocks : 0), c.table ? base : base + off * c.sb, c.table ? zbase : zbase + off * c.zb, j);
+    };
 
     // lds: the ring of each wavefront's stages, then q; after the last step the merge's rows and states.
     const unsigned ring_at = (unsigned)wave * (kStages * T::kStage);
@@ -632,32 +650,52 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
     // Kernels with biases go from the last tokens to the first: the nearest weigh the most, and a reference that is near the largest from the start stays (the other way round it moved at every step,
     // and the sums with it: a prompt of 4K took 334 us with slopes where 253 are its time without).
     constexpr bool kBack = SHAPED;
+    // The wavefront's step with tokens of both places, and in caches without blocks the one from which on the other place's starts are taken.
+    [[maybe_unused]] int both_places = -1, turn = -1;
+    unsigned long long start = base, zstart = zbase;
+    if (GROUP && shared > s0 && mine > 0) {
+        const int of_lead = (shared - s0 - 32 * wave + 32 * kWaves - 1) / (32 * kWaves), i = max(0, min(of_lead, mine));   // steps that begin before `shared`
+        if ((shared & 31) && i > 0 && (shared - s0) / 32 == wave + (i - 1) * kWaves) both_places = kBack ? mine - i : i - 1;
+        turn = kBack ? mine - i : i;
+        if (!kBack && i > 0 && !p.c.table) {
+            start += ((long long)u.lead - b) * p.c.sb;
+            zstart += ((long long)u.lead - b) * p.c.zb;
+        }
+        if (!kBack && i == 0) turn = -1;
+    }
     auto where = [&](int m) {   // this wavefront's m-th step; called for each in turn
         const int j0 = s0 + 32 * (wave + (kBack ? mine - 1 - m : m) * kWaves), left = total - 1 - j0;
         const int lowest = GROUP ? max(0, begin - j0) : 0;   // before it rows are another sequence's
-        groups = p.grouped && left >= 31 && lowest == 0;
+        const bool of_both = GROUP && m == both_places;
+        groups = p.grouped && left >= 31 && lowest == 0 && !of_both;
         next_there = ~0u;
-        if (!p.grouped) {
-            const CacheAddr c = arguments<P>().c;
-            const RowAt r = row_at(c, table, base, zbase, j0 + max(min(lane & 31, left), lowest));
+        auto by_row = [&] {
+            const RowAt r = place(arguments<P>().c, j0 + max(min(lane & 31, left), lowest));
             lane_at = r.at;
             lane_z = r.z;
             next_there = (unsigned)__ballot(r.there);
+        };
+        if (!p.grouped) {
+            by_row();
             return;
         }
         if (!p.c.table) {
             // from one step to the next a sum, not a product
-            at0 = m == 0 ? base + (unsigned)j0 * p.c.ss : kBack ? at0 - 32 * kWaves * (unsigned)p.c.ss : at0 + 32 * kWaves * (unsigned)p.c.ss;
-            at1 = at0 + 16 * (unsigned)p.c.ss;
-            if (T::kBlocks) {
-                z0 = m == 0 ? zbase + (unsigned)j0 * p.c.zs : kBack ? z0 - 32 * kWaves * (unsigned)p.c.zs : z0 + 32 * kWaves * (unsigned)p.c.zs;
-                z1 = z0 + 16 * (unsigned)p.c.zs;
+            at0 = m == 0 ? start + (unsigned)j0 * p.c.ss : kBack ? at0 - 32 * kWaves * (unsigned)p.c.ss : at0 + 32 * kWaves * (unsigned)p.c.ss;
+            if (T::kBlocks) z0 = m == 0 ? zstart + (unsigned)j0 * p.c.zs : kBack ? z0 - 32 * kWaves * (unsigned)p.c.zs : z0 + 32 * kWaves * (unsigned)p.c.zs;
+            if (GROUP && m == turn) {   // to the leader's place, or back
+                const P p = arguments<P>();
+                const long long off = kBack ? (long long)u.lead - b : (long long)b - u.lead;
+                at0 += off * p.c.sb;
+                z0 += off * p.c.zb;
             }
+            at1 = at0 + 16 * (unsigned)p.c.ss;
+            if (T::kBlocks) z1 = z0 + 16 * (unsigned)p.c.zs;
         } else {
             if (m % 32 == 0) {   // the starts of 32 steps at a time, a lane each
                 const P p = arguments<P>();
                 const int j = min(kBack ? max(j0 - 32 * kWaves * (lane >> 1), 0) + 16 * (lane & 1) : j0 + 32 * kWaves * (lane >> 1) + 16 * (lane & 1), total - 1) & ~15, at = p.bt_shift >= 0 ? j >> p.bt_shift : j / p.c.bt;
-                unsigned id = (unsigned)table[at];
+                unsigned id = (unsigned)table[at + (GROUP && j < shared ? ((int)u.lead - (int)b) * (long long)p.c.max_blocks : 0)];
                 const unsigned in = j - at * p.c.bt;
                 ids_there = __ballot(id < (unsigned)p.c.n_pool);
                 id = id < (unsigned)p.c.n_pool ? id : 0;
@@ -678,7 +716,9 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
             const unsigned both = (unsigned)(ids_there >> l) & 3;
             next_there = both == 3 ? ~0u : both == 2 ? 0xffff0000u : both == 1 ? 0xffffu : 0;
         }
-        if (!groups) {
+        if (of_both) {
+            by_row();
+        } else if (!groups) {
             const int t = max(min(lane & 31, left), lowest);
             lane_at = (t & 16 ? at1 : at0) + (unsigned)(t & 15) * (unsigned)p.c.ss;
             lane_z = (t & 16 ? z1 : z0) + (unsigned)(t & 15) * (unsigned)p.c.zs;
@@ -1143,7 +1183,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
                 const int from = max(begin, a.from ? a.from[first + t] : 0), to = a.to ? a.to[first + t] : 0;
                 const float bias = SHAPED && a.slopes ? a.slopes[(int)h * a.G + r - t * a.G] : 0.f;
                 const int pos = SHAPED && a.slopes ? a.positions[first + t] : 0;
-                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, t, from, to, j) & 1); },
+                plain_row<D, BF16, FORMAT>(a, place, h, first, r, t, s0, s1, slot + split, lane, [&](int j) { return (bool)(group_sees32(a, u, t, from, to, j) & 1); },
                                            [&](float x, int j) {
                                                if constexpr (!SHAPED) return x * a.scale_log2e;
                                                x = a.cap > 0.f ? a.cap * tanh_of(x * a.cap_in) : x * a.scale;
@@ -1152,7 +1192,7 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
                                                return x * 1.44269504f;
                                            });
             } else {
-                plain_row<D, BF16, FORMAT>(a, table, base, zbase, h, first, r, t, s0, s1, split, lane, [&](int j) { return row_sees(a, first, r, j, len, total); },
+                plain_row<D, BF16, FORMAT>(a, place, h, first, r, t, s0, s1, split, lane, [&](int j) { return row_sees(a, first, r, j, len, total); },
                                            [&](float x, int) { return x * a.scale_log2e; });
             }
         }

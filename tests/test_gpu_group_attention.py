@@ -357,3 +357,93 @@ def test_rows_looked_up_one_by_one():
         b.c.dev[kind] = far
     b.c.remake()
     assert torch.equal(b.attend(n_splits=1), want)
+
+
+# ------------------------------------------------------------------------------------------ many rows behind a prefix: sequences go over it each for itself
+@pytest.mark.parametrize("layout,bt", [("bhsd", 0), ("paged", 16), ("paged", 32), ("paged", 8), ("paged", 48)])
+@pytest.mark.parametrize("fmt", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("P", [1, 15, 16, 31, 32, 33, 100, 129, 515])
+def test_prompts_behind_a_prefix(layout, bt, fmt, P):
+    """The last of it may be anywhere in a tile; the sequence that holds it is not the first, and may have no new tokens itself."""
+    lens, news = [20, P, P + 5, P + 70, 3], [9, 0 if P % 2 else 140, 33, 200, 1]
+    kw = dict(slopes=slopes_of(4), cap=20.0) if P % 3 == 0 else dict(cap=0.0)
+    b = Batch(lens, news, 2, 2, 64, torch.bfloat16, fmt, layout, bt=bt or 16, seed=P, first=[1, 4], prefix=[P], **kw)
+    b.check(b.attend())
+    b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("D,H,G,dtype", [(64, 1, 6, torch.float16), (128, 2, 3, torch.bfloat16), (256, 1, 2, torch.float16)])
+def test_prompts_behind_prefixes_of_two_groups(fmt, D, H, G, dtype):
+    lens, news, at = [70, 90, 300, 250, 280], [150, 131, 7, 140, 260], []
+    for n, t in zip(lens, news):
+        at += range(n, n + t)
+    for kw in (dict(), dict(slopes=slopes_of(H * G)), dict(cap=5.0, sees_from=[max(0, j - 100) for j in at])):
+        b = Batch(lens, news, H, G, D, dtype, fmt, "paged" if D == 64 else "bhsd", seed=D, first=[0, 2, 5], prefix=[60, 250], **kw)
+        b.check(b.attend())
+        b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+def test_what_followers_hold_of_a_prefix_before_their_prompts_is_not_read():
+    """As above: NaN and blocks that are not there change no bit."""
+    for layout, fmt in (("bhsd", "16"), ("paged", "16"), ("paged", "fp8"), ("bhsd", "fp4")):
+        P = 117
+        b = Batch([P + 3, P + 50, P], [100, 140, 170], 2, 4, 128, torch.bfloat16, fmt, layout, seed=5, first=[0, 3], prefix=[P])
+        want = b.attend()
+        b.check(want)
+        for s in (1, 2):
+            for j in range(P):
+                i, r = b.c.place(s, j)
+                for kind in "kv":
+                    if fmt == "16":
+                        b.c.dev[kind][i, :, r] = float("nan")
+                    else:
+                        b.c.dev[kind + "_scale"][i, :, r] = 255
+        assert torch.equal(b.attend(), want)
+        if layout == "paged":
+            b.c.table[1:, :P // 16] = 2 ** 31 - 1
+            assert torch.equal(b.attend(), want)
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+@pytest.mark.parametrize("layout,bt", [("bhsd", 0), ("paged", 16), ("paged", 24)])
+def test_long_prefixes_and_contexts(layout, bt, fmt):
+    """More tokens than the block ids that a wavefront looks up at once (4096), from both ends, whole and in splits."""
+    for P, more in ((4300, 40), (0, 9000)):
+        for kw in (dict(), dict(slopes=slopes_of(2), cap=30.0)):
+            lens, news = [P + more, P + 7], [131 if P else 3, 130 if P else 2]
+            b = Batch(lens, news, 1, 2, 64, torch.float16, fmt, layout, bt=bt or 16, seed=P + 1, first=[0, 2] if P else (), prefix=[P] if P else (), **kw)
+            for n_splits in (0, 1, 2):
+                b.check(b.attend(n_splits=n_splits))
+
+
+def test_slopes_of_groups_wider_than_a_wavefront():
+    """A row block has rows of some heads of a token, and of several tokens."""
+    for G, D in ((70, 64), (33, 128), (11, 256)):
+        b = Batch([130, 40], [3, 2], 1, G, D, torch.bfloat16, seed=G, slopes=slopes_of(G), first=[0, 2], prefix=[40])
+        for n_splits in (0, 1, 2):
+            b.check(b.attend(n_splits=n_splits))
+        b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+@pytest.mark.parametrize("H", [1, 2, 3, 5, 7, 9, 10])
+def test_heads_that_are_no_eights(H):
+    b = Batch([100, 0], [90, 140], H, 2, 64, torch.float16, seed=H, cap=9.0)
+    for n_splits in (0, 1, 3):
+        b.check(b.attend(n_splits=n_splits))
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own():
+    """On two streams, again and again: the bits of each alone."""
+    a = Batch([900, 40], [2, 9], 2, 4, 128, torch.bfloat16, seed=1, first=[0, 2], prefix=[40])
+    b = Batch([500, 700], [9, 1], 2, 4, 128, torch.bfloat16, seed=2, cap=9.0)
+    want = [x.attend(n_splits=4) for x in (a, b)]
+    size = kv.kv_group_attn_workspace(a.c.plan, 11, 900)
+    runs = [(x, torch.empty(size, dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), x.handles(), x.q.cuda(), torch.zeros_like(w)) for x, w in zip((a, b), want)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, ws, s, (tree, groups, scores), q, out in runs:
+            kv.kv_group_attn(x.c.plan, x.c.view, x.c.blocks, 0, tree, q, out, kv.KV_OUT_F32, 4, ws, groups, scores, stream=s)
+    torch.cuda.synchronize()
+    for w, run in zip(want, runs):
+        assert torch.equal(run[-1], w)
