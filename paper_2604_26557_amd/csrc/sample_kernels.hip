@@ -6,12 +6,15 @@
 //
 // A workgroup has a row. It is read from HBM once, for its maximum, and from L2 after that.
 //   Few of the largest (top_k up to 256): no fewer than k tokens reach the k-th largest of the threads' own maxima; a list of those that do is all there is to rank.
-//   top_p alone: the sum of all, and a histogram over distances from the maximum. Tokens below (1 - p) / n_vocab of the sum are not needed to get from p to the whole: a sample says about where that is, and
-//     only what is above goes into the histogram (a third of the tokens in a usual case). Then a list of what is kept for sure, and one of the bin with the border, which is ranked.
-//   min_p alone: a list of what is above.
-//   What these have no room for, or larger top_k: histograms over the whole row, of its keys in the end, in as many rounds as they need.
+//   More of them, without top_p: a histogram of their number by distance from the maximum says which bin the k-th is in; what is above is kept, the bin is a list, which is ranked.  2 rows of 106775
+//     in 32 bits, the largest 1000: 62 us; 115 by the rounds below.
+//   top_p alone: the sum of all, and a histogram of weights by distance from the maximum.  Tokens below (1 - p) / n_vocab of the sum are not needed to get from p to the whole: a sample says about where
+//     that is, and only what is above goes into the histogram (a third of the tokens in a usual case).  Then as before.
+//   min_p alone: what is above it is kept.
+//   What these have no room for, and top_k past 256 with top_p: histograms over the whole row, of its keys in the end, in as many rounds as they need.
 // What bounds it: some 30 instructions, most of them in double precision, for every weight where the sum of all is needed, otherwise a pass' latencies.  So few rows of many tokens are shared by several
-// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 75 us with a workgroup each, SPLIT_TIME so.
+// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 46 us, 75 with a workgroup each.  One row
+// of 32000 in 32 bits with top_k and top_p takes 16 us: a workgroup's three passes, and what its threads tell each other, one after the other.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -300,6 +303,17 @@ struct Row {
         });
         return sum;
     }
+    // The histogram of numbers of tokens.
+    __device__ __forceinline__ void count_bins(int tid, int threads, float per, u64 *count) const
+    {
+        for_loads<DTYPE, 4>(at, V, tid, threads, [&](const float (&l)[E], int, int n) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float bin = (top - l[e]) * per;
+                if (e < n && bin < (float)kBins) atomicAdd(&count[(int)bin], 1ull);
+            }
+        });
+    }
     __device__ __forceinline__ void sum_tiles(int tid, int threads, u64 *weight) const
     {
         for_loads<DTYPE, 1>(at, V, tid, threads, [&](const float (&l)[E], int i, int n) {
@@ -312,6 +326,7 @@ struct Row {
     __device__ __forceinline__ bool nothing_cut() const { return !greedy && !cut_k && !cut_p && !(min_p > 0.f); }
     __device__ __forceinline__ bool by_bins() const { return !cut_k && cut_p; }
     __device__ __forceinline__ bool few() const { return cut_k && k <= 256; }
+    __device__ __forceinline__ bool by_counts() const { return cut_k && k > 256 && !cut_p; }
     __device__ __forceinline__ u64 target_of(u64 sum) const   // of top_p
     {
         const double want = ceil((double)(top_p > 0.f ? top_p : 0.f) * (double)sum);
@@ -702,7 +717,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
     // What is kept for sure, in s.tile_weight, and what may be: s.some
     bool fits = false;
     u64 in_bin = 0;
-    if (state) {
+    if (state && !row.by_counts()) {
         fits = state->fits != 0 && state->n_some <= (unsigned)kRanked;
         if (fits) {
             s.tile_weight[tid] = state->tile_weight[tid];
@@ -724,6 +739,19 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             if (per != 0.f) {
                 const u64 sum = g.sum_of(row.sum_and_bins(tid, kThreads, per, s.weight));
                 const unsigned bin = g.bin_of_target(row.target_of(sum), &in_bin);
+                if (bin < (unsigned)kBins) {
+                    if (bin > 0) sure = g.least_of(row, per, (float)bin);
+                    from = g.least_of(row, per, (float)bin + 1.f);
+                }
+            }
+        } else if (row.by_counts()) {
+            s.weight[tid] = s.weight[kThreads + tid] = 0;
+            __syncthreads();
+            const float per = 64.f / T;
+            if (per <= FLT_MAX) {
+                row.count_bins(tid, kThreads, per, s.weight);
+                __syncthreads();
+                const unsigned bin = g.bin_of_target(k, &in_bin);
                 if (bin < (unsigned)kBins) {
                     if (bin > 0) sure = g.least_of(row, per, (float)bin);
                     from = g.least_of(row, per, (float)bin + 1.f);
@@ -761,7 +789,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
                 in = in && before_in_order(n, std::true_type{}) < target;
             }
         } else {
-            in = in && before_in_order(n, std::true_type{}) < in_bin;
+            in = in && (row.by_counts() ? before_in_order(n, std::false_type{}) : before_in_order(n, std::true_type{})) < in_bin;
         }
         if (in) {
             atomicMin(&s.told_all, s.ranked[tid]);

@@ -402,3 +402,58 @@ def test_a_batch_decodes_behind_a_shared_prompt(fmt):
             want = p @ vb[:, h // G] / p.sum()
             # scores below 20 with (64 + 8 + 16) roundings of at most their terms' sum, some 30; weights off by that twice
             assert np.abs(last[0][b, h].double().cpu().numpy() - want).max() <= 2 * 30 * 90 * 2.0 ** -24 * np.abs(vb).max()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,B", [(66000, 5), (70001, 40), (65537, 127), (65537, 128)])
+def test_sample_rows_shared_by_workgroups(dtype, V, B):
+    """Long rows, few enough to be shared, and one more: each way through them, ties by the thousand, rows without an answer, odd starts."""
+    gen = torch.Generator().manual_seed(V + B)
+    rows = 5 if B <= 40 else 3
+    x = torch.randn((rows, V + 3), generator=gen) * 2
+    x[1] = torch.round(x[1])          # ties by the thousand, in the bin of any border
+    x[2, 5:] = x[2, 5:] * 0.01        # flat, and some above
+    if rows > 3:
+        x[3, 7] = float("nan")
+        x[4, V // 2:] = float("-inf")
+    x = x.to(dtype).cuda()[torch.arange(B) % rows]
+    u = np.random.default_rng(B).random(B)
+    some = [0, 1, 2, 3, 4] + list(range(B - 3, B)) if B <= 40 else [0, 1, 2, B - 1]
+    for start, kw in ((0, dict(t=[0.0] * B)), (0, dict()), (1, dict(p=0.9)), (2, dict(k=40, p=0.8)), (0, dict(k=256)), (3, dict(k=257)), (1, dict(k=2000)), (0, dict(k=2000, m=0.001)), (0, dict(m=0.02)),
+                      (1, dict(p=0.999, t=3.0)), (0, dict(k=900, p=0.95)), (0, dict(p=0.9, m=0.1))):
+        part = x[:, start:start + V]
+        tokens, probs = sample(part, u, **kw)
+        host = part[some].double().cpu().numpy()
+        for r, b in enumerate(some):
+            token, prob = ref_sample(host[r], **{n: float(np.float32(v[b] if isinstance(v, list) else v)) if n != "k" else v for n, v in kw.items()}, u=float(np.float32(u[b])))
+            assert tokens[b] == token, (b, kw, tokens[b], token)
+            assert abs(probs[b] - prob) <= 2.0 ** -23 * prob + V * 2.0 ** -39, (b, kw, probs[b], prob)
+
+
+@pytest.mark.parametrize("V", [300, 5000, 40000])
+def test_sample_of_more_than_256(V):
+    """top_k past what is ranked at once, alone and with min_p: bins that hold more ties than a list, temperatures that leave a bin or all of them, infinities."""
+    x = torch.randn((6, V), generator=torch.Generator().manual_seed(V)) * 2
+    x[1] = torch.round(x[1])
+    x[2] = 1.5
+    x[3, V // 3:] = float("-inf")
+    x[4] = x[4] * 40
+    x[5] = x[5].clamp(max=0.5)
+    x = x.cuda()
+    for k in (257, 270, V // 2, V - 1):
+        for kw in (dict(), dict(t=0.01), dict(t=1.0e-38), dict(t=100.0), dict(m=0.05), dict(t=3.0, m=0.3)):
+            check_sample(x, np.random.default_rng(k).random(6), k=k, **kw)
+
+
+def test_sample_with_the_workspace_of_more_rows():
+    """Fewer rows than the workspace is for, of a kind that needs more of it each."""
+    V = 66000
+    x = (torch.randn((9, V), generator=torch.Generator().manual_seed(9)) * 2).to(torch.bfloat16).cuda()
+    ws = torch.empty(kv.kv_sample_workspace(200, V), dtype=torch.uint8, device="cuda").fill_(255)
+    u = torch.full((9,), 0.5, device="cuda")
+    p = torch.full((9,), 0.9, device="cuda")
+    want = sample(x, [0.5] * 9, p=0.9)[0]
+    for n in (9, 5, 1):
+        tokens = i32([-9] * 9)
+        kv.kv_sample(x[:n], u[:n], tokens[:n], ws, top_p=p[:n])
+        assert tokens.tolist() == want[:n] + [-9] * (9 - n)
