@@ -457,3 +457,18 @@ def test_sample_with_the_workspace_of_more_rows():
         tokens = i32([-9] * 9)
         kv.kv_sample(x[:n], u[:n], tokens[:n], ws, top_p=p[:n])
         assert tokens.tolist() == want[:n] + [-9] * (9 - n)
+
+
+@pytest.mark.parametrize("fmt,requests", [("16", 6), ("fp8", 1), ("fp4", 9)])
+def test_example_of_a_batch(fmt, requests):
+    """Requests that begin, share, end and begin again."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "batch_step.py")
+    spec = importlib.util.spec_from_file_location("batch_step", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    worst, drawn, blocks = mod.main(layers=2, requests=requests, prompt=150, steps=7, fmt=fmt, say=lambda *a: None)
+    # results are rounded once, to 8 bits; the parts of probabilities lose 2^-16 in numerator and sum, scores up to 30 and their plain form some hundred units of 2^-24
+    assert worst <= 2.0 ** -8 + 2.0 ** -12
+    assert len(drawn) >= 7 and 150 // 16 < blocks <= requests * ((150 + 60 + 7) // 16 + 2)
