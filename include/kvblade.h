@@ -733,10 +733,12 @@ typedef struct kv_scores {
 /*
  * kv_group_attn -- attention of new tokens over one layer of a cache, as kv_tree_attn, for sequences that may share prefixes (groups, nullable) and scores that may be capped,
  * biased or bounded (scores, nullable); without a mask a sequence may have any number of new tokens (a prompt, or a chunk of one): a chain.
- * The K and V of a group's prefix are read once for all of its sequences' query rows, those of a sequence's own tokens once for it; workgroups whose rows see none of their tokens leave out
- * what they would read.  args, types, layouts, formats and limits are kv_tree_attn's otherwise: head_dim 64, 128 or 256; with a mask at most KV_TREE_MAX new tokens per sequence.
- * A row that sees nothing yields zeros.  workspace: at least kv_group_attn_workspace() bytes lets the library split as it likes; with less it splits less.
- * Two calls that overlap in time need a workspace each.
+ * The K and V of a group's prefix are read once for all of its sequences' query rows, or by each sequence for itself where it has many; those of a sequence's own tokens once for it; workgroups
+ * whose rows see none of their tokens leave out what they would read.  args, types, layouts, formats and limits are kv_tree_attn's otherwise: head_dim 64, 128 or 256; with a mask at most KV_TREE_MAX
+ * new tokens per sequence.  At most 64 groups (KV_EINVAL).  A row that sees nothing yields zeros.
+ * A cap of up to 64 with 16-bit results is off by cap * 2^-21 at most, others by 6 units of 2^-24 of the score.
+ * workspace: at least kv_group_attn_workspace() bytes lets the library split as it likes; with less it splits less; groups need room for two partial results of every query row at least,
+ * (head_dim + 2) * 8 bytes each (KV_ENOSPC).  Two calls that overlap in time need a workspace each.
  */
 int kv_group_attn(const kv_plan_t *plan, const kv_view_t *view, const kv_blocks_t *blocks, int layer, const kv_tree_args_t *args, const kv_groups_t *groups,
                   const kv_scores_t *scores, void *workspace, size_t ws_bytes, void *hip_stream);

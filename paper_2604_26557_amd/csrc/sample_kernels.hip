@@ -13,7 +13,7 @@
 //   min_p alone: what is above it is kept.
 //   What these have no room for, and top_k past 256 with top_p: histograms over the whole row, of its keys in the end, in as many rounds as they need.
 // What bounds it: some 30 instructions, most of them in double precision, for every weight where the sum of all is needed, otherwise a pass' latencies.  So few rows of many tokens are shared by several
-// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 46 us, 75 with a workgroup each.  One row
+// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 44 us, 75 with a workgroup each.  One row
 // of 32000 in 32 bits with top_k and top_p takes 16 us: a workgroup's three passes, and what its threads tell each other, one after the other.
 #include <hip/hip_runtime.h>
 
@@ -265,7 +265,7 @@ struct Row {
         });
         return t;
     }
-    // Every thread's part of a sample, a load of each of up to 1024, and how many logits that is in all: about the sum of the weights.
+    // Every thread's part of a sample, a load of each of up to 1024, eights of which are a cache line, and how many logits that is in all: about the sum of the weights.
     __device__ __forceinline__ int sample_size() const { return min((V - before_loads) / E, kThreads) * E; }
     __device__ __forceinline__ float sampled(int i) const
     {
@@ -273,7 +273,7 @@ struct Row {
         float x = 0.f;
         if ((unsigned)i < vectors) {
             float l[E];
-            unpack<DTYPE>(((const uint4 *)(at + (long long)before_loads * (16 / E)))[vectors > kThreads ? (unsigned)i * vectors / kThreads : i], l);
+            unpack<DTYPE>(((const uint4 *)(at + (long long)before_loads * (16 / E)))[vectors > kThreads ? (unsigned)(i / 8) * vectors / (kThreads / 8) + i % 8 : i], l);
 #pragma unroll
             for (int e = 0; e < E; ++e) x += __expf((l[e] - top) / T);
         }

@@ -23,6 +23,15 @@
 //   (D = 128; 8-bit rows most: 48 registers): 91 in the loop in which 16-bit results take 76.
 //   Four wavefronts, merged by halves: what one gives another goes through LDS twice (half, then a quarter of the sums), and two workgroups share a compute unit: one
 //   merges while the other reads.
+//
+// kv_group_attn's kernels are the same (GROUP), in translation units of their own, so that kv_tree_attn's keep their registers.  What a row sees is a range of tokens, its mask or chain and a second bound, which
+// the lane with the row's number holds; steps that all rows see in whole are not masked (a prompt of 4096 x 8 heads x 4 x 128 with a cap: 301 -> 248 us).  Splits share out what the rows of a workgroup see, not
+// what there is, and a chain's last row blocks, which see the most, begin first.  Scores are capped or biased in kernels of their own again (SHAPED: as a run-time choice the others spilled):
+//   a cap takes a rational function for tanh where results are of 32 bits or the cap passes 64, and a sigmoid, an exponential and a reciprocal, otherwise: the prompt takes 215 us without a cap, 306 with the one,
+//   247 with the other (which also spares the running maximum: no score passes the cap);
+//   a bias by distance counts from the farthest position of the rows, a multiplication and an addition a score, and steps go from the nearest tokens to the farthest: 256 us.
+// What bounds them, us per call: HBM, where rows are few (32 requests behind 8K, 172 MB: 42, the second launch of 5 included = 4.1 TB/s); the vector ALU beside the matrix cores, where they are many (the prompt,
+// 137 GFLOP in 215 = 640 TFLOP/s, with the cap 555: its probabilities enter in two parts, which is half as many products again, and matrix cores are busy 37 %).
 #pragma once
 
 #include <hip/hip_runtime.h>
