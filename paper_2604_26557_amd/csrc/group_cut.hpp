@@ -87,12 +87,30 @@ inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, boo
     const int room = (int)std::max<uint64_t>(least_ns, std::min<uint64_t>(fit, kMaxTreeSplits));
     const int most = n_splits > 0 ? room : std::min(room, std::max(least_ns, tree_most_splits(s, n_tok)));
     const double row = s.H * 2.0 * s.D * s.bits / 8e6, part = 2.0 * s.H * s.G * s.D * 4 / 1e6;
+    // Of one kind: its workgroups, what they take in us together and the longest of them, rows that K and V are read for again, and partial results.
+    struct Part {
+        double groups = 0, work = 0, longest = 0, again = 0, parts = 0;
+    };
+    auto part_of = [&](const GroupWork &w, int nb, int tokens) {
+        Part x;
+        if (w.units == 0) return x;
+        const int rows16 = 1 << nb;
+        const double step = (1.039 + 0.16 * rows16 * s.D / 128 * (s.D == 256 ? 2.837 : 1) + (s.bits < 16 ? 0.045 : 0) + (shaped ? 0.144 * rows16 : 0)) / 128, start = 3.0 + 1.55 * rows16;
+        // about as many splits as there are: half a one more of each unit than its tokens fill
+        const double splits = w.longest <= tokens ? w.blocks[nb] : std::max(w.blocks[nb], w.over[nb] / tokens + 0.5 * w.blocks[nb]);
+        x.longest = start + std::min(tokens, w.longest) * (bounded ? 0.5 : 1) * step;
+        x.groups = splits * s.H;
+        x.work = (splits * start + w.seen[nb] * step) * s.H;
+        x.again = w.seen[nb] - w.context;
+        x.parts = w.longest <= tokens ? w.tokens : std::max(w.tokens, w.parts / tokens + 0.5 * w.tokens);
+        return x;
+    };
     GroupCut best{};
     double least = 1e30;
-    auto consider = [&](int st, int pt) {
+    const int most_nb = s.D == 256 ? 1 : 2;   // of 0, 1, 2
+    auto consider = [&](int st, int pt, const Part (&of_own_rows)[3], const Part (&of_prefix_rows)[3]) {
         const int of_prefix = splits_of(prefix.longest, pt), of_own = splits_of(own.longest, st), ns = of_prefix + of_own;
         if (ns > most) return;
-        const int most_nb = s.D == 256 ? 1 : 2;   // of 0, 1, 2
         for (int k = 0; k < 4; ++k) {   // 1, 2, 4 row groups of both kinds; the most for prefixes alone
             const int of = k == 3 ? 0 : k, of_p = k == 3 ? most_nb : k;
             if (of > most_nb || (k == 3 && prefix.units == 0)) continue;
@@ -100,24 +118,16 @@ inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, boo
             // workgroups that a compute unit holds, by their LDS
             const bool one_each = s.D == 256 && (s.bits == 16 || (s.bits == 8 && of_p == 1));
             const double slots = one_each ? s.cus : 2 * s.cus, slower = one_each ? 1 : 1.256;
-            double work = 0, groups = 0, longest = 0, again = 0, parts = 0, rounds = 0;
-            auto kind = [&](const GroupWork &w, int nb, int tokens, bool ahead) {
-                if (w.units == 0) return;
-                const int rows16 = 1 << nb;
-                const double step = (1.039 + 0.16 * rows16 * s.D / 128 * (s.D == 256 ? 2.837 : 1) + (s.bits < 16 ? 0.045 : 0) + (shaped ? 0.144 * rows16 : 0)) / 128, start = 3.0 + 1.55 * rows16;
-                // about as many splits as there are: half a one more of each unit than its tokens fill
-                const double splits = w.longest <= tokens ? w.blocks[nb] : std::max(w.blocks[nb], w.over[nb] / tokens + 0.5 * w.blocks[nb]);
-                const double one = start + std::min(tokens, w.longest) * (bounded ? 0.5 : 1) * step, r = splits * s.H / slots;
-                groups += splits * s.H;
-                work += (splits * start + w.seen[nb] * step) * s.H;
-                longest = std::max(longest, one);
-                again += w.seen[nb] - w.context;
-                parts += w.longest <= tokens ? w.tokens : std::max(w.tokens, w.parts / tokens + 0.5 * w.tokens);
-                // prefixes go first, and others fill what they leave; one kind alone, of unequal lengths, is over a little earlier
-                if (ahead || prefix.units == 0) rounds = std::max(rounds, (r < 4 ? std::ceil(r - 0.02) : r + 0.5) * one * slower * (ahead ? 1 : 0.8));
+            const Part &o = of_own_rows[of], &f = of_prefix_rows[of_p];
+            const double groups = o.groups + f.groups, work = o.work + f.work, longest = std::max(o.longest, f.longest), again = o.again + f.again, parts = o.parts + f.parts;
+            // prefixes go first, and others fill what they leave; one kind alone, of unequal lengths, is over a little earlier
+            double rounds = 0;
+            auto in_rounds = [&](const Part &x, double by) {
+                const double r = x.groups / slots;
+                rounds = std::max(rounds, (r < 4 ? std::ceil(r - 0.02) : r + 0.5) * x.longest * slower * by);
             };
-            kind(own, of, st, false);
-            kind(prefix, of_p, pt, true);
+            if (prefix.units > 0) in_rounds(f, 1);
+            else in_rounds(o, 0.8);
             const double memory = (own.context + prefix.context) * row / 10.3 + again * row / 15.8 + 0.345 * longest;
             const double us = (groups <= s.cus ? std::max(longest, memory) : std::max({work * slower / slots + 0.355 * longest, rounds, memory})) +
                               (ns > 1 ? 6.1 + parts * part / 4.37 + 0.047 * ns : 0);
@@ -127,21 +137,36 @@ inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, boo
             }
         }
     };
+    auto parts_of = [&](const GroupWork &w, int tokens, Part (&to)[3]) {
+        for (int nb = 0; nb <= most_nb; ++nb) to[nb] = part_of(w, nb, tokens);
+    };
     const int span = std::max(own.longest, prefix.longest);
     auto even = [&](int ns) { return (int)((((long long)span + ns - 1) / ns + 31) / 32 * 32); };
     if (n_splits > 0) {
-        for (int ns = n_splits; best.nb == 0 && ns >= 1; --ns) consider(even(ns), even(ns));
+        for (int ns = n_splits; best.nb == 0 && ns >= 1; --ns) {
+            Part o[3], f[3];
+            parts_of(own, even(ns), o);
+            parts_of(prefix, even(ns), f);
+            consider(even(ns), even(ns), o, f);
+        }
         return best;
     }
     // lengths of which those past twice a kind's longest say nothing new; the last is the whole
     static constexpr int kLengths[] = {128, 256, 384, 512, 768, 1024, 1536, 2048, 2816, 4096, 8192, 16384};
-    for (int i = 0; i <= 12; ++i) {
-        const bool whole = i == 12 || kLengths[i] >= own.longest;
-        for (int j = 0; j <= 12; ++j) {
-            const bool whole_prefix = j == 12 || kLengths[j] >= prefix.longest;
-            consider(whole ? even(1) : kLengths[i], whole_prefix ? even(1) : kLengths[j]);
-            if (whole_prefix) break;
-        }
+    constexpr int kN = sizeof(kLengths) / sizeof(*kLengths);
+    Part of_prefix_rows[kN + 1][3];
+    int n_prefix = 0;
+    for (;; ++n_prefix) {
+        const bool whole = n_prefix == kN || kLengths[n_prefix] >= prefix.longest;
+        parts_of(prefix, whole ? even(1) : kLengths[n_prefix], of_prefix_rows[n_prefix]);
+        if (whole) break;
+    }
+    for (int i = 0; i <= kN; ++i) {
+        const bool whole = i == kN || kLengths[i] >= own.longest;
+        const int st = whole ? even(1) : kLengths[i];
+        Part of_own_rows[3];
+        parts_of(own, st, of_own_rows);
+        for (int j = 0; j <= n_prefix; ++j) consider(st, j == n_prefix ? even(1) : kLengths[j], of_own_rows, of_prefix_rows[j]);
         if (whole) break;
     }
     return best;
