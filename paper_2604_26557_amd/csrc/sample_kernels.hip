@@ -963,7 +963,7 @@ extern "C" int kv_sample(const kv_sample_args_t *a, void *workspace, size_t ws_b
     if (a->n_rows < 0 || a->n_vocab < 1 || a->stride < 0) return KV_EINVAL;
     if (ws_bytes < kv_sample_workspace(a->n_rows, a->n_vocab)) return KV_ENOSPC;
     if (a->n_rows == 0) return KV_OK;
-    if (a->n_vocab > 1 << 24) return KV_ERANGE;
+    if (a->n_vocab > 1 << 24 || (uint64_t)a->n_rows * kThreads >= 1ull << 32) return KV_ERANGE;   // threads of a launch
     if (!a->logits || !a->u || !a->tokens || ((uintptr_t)a->logits & (a->dtype == KV_F32 ? 3 : 1))) return KV_EINVAL;
     SampleParams p{};
     p.a = *a;

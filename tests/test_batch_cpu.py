@@ -169,6 +169,7 @@ def test_sample_sizes():
     call = lambda **kw: kv.lib().kv_sample(C.byref(kv.kv_sample_args_t(**{**a, **kw})), P, kw.pop("ws_bytes", 1 << 30), None)  # noqa: E731
     assert call() == kv.KV_OK   # no rows: nothing is launched
     assert call(n_rows=2, n_vocab=(1 << 24) + 1) == kv.KV_ERANGE
+    assert call(n_rows=1 << 22) == kv.KV_ERANGE   # threads of a launch
     assert kv.lib().kv_sample(None, P, 1 << 20, None) == kv.KV_EINVAL
     assert kv.lib().kv_sample(C.byref(kv.kv_sample_args_t(**{**a, "n_rows": 2})), P, kv.kv_sample_workspace(2, 100) - 1, None) == kv.KV_ENOSPC
     assert kv.kv_sample_workspace(1, 1000) >= 16 and kv.kv_sample_workspace(-1, 10) == 0 and kv.kv_sample_workspace(1, -1) == 0
