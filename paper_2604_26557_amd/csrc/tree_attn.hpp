@@ -513,7 +513,8 @@ __device__ __forceinline__ bool find_unit(const GroupParams &p, int lane, Unit &
         unsigned units = 0, of_unit = 0;
         if (n > 0) {
             const int span = is_group ? l : l + n - (p.joined ? 0 : from & ~31);
-            of_unit = quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1;
+            // never more than a row has partial results, whatever the lengths are by now: splits share out what there is
+            of_unit = min(quotient((unsigned)(span - 1), (unsigned)st, is_group ? p.by_prefix : p.by_split) + 1, (unsigned)(is_group ? p.prefix_ns : p.ns - p.prefix_ns));
             units = of_unit * (unsigned)p.H;
         }
         const unsigned blocks = (unsigned)(((long long)n * p.G + rows - 1) / rows), all = units * blocks;

@@ -143,7 +143,7 @@ class Batch:
                     if self.slopes is not None:
                         dist = np.abs(self.positions[at + i] - key_pos[idx])
                         x = x - self.slopes[h] * dist
-                        e = e + 8 * self.slopes[h] * (dist + 64)
+                        e = e + 8 * abs(self.slopes[h]) * (dist + 64)
                     e = e + 4 * np.abs(x) + 4 * np.abs(x).min() + 8
                     with np.errstate(all="ignore"):
                         p = np.exp(x - x.max())

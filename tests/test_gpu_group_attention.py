@@ -447,3 +447,32 @@ def test_two_calls_at_once_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for w, run in zip(want, runs):
         assert torch.equal(run[-1], w)
+
+
+def test_slopes_below_zero():
+    """Farther tokens weigh more: references move at every step, and where a cap bounds the scores their biases pass it."""
+    for cap in (0.0, 4.0):
+        b = Batch([500, 30], [3, 70], 2, 3, 64, torch.bfloat16, seed=1, slopes=[-0.5, -0.01, 0.0, 0.02, -2.0, -1.0e-3], cap=cap, first=[0, 2], prefix=[30])
+        for n_splits in (0, 1, 3):
+            b.check(b.attend(n_splits=n_splits))
+        b.check(b.attend(kv.KV_OUT_SAME), False)
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+def test_lengths_that_change_behind_the_hosts(grouped):
+    """Lengths on the device that sum up to the host's: what is longer than the host knew has no more partial results than there is room for, and all of its tokens."""
+    kw = dict(first=[2, 4], prefix=[700]) if grouped else {}
+    lens = [900, 33, 760, 701] if grouped else [900, 33]
+    for news in ([1] * len(lens), [40] * len(lens)):
+        b = Batch(lens, news, 2, 4, 64, torch.float16, seed=3, **kw)
+        want = b.attend(n_splits=1)
+        b.check(want)
+        host = b.c.view.struct.seq_lens_host
+        host[0], host[1] = 33, 900
+        for n_splits in (1, 2, 5):
+            size = kv.kv_group_attn_workspace(b.c.plan, sum(news), 900)
+            ws = torch.full((size + 4096,), 171, dtype=torch.uint8, device="cuda")
+            got = b.attend(n_splits=n_splits, ws=ws[:size])
+            assert (ws[size:] == 171).all()
+            b.check(got)
+        host[0], host[1] = 900, 33
