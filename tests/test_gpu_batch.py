@@ -472,3 +472,46 @@ def test_example_of_a_batch(fmt, requests):
     # results are rounded once, to 8 bits; the parts of probabilities lose 2^-16 in numerator and sum, scores up to 30 and their plain form some hundred units of 2^-24
     assert worst <= 2.0 ** -8 + 2.0 ** -12
     assert len(drawn) >= 7 and 150 // 16 < blocks <= requests * ((150 + 60 + 7) // 16 + 2)
+
+
+@pytest.mark.parametrize("kw", [dict(k=50, p=0.9), dict(p=0.9), dict(k=900), dict(m=0.02), dict()])
+def test_sample_two_calls_at_once(kw):
+    """On two streams with workspaces of their own, again and again, and as a graph of both: the tokens of each alone."""
+    V, runs = 70000, []
+    for seed in (1, 2):
+        x = (torch.randn((9, V), generator=torch.Generator().manual_seed(seed)) * 2).to(torch.bfloat16).cuda()
+        dev = {n: torch.full((9,), v, dtype=torch.int32 if n == "k" else torch.float32, device="cuda") for n, v in kw.items()}
+        args = dict(top_k=dev.get("k"), top_p=dev.get("p"), min_p=dev.get("m"))
+        u = torch.rand(9, generator=torch.Generator().manual_seed(seed)).cuda()
+        ws = torch.empty(kv.kv_sample_workspace(9, V), dtype=torch.uint8, device="cuda").fill_(255)
+        runs.append((x, u, i32([-9] * 9), ws, args, torch.cuda.Stream(), sample(x, u.tolist(), **kw)[0]))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, u, tokens, ws, args, stream, _w in runs:
+            kv.kv_sample(x, u, tokens, ws, stream=stream, **args)
+    torch.cuda.synchronize()
+    assert all(tokens.tolist() == want for _, _, tokens, _, _, _, want in runs)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for x, u, tokens, ws, args, _s, _w in runs:
+            kv.kv_sample(x, u, tokens, ws, **args)
+    for _ in range(3):
+        for run in runs:
+            run[2].fill_(-9)
+            run[3].fill_(85)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(tokens.tolist() == want for _, _, tokens, _, _, _, want in runs)
+
+
+@pytest.mark.parametrize("V", [700, 32768, 32770, 65537])
+@pytest.mark.parametrize("start", [0, 1, 7])
+def test_sample_few_of_rows_that_fit_registers(V, start):
+    """Up to, at and past what a workgroup's threads hold; lists of one, of a wavefront's lanes and more; the largest at both ends."""
+    for dtype in (torch.float32, torch.float16):
+        x = (torch.randn((4, V + 8), generator=torch.Generator().manual_seed(V)) * 2).to(dtype)
+        x[0, start] = x[0, start + V - 1] = 20
+        x[1] = torch.round(x[1].float()).to(dtype)
+        x = x.cuda()[:, start:start + V]
+        for kw in (dict(k=1), dict(k=2, t=0.5), dict(k=40, p=0.8), dict(k=64), dict(k=65, p=0.99), dict(k=256, m=0.1), dict(k=60, p=0.5, m=0.5)):
+            check_sample(x, [0.0, 0.3, 0.7, 0.999], **kw)
