@@ -476,3 +476,18 @@ def test_lengths_that_change_behind_the_hosts(grouped):
             assert (ws[size:] == 171).all()
             b.check(got)
         host[0], host[1] = 900, 33
+
+
+@pytest.mark.parametrize("fmt", ["16", "fp8"])
+def test_trees_with_bounds_and_groups_of_nobody(fmt):
+    """A mask, a window, and tokens seen in any case at once; groups without sequences, and of sequences without new tokens."""
+    rng = np.random.default_rng(5)
+    lens, news = [140, 100, 100, 60, 300, 90], [5, 0, 33, 1, 70, 0]
+    trees = [random_parents(rng, n) if n else [] for n in news]
+    n = sum(news)
+    at = [lens[b] + i for b, t in enumerate(news) for i in range(t)]
+    b = Batch(lens, news, 2, 3, 64, torch.bfloat16, fmt, "paged", seed=6, first=[0, 0, 1, 3, 3, 5], prefix=[50, 90, 100, 7, 60], trees=trees, cap=12.0,
+              sees_from=[max(0, j - int(w)) for j, w in zip(at, rng.integers(1, 200, n))], sees_to=[int(x) for x in rng.integers(0, 400, n)])
+    for n_splits in (0, 1, 4):
+        b.check(b.attend(n_splits=n_splits))
+    b.check(b.attend(kv.KV_OUT_SAME), False)
