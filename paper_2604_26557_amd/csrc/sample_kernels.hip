@@ -9,7 +9,8 @@
 //   More of them, without top_p: a histogram of their number by distance from the maximum says which bin the k-th is in; what is above is kept, the bin is a list, which is ranked.  2 rows of 106775
 //     in 32 bits, the largest 1000: 62 us; 115 by the rounds below.
 //   top_p alone: the sum of all, and a histogram of weights by distance from the maximum.  Tokens below (1 - p) / n_vocab of the sum are not needed to get from p to the whole: a sample says about where
-//     that is, and only what is above goes into the histogram (a third of the tokens in a usual case).  Then as before.
+//     that is, and only what is above goes into the histogram (a third of the tokens in a usual case).  Then as before; or, where no more than 256 tokens can have what there is up to the border, as with
+//     few: a row of 32000 of which a dozen have nine tenths of the weight 19.5 -> 17.0 us (with room for 1024 rows of 74 were ranked for longer than it saved: 64 of 128256 43 -> 48).
 //   min_p alone: what is above it is kept.
 //   What these have no room for, and top_k past 256 with top_p: histograms over the whole row, of its keys in the end, in as many rounds as they need.
 // What bounds it: some 30 instructions, most of them in double precision, for every weight where the sum of all is needed, otherwise a pass' latencies.  So few rows of many tokens are shared by several
@@ -45,7 +46,7 @@ struct RowState {
     float some_logit[kRanked];
     u64 in_bin;                            // of the target, what its bin has to give
     float per;                             // bins per unit of a logit, of top_p rows
-    unsigned n_some, fits, unused;         // fits: the above says it all, if n_some does not pass kRanked
+    unsigned n_some, fits, unused;         // fits: the above says it all, if n_some does not pass kRanked; 2: the list alone
 };
 // And each slice of a top_p row.
 struct SliceState {
@@ -400,7 +401,7 @@ struct Shared {
     unsigned wave_u32[kWaves];
     float wave_f32[kWaves];
     // what one thread tells the others
-    u64 told_weight, told_all;
+    u64 told_weight, told_all, told_above;
     unsigned told_bin;
 };
 
@@ -507,6 +508,20 @@ struct Group {
         });
         __syncthreads();
     }
+    // Where top_p ends, in the bin to which s.weight[.. bin] leads: all from `sure` on are kept, and of those from `from` on some, *in_bin of their weight. Or, as often where a few tokens have most of the
+    // weight, no more than 256 tokens can have what there is from `from` on, none of which weighs less: then true, and *in_bin is of all of them.
+    template <int DTYPE>
+    __device__ __forceinline__ bool cut_at(const Row<DTYPE> &row, float per, unsigned bin, u64 *in_bin, float *sure, float *from)
+    {
+        const u64 above = s.told_above, here = s.weight[bin];
+        *from = fmaxf(least_of(row, per, (float)bin + 1.f), row.least);
+        if (above + here <= 256 * row.units_of(*from)) {
+            *in_bin += above;
+            return true;
+        }
+        if (bin > 0) *sure = least_of(row, per, (float)bin);
+        return false;
+    }
     // The list of those from `from` on alone.
     template <int DTYPE>
     __device__ __forceinline__ void list_from(const Row<DTYPE> &row, int tid, int threads, float from)
@@ -541,7 +556,8 @@ struct Group {
         if (before < target && target <= before + w0 + w1) {
             const bool second = target > before + w0;
             s.told_bin = 2 * tid + second;
-            s.told_weight = target - before - (second ? w0 : 0);
+            s.told_above = before + (second ? w0 : 0);
+            s.told_weight = target - s.told_above;
         }
         __syncthreads();
         *in_bin = s.told_weight;
@@ -648,6 +664,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_keep_kernel(SampleParams p
     row.set_top(top, s.exps);
     s.tile_weight[tid] = 0;
     float sure = INFINITY, from;
+    bool whole = row.few();   // a list has all that may be kept
     if (row.few()) {
         from = g.reached_by(row, mine);
         if (!(from == from)) return;
@@ -667,15 +684,14 @@ __global__ void __launch_bounds__(kThreads) kv_sample_keep_kernel(SampleParams p
         u64 in_bin;
         const unsigned bin = g.bin_of_target(row.target_of(sum), &in_bin);
         if (bin >= (unsigned)kBins) return;
-        if (bin > 0) sure = g.least_of(row, per, (float)bin);
-        from = g.least_of(row, per, (float)bin + 1.f);
+        whole = g.cut_at(row, per, bin, &in_bin, &sure, &from);
         if (blockIdx.x == 0 && tid == 0) state.in_bin = in_bin;
     } else {
         sure = from = row.least;
     }
-    if (blockIdx.x == 0 && tid == 0) state.fits = 1;
+    if (blockIdx.x == 0 && tid == 0) state.fits = whole ? 2 : 1;
     __syncthreads();
-    if (row.few()) g.list_from(row, blockIdx.x * kThreads + tid, threads, from);
+    if (whole) g.list_from(row, blockIdx.x * kThreads + tid, threads, from);
     else g.keep(row, blockIdx.x * kThreads + tid, threads, sure, from, 0);
     const unsigned n = s.n_some;
     if (tid == 0) s.told_bin = n ? atomicAdd(&state.n_some, n) : 0;
@@ -786,11 +802,12 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
     }
 
     // What is kept for sure, in s.tile_weight, and what may be: s.some
-    bool fits = false;
+    bool fits = false, whole = row.few();   // whole: s.some alone has all of it
     u64 in_bin = 0;
     if (state && !row.by_counts()) {
         fits = state->fits != 0 && state->n_some <= (unsigned)kRanked;
         if (fits) {
+            whole = whole || state->fits == 2;
             s.tile_weight[tid] = state->tile_weight[tid];
             if (tid < (int)state->n_some) s.some[tid] = state->some[tid], s.some_logit[tid] = state->some_logit[tid];
             if (tid == 0) s.n_some = state->n_some;
@@ -810,10 +827,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             if (per != 0.f) {
                 const u64 sum = g.sum_of(row.sum_and_bins(tid, kThreads, per, s.weight));
                 const unsigned bin = g.bin_of_target(row.target_of(sum), &in_bin);
-                if (bin < (unsigned)kBins) {
-                    if (bin > 0) sure = g.least_of(row, per, (float)bin);
-                    from = g.least_of(row, per, (float)bin + 1.f);
-                }
+                if (bin < (unsigned)kBins) whole = g.cut_at(row, per, bin, &in_bin, &sure, &from);
             }
         } else if (row.by_counts()) {
             s.weight[tid] = s.weight[kThreads + tid] = 0;
@@ -834,7 +848,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
         if (from == from) {
             __syncthreads();
             if (is_held) g.list_from(held, from);
-            else if (row.few()) g.list_from(row, tid, kThreads, from);
+            else if (whole) g.list_from(row, tid, kThreads, from);
             else g.keep(row, tid, kThreads, sure, from, 0);
             fits = s.n_some <= (unsigned)kRanked;
         }
@@ -842,7 +856,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
     if (fits) {
         __syncthreads();
         const int n = (int)s.n_some;
-        if (row.few() && n <= 64) {
+        if (whole && n <= 64) {
             // A wavefront has them all, a lane each, and needs nobody else (the largest 50 of 32000 with top_p: 15.6 -> 12.5 us, and 11.6 with the row held).
             if (wave != 0) return;
             const int i = lane < n ? (int)s.some[lane] : INT_MAX;
@@ -865,7 +879,7 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             sums(own, weight, [&](bool is, u64 w) { ahead += is, before += is ? w : 0; });
             bool in = lane < n && ahead < k;
             if (row.cut_p) {   // all lanes take part in a sum
-                const u64 target = row.target_of(wave_sum(in ? weight : 0));
+                const u64 sum = wave_sum(in ? weight : 0), target = row.few() ? row.target_of(sum) : in_bin;
                 in = in && before < target;
             }
             const u64 kept = in && row.weighs(x) ? weight : 0, all = wave_sum(kept);
