@@ -662,7 +662,7 @@ size_t kv_tree_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
 
 /* ------------------------------------------------------------------------------------------ */
 /* A serving step of a batch of requests: its tables, attention over shared prefixes and of   */
-/* capped, biased or bounded scores, sampling (stream-ordered, no blocking, no allocation)    */
+/* capped, biased or bounded scores, sampling (stream-ordered, no blocking, no device memory) */
 /* ------------------------------------------------------------------------------------------ */
 
 /*

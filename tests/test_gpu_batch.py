@@ -515,3 +515,16 @@ def test_sample_few_of_rows_that_fit_registers(V, start):
         x = x.cuda()[:, start:start + V]
         for kw in (dict(k=1), dict(k=2, t=0.5), dict(k=40, p=0.8), dict(k=64), dict(k=65, p=0.99), dict(k=256, m=0.1), dict(k=60, p=0.5, m=0.5)):
             check_sample(x, [0.0, 0.3, 0.7, 0.999], **kw)
+
+
+@pytest.mark.parametrize("V", [900, 33000, 70000])
+@pytest.mark.parametrize("spread", [5.0, 12.0, 40.0])
+def test_sample_of_which_few_have_most(V, spread):
+    """top_p alone, and with min_p, where lists of one, some and hundreds of tokens hold all that is kept."""
+    x = torch.randn((6, V), generator=torch.Generator().manual_seed(int(spread))) * spread
+    x[1] = torch.round(x[1] / 4) * 4          # the border in ties
+    x[2, 100:160] = x[2].max()                # sixty of the largest
+    x[3, :300] = x[3].max()                   # and more than a list is taken for
+    x = x.to(torch.float16 if spread < 40 else torch.float32).cuda()
+    for kw in (dict(p=0.5), dict(p=0.9, t=0.7), dict(p=0.999), dict(p=0.95, m=0.2), dict(p=0.9, m=1.0), dict(p=0.0)):
+        check_sample(x, [0.1, 0.999, 0.4, 0.7, 0.5, 0.01], **kw)
