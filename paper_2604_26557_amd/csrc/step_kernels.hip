@@ -161,12 +161,13 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
     __syncthreads();
 
     if (maps) {
-        const int t0 = ((int)blockIdx.x - p.table_groups) * kTokens, t1 = min(a.n_tok, t0 + kTokens);
-        for (int t = t0 + tid; t < t1; t += kThreads) {
-            const bool there = (unsigned)t < first[B];
-            const int b = there ? segment_of(first, B, (unsigned)t) : 0;
+        // rows up to 2^31 - 1: the end of the last workgroup's is past 31 bits
+        const unsigned t0 = (blockIdx.x - (unsigned)p.table_groups) * kTokens, t1 = min((unsigned)a.n_tok, t0 + kTokens);
+        for (unsigned t = t0 + tid; t < t1; t += kThreads) {
+            const bool there = t < first[B];
+            const int b = there ? segment_of(first, B, t) : 0;
             a.tok_seq[t] = there ? b : -1;
-            a.tok_slot[t] = there ? (int)(max(a.seq_lens[b], 0) + ((unsigned)t - first[b])) : -1;
+            a.tok_slot[t] = there ? (int)(max(a.seq_lens[b], 0) + (t - first[b])) : -1;
         }
         return;
     }
