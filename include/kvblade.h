@@ -675,6 +675,7 @@ size_t kv_tree_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
  *   stay with their sequence.
  * leader[b] outside [0, batch) or b itself: none, and shared[b] counts as 0.  Shared entries belong to the leader, which has to end after those that follow it.
  * free_ids[0 .. n_free) is a stack: what ends is pushed in the order of sequences and entries, then blocks are taken from its top in that order.
+ * What would lie past its n_pool entries then is lost: a program that counts on every block makes room for all of them.
  * If there are too few of them, or need exceeds max_blocks somewhere, nothing is handed out (requests that ended are released all the same) and held_out = held for the others:
  * status[0] = blocks missing, status[1] = sequences that do not fit their row, both 0 otherwise.
  * tok_first, tok_seq, tok_slot: the step's new tokens in order of sequences, token i of sequence b at row tok_first[b] + i, place seq_lens[b] + i (kv_cache_write's maps, and positions

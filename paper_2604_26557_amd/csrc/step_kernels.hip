@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p
     if (blockIdx.x == 0) {
         for (int b = tid; b <= B; b += kThreads) a.tok_first[b] = (int)first[b];
         if (tid == 0) {
-            a.n_free_out[0] = (int)max(0ll, (long long)min(top, (unsigned long long)a.n_pool) - (long long)(fine ? all[1] : 0));
+            a.n_free_out[0] = (int)min(top - (fine ? all[1] : 0), (unsigned long long)a.n_pool);   // fine: all[1] <= top
             a.status[0] = all[1] > top ? (int)count(all[1] - top) : 0;
             a.status[1] = over;
         }

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from batchcase import ref_tables
 from paper_2604_26557_amd import binding as kv
 
 pytestmark = pytest.mark.gpu
@@ -25,3 +26,20 @@ def test_maps_of_as_many_rows_as_there_can_be(in_place):
     assert seq[n - 1003:].tolist() == [1] * 3 + [-1] * 1000 and slot[n - 1003:].tolist() == [n - 1013, n - 1012, n - 1011] + [-1] * 1000
     at = torch.arange(10, n - 1000, 4099, device="cuda")
     assert (seq[at] == 1).all() and torch.equal(slot[at].long(), at - 10)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("begin", [0, 16, 30, 64, 80, 96, 112])
+def test_a_stack_with_less_room_than_what_ends(in_place, begin):
+    """Four blocks are free and fill their array; three more end in the call, of which as many as begin are handed out. What is left past the array is lost, and nothing that lies in it."""
+    lens, news, held, rows = [40, 0], [-1, begin], [3, 0], [[11, 12, 13, -1, -1, -1, -1], [-1] * 7]
+    want_rows, want_held, stack, n_free, status, *_ = ref_tables(16, lens, news, held, [1, 2, 3, 4], 4, rows)
+    assert status == [0, 0]
+    free, n_dev, table, held_dev, status = i32([1, 2, 3, 4]), i32([4]), i32(rows), i32(held), i32([5, 5])
+    outs = dict(held_out=i32([5, 5]), n_free_out=i32([5]), block_table_out=torch.full_like(table, 5))
+    kv.kv_step_tables(kv.step_tables(16, i32(lens), i32(news), held_dev, free, n_dev, table, i32([5, 5, 5]), i32([]), i32([]), status, **({} if in_place else outs)))
+    got = (table, held_dev, n_dev) if in_place else (outs["block_table_out"], outs["held_out"], outs["n_free_out"])
+    assert status.tolist() == [0, 0] and got[0].tolist() == want_rows and got[1].tolist() == want_held
+    assert free.tolist() == stack[:4] and int(got[2]) == min(n_free, 4)
+    used = {i for r in want_rows for i in r if i >= 0}
+    assert not used & set(free.tolist()[:int(got[2])])
