@@ -43,3 +43,27 @@ def test_a_stack_with_less_room_than_what_ends(in_place, begin):
     assert free.tolist() == stack[:4] and int(got[2]) == min(n_free, 4)
     used = {i for r in want_rows for i in r if i >= 0}
     assert not used & set(free.tolist()[:int(got[2])])
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n_free", [0, 1, 3])
+@pytest.mark.parametrize("more", [-1, 0, 1])
+def test_the_last_free_block_and_one_more(in_place, n_free, more):
+    """Two requests end with 8 blocks; what the others want is one block less than there is, all of it, or one too many: then nobody gets any."""
+    lens, held = [40, 33, 64, 10], [3, 3, 5, 1]
+    rows = [r + [-1] * (16 - len(r)) for r in ([1, 2, 3], [4, 5, 6], [7, 8, 9, 10, 11], [12])]
+    # the fourth wants 2 blocks, the second what is left of 8 + n_free
+    want = 8 + n_free - 2 + more
+    news, free = [-1, 16 * (3 + want) - 33, -1, 38], [20 + i for i in range(n_free)] + [-1] * (16 - n_free)
+    after = ref_tables(16, lens, news, held, free, n_free, rows, n_tok=4)
+    assert after[4] == [max(0, more), 0]
+    free_dev, n_dev, table, held_dev, status = i32(free), i32([n_free]), i32(rows), i32(held), i32([5, 5])
+    seq, slot, first = i32([5] * 4), i32([5] * 4), i32([5] * 5)
+    outs = dict(held_out=i32([5] * 4), n_free_out=i32([5]), block_table_out=torch.full_like(table, 5))
+    kv.kv_step_tables(kv.step_tables(16, i32(lens), i32(news), held_dev, free_dev, n_dev, table, first, seq, slot, status, **({} if in_place else outs)))
+    got = (table, held_dev, n_dev) if in_place else (outs["block_table_out"], outs["held_out"], outs["n_free_out"])
+    assert (got[0].tolist(), got[1].tolist(), free_dev.tolist(), int(got[2]), status.tolist(), first.tolist(), seq.tolist(), slot.tolist()) == tuple(after)
+    if more > 0:
+        assert got[0][1].tolist() == rows[1] and got[1].tolist() == [0, 3, 0, 1] and int(got[2]) == 8 + n_free
+    else:
+        assert int(got[2]) == -more
