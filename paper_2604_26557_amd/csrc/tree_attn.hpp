@@ -1071,10 +1071,14 @@ __device__ __forceinline__ void tree_work(const typename std::conditional<GROUP,
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const int r = min(nb * 16 + here(n), n_rows - 1), pos = __shfl(row_pos, nb * 16 + here(n)), ahead = by_row ? 0 : pos - origin;
+                    const int r = min(nb * 16 + here(n), n_rows - 1), pos = __shfl(row_pos, nb * 16 + here(n)), behind = by_row ? 0 : origin - pos;
                     const float slope = slope_of(p, r);
+                    // A distance may be 2^31, and up to 1024 more with what the row is behind its origin: no signs, which a token that the row sees never has.
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[nb][j / 4][j % 4] = fmaf(slope, (float)(ahead - abs(pos - at[j])), s[nb][j / 4][j % 4]);
+                    for (int j = 0; j < 8; ++j) {
+                        const unsigned d = (unsigned)pos - (unsigned)at[j], off = (unsigned)max((int)d, (int)(0u - d));
+                        s[nb][j / 4][j % 4] = fmaf(-slope, (float)(off + (unsigned)behind), s[nb][j / 4][j % 4]);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
