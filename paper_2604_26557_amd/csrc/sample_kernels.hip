@@ -864,8 +864,13 @@ __global__ void __launch_bounds__(kThreads) kv_sample_kernel(SampleParams p)
             const u64 own = lane < n ? place_of(key_of(x), i) : 0, weight = lane < n ? row.units_of(x) : 0;
             // Sums over those that are before this one, in the order, then by index. Of the first k all that are ahead of one are of them too.
             auto sums = [&](u64 place, u64 w, auto counts) {
+                // what the lanes have read before is read, and what they write is there for all of them after: an order for the compiler, LDS keeps it by itself
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+                __builtin_amdgcn_wave_barrier();
                 s.ranked[lane] = place;
                 s.ranked_weight[lane] = w;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+                __builtin_amdgcn_wave_barrier();
                 for (int j0 = 0; j0 < n; j0 += 16) {
                     u64 at[16], of[16];
 #pragma unroll

@@ -4,6 +4,7 @@ import torch
 
 from batchcase import ref_tables
 from paper_2604_26557_amd import binding as kv
+from test_gpu_batch import check_sample
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +68,15 @@ def test_the_last_free_block_and_one_more(in_place, n_free, more):
         assert got[0][1].tolist() == rows[1] and got[1].tolist() == [0, 3, 0, 1] and int(got[2]) == 8 + n_free
     else:
         assert int(got[2]) == -more
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_samples_of_lists_of_every_length_of_a_wavefront(dtype):
+    """The k largest of equal, of few different and of different logits, k up to a lane more than there are, at once: a row for each."""
+    k = list(range(1, 66)) * 3
+    x = torch.randn((len(k), 333), generator=torch.Generator().manual_seed(3)) * 2
+    x[65:130] = torch.round(x[65:130])
+    x[130:] = 0.25
+    u = torch.rand(len(k), generator=torch.Generator().manual_seed(4)).tolist()
+    for kw in (dict(), dict(p=[0.7] * len(k)), dict(m=[0.1] * len(k), t=[0.6] * len(k))):
+        check_sample(x.to(dtype).cuda(), u, k=k, **kw)
