@@ -80,3 +80,28 @@ def test_samples_of_lists_of_every_length_of_a_wavefront(dtype):
     u = torch.rand(len(k), generator=torch.Generator().manual_seed(4)).tolist()
     for kw in (dict(), dict(p=[0.7] * len(k)), dict(m=[0.1] * len(k), t=[0.6] * len(k))):
         check_sample(x.to(dtype).cuda(), u, k=k, **kw)
+
+
+def test_samples_of_rows_that_each_ask_for_something_else():
+    """Of long rows that workgroups share: the largest, few of the largest, many, a border by weight, by both, by min_p, nothing, in one call."""
+    V, B = 70003, 40
+    x = (torch.randn((B, V), generator=torch.Generator().manual_seed(5)) * 2).to(torch.bfloat16).cuda()
+    x[9, 77] = float("nan")
+    x[17] = float("-inf")
+    kw = dict(t=[0.0, 1.0, 0.7, 1.3, 1.0, 0.9, 2.0, 1.0] * 5, k=[0, 40, 1000, 0, 300, 0, 0, 1] * 5, p=[1.0, 0.9, 1.0, 0.95, 0.8, 1.0, 1.0, 0.5] * 5, m=[0.0, 0.0, 0.01, 0.02, 0.0, 0.03, 0.0, 0.0] * 5)
+    check_sample(x, torch.rand(B, generator=torch.Generator().manual_seed(6)).tolist(), **kw)
+
+
+def test_samples_of_the_largest_vocabulary():
+    V = 1 << 24
+    x = (torch.randn((1, V), generator=torch.Generator().manual_seed(7)) * 2).to(torch.float16).cuda()
+    for kw in (dict(), dict(p=0.9), dict(k=50), dict(m=0.01), dict(t=0.0)):
+        check_sample(x, [0.83], **kw)
+
+
+def test_samples_of_as_many_rows_as_a_launch_may_have():
+    n = (1 << 22) - 1
+    x = torch.randn((n, 3), generator=torch.Generator().manual_seed(8)).cuda()
+    tokens, probs, t = torch.full((n,), -9, dtype=torch.int32, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    kv.kv_sample(x, t, tokens, torch.empty(16, dtype=torch.uint8, device="cuda"), temperature=t, probs=probs)
+    assert torch.equal(tokens.long(), x.argmax(1)) and (probs == 1).all()
