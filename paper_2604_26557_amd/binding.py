@@ -773,7 +773,8 @@ def kv_group_attn_workspace(plan: Plan, n_tok: int, max_len: int) -> int:
 def kv_group_attn(plan: Plan, view: View, blocks: Optional[Blocks], layer: int, tree: TreeBatch, q, out, out_dtype: int, n_splits: int, workspace,
                   groups: Optional[Groups] = None, scores: Optional[Scores] = None, scale: float = 0.0, stream=None) -> None:
     """kv_tree_attn for sequences that share prefixes (groups) and scores that are capped, biased or bounded (scores), and for prompts.  q, out: [n_tok, H_q, D], last dim
-    contiguous; q of the plan's dtype, out of that or fp32 (out_dtype)."""
+    contiguous; q of the plan's dtype, out of that or fp32 (out_dtype).  Chunks of prompts are better calls of their own than beside single tokens of long contexts.  Two calls that
+    overlap in time need a workspace each."""
     (n, hq, d), (qt, qh, qd), (ot, oh, od), shape = q.shape, q.stride(), out.stride(), plan.shape
     if qd != 1 or od != 1 or n < tree.n_tok or hq != shape[1] or d != shape[2] or q.dtype != shape[3] or out.shape != q.shape \
             or len(tree.first) != shape[4] or out.dtype != shape[5 if out_dtype == KV_OUT_F32 else 3]:
@@ -795,7 +796,8 @@ def kv_sample_workspace(n_rows: int, n_vocab: int) -> int:
 
 
 def kv_sample(logits, u, tokens, workspace, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, stream=None) -> None:
-    """logits: [rows, vocabulary] fp16, bf16 or fp32, last dim contiguous; temperature, top_p, min_p, u, probs: device float32 [rows]; top_k, tokens: device int32 [rows]."""
+    """logits: [rows, vocabulary] fp16, bf16 or fp32, last dim contiguous; temperature, top_p, min_p, u, probs: device float32 [rows]; top_k, tokens: device int32 [rows].
+    Two calls that overlap in time need a workspace each."""
     if not _logit_dtypes:
         import torch
         _logit_dtypes.update({torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float32: KV_F32})

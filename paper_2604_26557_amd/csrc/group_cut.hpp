@@ -73,6 +73,9 @@ struct GroupWork {
 // what the bytes of K and V take, read once and again by further row blocks; where there are splits of the second launch and partial results. Its numbers were fitted to choose well rather than to
 // tell the time: to 20 shapes (1 to 64 sequences, up to 4 prefixes of 300 to 16K tokens, 1 to 900 new tokens, every format and head_dim), each with 10 to 300 of the cuts below; what it
 // chose there took 2 % longer than the best on average, 10 % at most (a common length of all splits, by cut_tree's numbers: 13 % and 45 %).
+// One length of splits for sequences' own tokens, one for prefixes, and as many partial results for every row, whose sum is bounded: a chunk of a prompt in the batch leaves the contexts beside it in few splits.
+// One token at 32K beside a chunk of 2048 (8 x 4 x 128, 16 bits) takes 490 us, as two calls 31 + 79; 32 single tokens at 8K beside it 239, 166 + 79; 48 at 300 to 2000 beside a chunk of 700 123, 43 + 25, where
+// the second launch has workgroups for the chunk's rows in every sequence.
 // chain: without a mask a sequence sees half of its new tokens; bounded: rows see only some tokens, how many only the GPU knows: half is taken. At least one unit has work.
 inline GroupCut cut_group(const TreeShape &s, const GroupUnit *units, int n, bool chain, bool bounded, bool shaped, int n_splits, uint64_t ws_bytes, long long n_tok)
 {

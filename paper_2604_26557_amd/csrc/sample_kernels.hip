@@ -4,7 +4,7 @@
 // and prefix sums of any shape give one answer, and adding takes no care.  With tokens ordered by (l from the largest, index), each of the three cuts keeps a beginning of that order: what is kept
 // is every token up to one, the border, in that order, and the token is found in order of indices: sums of tiles, of which one is gone over again.
 //
-// A workgroup has a row. It is read from HBM once, for its maximum, and from L2 after that.
+// A workgroup has a row. It is read from HBM for its maximum, and again for the rest, from the caches where they hold it by then, and where few of the largest are wanted out of registers if it fits them.
 //   Few of the largest (top_k up to 256): no fewer than k tokens reach the k-th largest of the threads' own maxima; a list of those that do is all there is to rank.
 //   More of them, without top_p: a histogram of their number by distance from the maximum says which bin the k-th is in; what is above is kept, the bin is a list, which is ranked.  2 rows of 106775
 //     in 32 bits, the largest 1000: 62 us; 115 by the rounds below.
@@ -13,9 +13,11 @@
 //     few: a row of 32000 of which a dozen have nine tenths of the weight 19.5 -> 17.0 us (with room for 1024 rows of 74 were ranked for longer than it saved: 64 of 128256 43 -> 48).
 //   min_p alone: what is above it is kept.
 //   What these have no room for, and top_k past 256 with top_p: histograms over the whole row, of its keys in the end, in as many rounds as they need.
-// What bounds it: some 30 instructions, most of them in double precision, for every weight where the sum of all is needed, otherwise a pass' latencies.  So few rows of many tokens are shared by several
-// workgroups for the maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 44 us, 75 with a workgroup each.  One row
-// of 32000 in 32 bits with top_k and top_p takes 11.6 us: 3.2 until it is there, 2.6 for the threads' maxima, the rest what threads tell each other, one after the other.
+// What bounds it: where the sum of all is needed, the row's second reading and some 35 vector instructions a token, many in double precision, which hide each other in part (256 rows of 50257 in 32 bits, nothing
+// cut: 24.3 us; 97 MB, 19 us at the rate of a large copy; vector instructions in 67 % of the cycles); otherwise a pass' latencies.  So few rows of many tokens are shared by several workgroups for the
+// maximum and for the weights, a launch each ahead of the rows' own: 64 rows of 128256 in 16 bits with top_p 43.5 us, 75 with a workgroup each (the sum's pass 16.2, vector instructions in 65 % of its
+// cycles; that of what is kept 16.3, in 49 %; launches and what they wait for are the rest).  One row
+// of 32000 in 32 bits with top_k and top_p takes 11.3 us: 3.2 until it is there, 2.6 for the threads' maxima, the rest what threads tell each other, one after the other.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

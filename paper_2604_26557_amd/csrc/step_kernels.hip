@@ -81,8 +81,8 @@ __device__ __forceinline__ unsigned long long wave_sums_to(unsigned long long x)
 
 // Every workgroup sums up all lengths by itself (a few loads a thread), so that one launch does: the first ones go over rows of the table, a wavefront a row or a part of it, the others
 // write the maps. In place it is one workgroup for the table, which looks everything up before it changes it. Bound by the launch and a chain of dependent loads: lengths, sums, the entry
-// of the stack, the table: 64 requests of a token each 5.1 us, 384 with chunks of up to 768 tokens (67K rows of maps) 6.6; with 1024 threads for the 64, what the lengths say read again from memory
-// and sums over LDS they took 12 and 14.
+// of the stack, the table: 64 requests of a token each 5.1 us, 384 with chunks of up to 768 tokens (128K rows of maps) 6.6; with 1024 threads for the 64, what the lengths say read again from memory
+// and sums over LDS they took 12 and 14. In place 10.9 and 44: 16 wavefronts have all rows, and go over them twice.
 template <int MOST, int kThreads>
 __global__ void __launch_bounds__(kThreads) kv_step_tables_kernel(TablesParams p)
 {

@@ -25,13 +25,13 @@
 //   merges while the other reads.
 //
 // kv_group_attn's kernels are the same (GROUP), in translation units of their own, so that kv_tree_attn's keep their registers.  What a row sees is a range of tokens, its mask or chain and a second bound, which
-// the lane with the row's number holds; steps that all rows see in whole are not masked (a prompt of 4096 x 8 heads x 4 x 128 with a cap: 301 -> 248 us).  Splits share out what the rows of a workgroup see, not
+// the lane with the row's number holds; steps that all rows see in whole are not masked (a prompt of 4096 x 8 heads x 4 x 128 with a cap: 301 -> 248 us when this was changed).  Splits share out what the rows of a workgroup see, not
 // what there is, and a chain's last row blocks, which see the most, begin first.  Scores are capped or biased in kernels of their own again (SHAPED: as a run-time choice the others spilled):
-//   a cap takes a rational function for tanh where results are of 32 bits or the cap passes 64, and a sigmoid, an exponential and a reciprocal, otherwise: the prompt takes 215 us without a cap, 306 with the one,
-//   247 with the other (which also spares the running maximum: no score passes the cap);
-//   a bias by distance counts from the farthest position of the rows, a multiplication and an addition a score, and steps go from the nearest tokens to the farthest: 256 us.
-// What bounds them, us per call: HBM, where rows are few (32 requests behind 8K, 172 MB: 42, the second launch of 5 included = 4.1 TB/s); the vector ALU beside the matrix cores, where they are many (the prompt,
-// 137 GFLOP in 215 = 640 TFLOP/s, with the cap 555: its probabilities enter in two parts, which is half as many products again, and matrix cores are busy 37 %).
+//   a cap takes a rational function for tanh where results are of 32 bits or the cap passes 64, and a sigmoid, an exponential and a reciprocal, otherwise: the prompt in fp16, calls one after another, takes 238 us
+//   without a cap, 328 with the one, 268 with the other (a few percent less after a pause of the card: 257);
+//   a bias by distance counts from the farthest position of the rows, a multiplication and an addition a score, and steps go from the nearest tokens to the farthest: 378 -> 290 us when this was changed.
+// What bounds them, us per call: HBM, where rows are few (32 requests behind 8K: 180 MB in the 38.7 of the first launch = 4.6 TB/s, then 5.2 for the second); the vector ALU beside the matrix cores, where they
+// are many (the prompt, 137 GFLOP in 238 = 578 TFLOP/s, with the cap 513: its probabilities enter in two parts, which is half as many products again, and matrix cores are busy 37 %).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -145,7 +145,8 @@ constexpr float kLargeRef = 1048576.f;  // beyond it the rounding of a reference
 template <bool BF16> constexpr float kLiftLog2 = BF16 ? 0.f : 11.f;
 template <bool BF16> constexpr float kMostProbability = BF16 ? 16.f : 32768.f;   // 2^(4 + kLiftLog2)
 // Probabilities as 16-bit operands: parts whose sum is the 32-bit value up to 2^-22 (fp16, two parts) or 2^-16 (bf16, two), or that value (bf16, three).  Two in bf16 go with
-// bf16 results, whose own rounding, to 2^-8, is 256 times as coarse.  One part, rounded, would make the error of a 16-bit result 1.4 times that of its own rounding, for 56.2 instead of 67.3 us
+// bf16 results, whose own rounding, to 2^-8, is 256 times as coarse: 0.43 % of them are the other neighbour of the exact number, with 32-bit arithmetic throughout 0.06 to 0.15 %, and their error is the same to
+// four digits.  32-bit results of fp16 have two parts as well: errors of 1.7e-7 of a result's norm where three parts of bf16 have 1.2e-7.  One part, rounded, would make the error of a 16-bit result 1.4 times that of its own rounding, for 56.2 instead of 67.3 us
 // with 64 drafted tokens over 32K x 8 heads x 128 in 8 bits, 48.2 instead of 49.9 in a ragged batch of 8, 49.5 either way where HBM is the limit.
 template <bool BF16, bool F32> constexpr int kParts = BF16 && F32 ? 3 : 2;
 
