@@ -758,7 +758,7 @@ size_t kv_group_attn_workspace(const kv_plan_t *plan, int n_tok, int max_len);
  * and tokens[row] is the smallest index i with (sum of w_j over kept j <= i) > u * (sum over all kept).  probs[row] = w of it / sum over all kept.
  * Not T > 0: the largest (the first of equal ones), probability 1.  Infinities of -1 are never drawn.  A row with a NaN or an infinity of +1, or without
  * any finite logit, yields token -1 and probability 0.  u is taken as within [0, 1).
- * Sums are of w held as integers, units of 2^-s with s = 62 - log2(n_vocab) rounded up, at most 51 (45 for 128K), so that they do not depend on an order; w is computed in double precision.
+ * Sums are of w held as integers, units of 2^-s with s = 62 - log2(n_vocab) rounded up, at most 51 (45 for 128K), so that they do not depend on an order: what weighs less than half a unit is never drawn. w is computed in double precision.
  * workspace: device, 16-byte aligned, >= kv_sample_workspace() bytes (else KV_ENOSPC); nothing in it has to start at zero. Two calls that overlap in time need a workspace each.
  */
 #define KV_F32 2 /* logits only */
